@@ -270,6 +270,105 @@ ccl_status ccl_gemm_splitk_noalloc(ccl_plan_t plan, float alpha, const void* A_c
 ccl_status ccl_gemm_rowmajor(ccl_plan_t plan, const void* A, const void* B, void* C, int remap,
                              void* stream);
 
+/* ---------------------------------------------------------------------------
+ * FFN operators around the GEMM. As above, the caller owns all device memory,
+ * calls are asynchronous on `stream`, and on an error nothing is launched.
+ * ------------------------------------------------------------------------- */
+
+/* z, max(z, 0), the tanh form of GELU, or z / (1 + exp(-z)). NaN stays NaN. */
+typedef enum { CCL_ACT_NONE = 0, CCL_ACT_RELU = 1, CCL_ACT_GELU = 2, CCL_ACT_SILU = 3 } ccl_activation;
+
+/* How A, B, C and the matrices of an epilogue are stored: all in the plan's
+ * CCL layouts, or all plain row-major without padding between rows (as in
+ * ccl_gemm_rowmajor with remap = 1). */
+typedef enum { CCL_LAYOUT_CCL = 0, CCL_LAYOUT_ROWMAJOR = 1 } ccl_operand_layout;
+
+/*
+ * Layout of a bf16 M x cols matrix on the plan's grid and page size: the
+ * matrices of a gated epilogue, which have N / 2 or 2 N columns (cols = N
+ * gives C's layout, cols = K that of a bf16 A).
+ * Errors: CCL_ERR_INVALID_ARG (NULL argument, cols not positive, not a
+ * multiple of the grid's columns, or 2^31 and more).
+ */
+ccl_status ccl_plan_matrix_layout(ccl_plan_t plan, int64_t cols, ccl_layout* out);
+
+/*
+ * Matrix product with bias, activation and residual in its epilogue:
+ *   Z = alpha A B + bias          (M x N, fp32)
+ *   C = act(Z) + beta R           (gated = 0: M x N)
+ *   C = act(Zg) * Zu + beta R     (gated = 1: M x N / 2)
+ * Gated: the columns of B (and of bias and Z) alternate in groups of 16, the
+ * gate columns j .. j + 15 at 2 j .. 2 j + 15 and their up columns behind
+ * them, so that one tile holds both; a weight is stored so once. Everything up
+ * to C is formed in fp32 and rounded to bf16 once (nearest even).
+ * Rows `rows` .. M - 1 (a ragged number of tokens in whole tiles) come out as
+ * zeros in C and in preact, whatever A and R hold there.
+ */
+typedef struct ccl_epilogue {
+  ccl_activation activation;
+  int32_t gated;               /* 0 or 1 */
+  ccl_operand_layout layout;
+  ccl_dtype bias_type;         /* CCL_DT_FP32 or CCL_DT_BF16 (read only with a bias) */
+  float alpha, beta;
+  int64_t rows;                /* valid rows, 0 .. M */
+  const void* bias;            /* N elements, 16-byte aligned, or NULL */
+  const void* residual;        /* bf16, laid out as C, or NULL; may be C itself */
+  void* preact;                /* bf16 M x N: Z rounded, for the backward pass, or NULL */
+} ccl_epilogue;
+
+/*
+ * ccl_gemm_fused_workspace: in: *splits = K ranges per tile (1..16, or 0 to
+ * choose, as ccl_gemm_splitk_workspace); out: the ranges used and the device
+ * workspace of ccl_gemm_fused for that request in bytes, which is not zero
+ * with one range either where the plan's GEMM kernel has no fused epilogue
+ * (the product's fp32 tiles then pass through it).
+ *
+ * ccl_gemm_fused: the product and epilogue above, for plans with a bf16 C
+ * (A and B bf16 or fp8 E4M3). All matrices 16-byte aligned; none may overlap
+ * another, except residual = C. The workspace (16-byte aligned; may be NULL
+ * where none is needed) is not read on entry, and calls that share one must be
+ * ordered on one stream.
+ * Errors: as ccl_gemm_splitk; CCL_ERR_INVALID_ARG also for a NULL epilogue,
+ * an unknown activation, layout or bias type, gated not 0 or 1, rows outside
+ * 0..M, or a workspace that is missing or too small;
+ * CCL_ERR_MISALIGNED_POINTER; CCL_ERR_UNSUPPORTED for an fp32 C.
+ */
+ccl_status ccl_gemm_fused_workspace(ccl_plan_t plan, ccl_operand_layout layout, int* splits,
+                                    int64_t* workspace_bytes);
+ccl_status ccl_gemm_fused(ccl_plan_t plan, const ccl_epilogue* epilogue, const void* A, const void* B,
+                          void* C, int splits, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * The gradient through that epilogue, in the epilogue of the product that
+ * gives the gradient of C's activations, D = alpha A B (M x N; dY times the
+ * stored transpose of the next weight):
+ *   dZ = D * act'(Z)                               (gated = 0: M x N)
+ *   dZg = D * Zu * act'(Zg), dZu = D * act(Zg)     (gated = 1: M x 2 N)
+ * with Z (and dZ) interleaved as above. dbias, fp32, one element per column of
+ * dZ, takes the column sums of the unrounded dZ, added up in a fixed order (the
+ * same bits every time). Rows `rows` .. M - 1 of dZ come out as zeros and add
+ * nothing. dZ may be preact itself.
+ * act'(0) = 0 for CCL_ACT_RELU.
+ */
+typedef struct ccl_epilogue_grad {
+  ccl_activation activation;
+  int32_t gated;
+  ccl_operand_layout layout;
+  float alpha;
+  int64_t rows;
+  const void* preact;          /* bf16, laid out as dZ; not needed (NULL) with
+                                  CCL_ACT_NONE and gated = 0 */
+  float* dbias;                /* 16-byte aligned, or NULL */
+} ccl_epilogue_grad;
+
+/* Workspace for ccl_gemm_fused_grad (dbias: 1 when it is asked for), and the
+ * call. Errors as ccl_gemm_fused. */
+ccl_status ccl_gemm_fused_grad_workspace(ccl_plan_t plan, ccl_operand_layout layout, int gated, int dbias,
+                                         int64_t* workspace_bytes);
+ccl_status ccl_gemm_fused_grad(ccl_plan_t plan, const ccl_epilogue_grad* epilogue, const void* A,
+                               const void* B, void* dZ, void* workspace, int64_t workspace_bytes,
+                               void* stream);
+
 /* Flags of ccl_remote_bytes and ccl_remote_bytes_l2. */
 #define CCL_TRAFFIC_A_TRANS 1   /* A is stored transposed (e.g. H held for A = H^T) */
 #define CCL_TRAFFIC_B_TRANS 2   /* B is stored transposed */

@@ -9,5 +9,8 @@ from .ccl import (CCL_A, CCL_B, CCL_C, CCL_PLACE_RR, CCL_PLACE_COARSE, CCL_PLACE
                   CCL_DT_BF16, CCL_DT_FP8_E4M3, CCL_DT_FP32,
                   CCLError, ccl_plan, ccl_plan_typed, ccl_plan_grid, ccl_plan_layout, ccl_pack, ccl_unpack,
                   ccl_gemm, ccl_gemm_scaled, ccl_gemm_splitk_workspace, ccl_gemm_splitk,
+                  CCL_ACT_NONE, CCL_ACT_RELU, CCL_ACT_GELU, CCL_ACT_SILU, CCL_LAYOUT_CCL, CCL_LAYOUT_ROWMAJOR,
+                  ccl_plan_matrix_layout, ccl_gemm_fused_workspace, ccl_gemm_fused,
+                  ccl_gemm_fused_grad_workspace, ccl_gemm_fused_grad,
                   ccl_gemm_rowmajor, ccl_remote_bytes, ccl_remote_bytes_l2, ccl_status_string,
                   ccl_last_error)

@@ -30,6 +30,7 @@ SOURCES = [
     ("host/plan.cpp", "host"),       # plain C++, no HIP
     ("host/l2sim.cpp", "host"),
     ("ccl_api.cpp", "hip"),
+    ("ccl_ops.cpp", "hip"),
     ("kernels/pack.hip", "hip"),
     ("kernels/gemm.hip", "hip"),
 ]

@@ -27,7 +27,9 @@ STATUS_NAMES = {0: "CCL_OK", 1: "CCL_ERR_INVALID_ARG", 2: "CCL_ERR_UNALIGNED_PAR
 # every symbol include/ccl.h declares
 EXPORTED = ("ccl_plan", "ccl_plan_typed", "ccl_plan_destroy", "ccl_plan_grid", "ccl_plan_layout",
             "ccl_pack", "ccl_unpack", "ccl_gemm", "ccl_gemm_scaled", "ccl_gemm_splitk_workspace",
-            "ccl_gemm_splitk", "ccl_gemm_splitk_noalloc", "ccl_gemm_rowmajor", "ccl_remote_bytes", "ccl_remote_bytes_l2", "ccl_status_string", "ccl_last_error",
+            "ccl_gemm_splitk", "ccl_gemm_splitk_noalloc", "ccl_gemm_rowmajor",
+            "ccl_plan_matrix_layout", "ccl_gemm_fused_workspace", "ccl_gemm_fused", "ccl_gemm_fused_grad_workspace",
+            "ccl_gemm_fused_grad", "ccl_remote_bytes", "ccl_remote_bytes_l2", "ccl_status_string", "ccl_last_error",
             "ccl_debug_tile_of_wg", "ccl_debug_gemm_config", "ccl_debug_dispatch",
             "ccl_debug_gemm_timeline", "ccl_debug_launch", "ccl_debug_launch_tile_of_wg",
             "ccl_debug_launch_dispatch", "ccl_debug_launch_timeline")
@@ -69,6 +71,19 @@ class _Launch(ctypes.Structure):
                [(n, ctypes.c_int) for n in ("tile_rows", "tile_cols", "waves", "k_ranges", "ragged", "far", "stream_b", "c_nt")]
 
 
+class _Epilogue(ctypes.Structure):
+    _fields_ = [("activation", ctypes.c_int), ("gated", ctypes.c_int32), ("layout", ctypes.c_int),
+                ("bias_type", ctypes.c_int), ("alpha", ctypes.c_float), ("beta", ctypes.c_float),
+                ("rows", ctypes.c_int64), ("bias", ctypes.c_void_p), ("residual", ctypes.c_void_p),
+                ("preact", ctypes.c_void_p)]
+
+
+class _EpilogueGrad(ctypes.Structure):
+    _fields_ = [("activation", ctypes.c_int), ("gated", ctypes.c_int32), ("layout", ctypes.c_int),
+                ("alpha", ctypes.c_float), ("rows", ctypes.c_int64), ("preact", ctypes.c_void_p),
+                ("dbias", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -101,6 +116,11 @@ def library() -> ctypes.CDLL:
         "ccl_gemm_splitk": [vp, ctypes.c_float, vp, vp, ctypes.c_float, vp, i32, vp, i64, vp],
         "ccl_gemm_splitk_noalloc": [vp, ctypes.c_float, vp, vp, ctypes.c_float, vp, i32, vp],
         "ccl_gemm_rowmajor": [vp, vp, vp, vp, i32, vp],
+        "ccl_plan_matrix_layout": [vp, i64, ctypes.POINTER(_Layout)],
+        "ccl_gemm_fused_workspace": [vp, i32, ctypes.POINTER(i32), ctypes.POINTER(i64)],
+        "ccl_gemm_fused": [vp, ctypes.POINTER(_Epilogue), vp, vp, vp, i32, vp, i64, vp],
+        "ccl_gemm_fused_grad_workspace": [vp, i32, i32, i32, ctypes.POINTER(i64)],
+        "ccl_gemm_fused_grad": [vp, ctypes.POINTER(_EpilogueGrad), vp, vp, vp, vp, i64, vp],
         "ccl_remote_bytes": [vp, i32, i32, ctypes.POINTER(_Traffic)],
         "ccl_remote_bytes_l2": [vp, i32, i32, ctypes.POINTER(_L2Config), ctypes.POINTER(_L2Traffic)],
         "ccl_debug_tile_of_wg": [vp, i64, ctypes.POINTER(i32), ctypes.POINTER(i64), ctypes.POINTER(i64)],
@@ -253,6 +273,62 @@ def ccl_gemm_splitk_noalloc(plan: Plan, alpha: float, A_ccl, B_ccl, beta: float,
 
 def ccl_gemm_rowmajor(plan: Plan, A, B, C, remap: int, stream=None) -> None:
     _check(library().ccl_gemm_rowmajor(plan, _ptr(A), _ptr(B), _ptr(C), remap, _stream(stream)))
+
+
+CCL_ACT_NONE, CCL_ACT_RELU, CCL_ACT_GELU, CCL_ACT_SILU = 0, 1, 2, 3
+CCL_LAYOUT_CCL, CCL_LAYOUT_ROWMAJOR = 0, 1
+
+
+def ccl_plan_matrix_layout(plan: Plan, cols: int) -> Layout:
+    """Layout of a bf16 M x cols matrix on the plan's grid."""
+    out = _Layout()
+    _check(library().ccl_plan_matrix_layout(plan, cols, ctypes.byref(out)))
+    return Layout(*(getattr(out, f) for f, _ in _Layout._fields_))
+
+
+def ccl_gemm_fused_workspace(plan: Plan, splits: int = 1, *, layout: int = CCL_LAYOUT_CCL) -> tuple[int, int]:
+    """(K ranges used, workspace bytes) of ccl_gemm_fused for a requested split count (0: choose)."""
+    s = ctypes.c_int(splits)
+    nbytes = ctypes.c_int64(0)
+    _check(library().ccl_gemm_fused_workspace(plan, layout, ctypes.byref(s), ctypes.byref(nbytes)))
+    return s.value, nbytes.value
+
+
+def _bias_type(bias, bias_type):
+    """The element type of a bias: as given, else a tensor's own (CCL_DT_FP32 for an address)."""
+    if bias_type is not None or bias is None or isinstance(bias, int):
+        return CCL_DT_FP32 if bias_type is None else bias_type
+    # -1, which the library refuses, for a tensor that is neither
+    return {"torch.float32": CCL_DT_FP32, "torch.bfloat16": CCL_DT_BF16}.get(str(bias.dtype), -1)
+
+
+def ccl_gemm_fused(plan: Plan, A, B, C, *, activation: int = CCL_ACT_NONE, gated: bool = False, bias=None,
+                   bias_type: int | None = None, residual=None, beta: float = 1.0, preact=None, alpha: float = 1.0,
+                   rows: int | None = None, layout: int = CCL_LAYOUT_CCL, splits: int = 1, workspace=None,
+                   workspace_bytes: int = 0, stream=None) -> None:
+    """C = act(alpha A B + bias) + beta residual, gated or not; preact takes alpha A B + bias."""
+    e = _Epilogue(activation, int(gated), layout, _bias_type(bias, bias_type), alpha, beta,
+                  plan.args[0] if rows is None else rows, _ptr(bias), _ptr(residual), _ptr(preact))
+    _check(library().ccl_gemm_fused(plan, ctypes.byref(e), _ptr(A), _ptr(B), _ptr(C), splits, _ptr(workspace),
+                                    workspace_bytes, _stream(stream)))
+
+
+def ccl_gemm_fused_grad_workspace(plan: Plan, *, gated: bool = False, dbias: bool = False,
+                                  layout: int = CCL_LAYOUT_CCL) -> int:
+    """Workspace bytes of ccl_gemm_fused_grad."""
+    nbytes = ctypes.c_int64(0)
+    _check(library().ccl_gemm_fused_grad_workspace(plan, layout, int(gated), int(dbias), ctypes.byref(nbytes)))
+    return nbytes.value
+
+
+def ccl_gemm_fused_grad(plan: Plan, A, B, preact, dZ, *, activation: int = CCL_ACT_NONE, gated: bool = False,
+                        dbias=None, alpha: float = 1.0, rows: int | None = None, layout: int = CCL_LAYOUT_CCL,
+                        workspace=None, workspace_bytes: int = 0, stream=None) -> None:
+    """dZ = (alpha A B) * act'(preact), gated or not; dbias takes its column sums."""
+    e = _EpilogueGrad(activation, int(gated), layout, alpha, plan.args[0] if rows is None else rows, _ptr(preact),
+                      _ptr(dbias))
+    _check(library().ccl_gemm_fused_grad(plan, ctypes.byref(e), _ptr(A), _ptr(B), _ptr(dZ), _ptr(workspace),
+                                         workspace_bytes, _stream(stream)))
 
 
 CCL_TRAFFIC_A_TRANS, CCL_TRAFFIC_B_TRANS, CCL_TRAFFIC_C_READ = 1, 2, 4

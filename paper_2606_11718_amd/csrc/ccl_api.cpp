@@ -9,17 +9,17 @@
 #include <string>
 
 #include "../../include/ccl.h"
+#include "ccl_api.hpp"
 #include "host/l2sim.hpp"
 #include "host/plan.hpp"
 #include "kernels/kernels.hpp"
 
-struct ccl_plan_s {
-  ccl::Plan plan;
-};
-
 namespace {
-
 thread_local std::string g_last_error;
+}  // namespace
+
+namespace ccl {
+namespace api {
 
 ccl_status fail(ccl_status s, const std::string& msg) {
   g_last_error = msg;
@@ -35,12 +35,12 @@ ccl_status from(ccl::Status s, const std::string& msg) {
   return s == ccl::Status::OK ? ok() : fail(static_cast<ccl_status>(s), msg);
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 // gfx950 check, once per device.
+namespace {
 constexpr int kMaxDevices = 64;
 std::once_flag g_dev_once[kMaxDevices];
 bool g_dev_ok[kMaxDevices];
+}  // namespace
 
 ccl_status check_device() {
   int dev = 0;
@@ -60,8 +60,6 @@ ccl_status hip_status(hipError_t e, const char* what) {
   if (e != hipSuccess) return fail(CCL_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
   return ok();
 }
-
-bool valid_op(ccl_operand op) { return op == CCL_A || op == CCL_B || op == CCL_C; }
 
 // Whether every element the GEMM kernel can touch through this addressing
 // lies inside buffers of a_bytes, b_bytes and c_bytes (the kernel's own
@@ -92,6 +90,13 @@ bool offsets_fit(const ccl::Plan& p, const ccl::OperandAddr& a, const ccl::Opera
   return 255 * (int64_t)a.ld * e + 256 < lim && 127 * (int64_t)b.ld * e + 256 * e < lim;
 }
 
+}  // namespace api
+}  // namespace ccl
+
+using namespace ccl::api;
+
+namespace {
+bool valid_op(ccl_operand op) { return op == CCL_A || op == CCL_B || op == CCL_C; }
 }  // namespace
 
 extern "C" {

@@ -1,0 +1,152 @@
+// C ABI of the FFN operators around the GEMM (declarations and contracts:
+// include/ccl.h).
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <string>
+
+#include "../../include/ccl.h"
+#include "ccl_api.hpp"
+#include "host/plan.hpp"
+#include "kernels/kernels.hpp"
+
+using namespace ccl::api;
+
+namespace {
+
+constexpr int64_t kMaxGrid = 0x7fffffff;
+
+bool valid_layout(int l) { return l == CCL_LAYOUT_CCL || l == CCL_LAYOUT_ROWMAJOR; }
+
+// What both directions check of the plan, the epilogue's fields and the
+// launch; on CCL_OK *form is what to launch.
+ccl_status check_fused(ccl_plan_t plan, int layout, int activation, int gated, int64_t rows, int splits, bool grad,
+                       bool dbias, ccl::FusedForm* form) {
+  const ccl::Plan& p = plan->plan;
+  if (!valid_layout(layout)) return fail(CCL_ERR_INVALID_ARG, "layout must be CCL_LAYOUT_CCL or CCL_LAYOUT_ROWMAJOR");
+  if (!ccl::valid_act(activation)) return fail(CCL_ERR_INVALID_ARG, "unknown activation");
+  if (gated != 0 && gated != 1) return fail(CCL_ERR_INVALID_ARG, "gated must be 0 or 1");
+  if (rows < 0 || rows > p.M) return fail(CCL_ERR_INVALID_ARG, "rows must be in 0..M");
+  if (!p.gemm.supported) return fail(CCL_ERR_UNSUPPORTED, p.gemm.why_unsupported);
+  if (p.c_type != ccl::DT_BF16) return fail(CCL_ERR_UNSUPPORTED, "the fused epilogues write a bf16 C");
+  if (splits < 1 || splits > ccl::kMaxSplits) return fail(CCL_ERR_INVALID_ARG, "splits must be in 1..16");
+  if (ccl::splitk_workgroups(p, splits) > kMaxGrid || ccl::splitk_reduce_workgroups(p) > kMaxGrid)
+    return fail(CCL_ERR_UNSUPPORTED, "grid exceeds the launch limit");
+  if (grad && gated && 2 * p.N > kMaxGrid) return fail(CCL_ERR_UNSUPPORTED, "2 N exceeds 31 bits");
+  *form = ccl::fused_form(p, layout == CCL_LAYOUT_ROWMAJOR, splits, grad, gated == 1, dbias);
+  if (!offsets_fit(p, form->a, form->b)) return fail(CCL_ERR_UNSUPPORTED, "rows too long for 32-bit in-tile offsets");
+  return CCL_OK;
+}
+
+ccl_status check_workspace(int64_t need, const void* workspace, int64_t bytes) {
+  if (need == 0) return CCL_OK;
+  if (!workspace) return fail(CCL_ERR_INVALID_ARG, "NULL workspace");
+  if (bytes < need) return fail(CCL_ERR_INVALID_ARG, "workspace smaller than the " + std::to_string(need) + " bytes reported");
+  if (!aligned16(workspace)) return fail(CCL_ERR_MISALIGNED_POINTER, "the workspace must be 16-byte aligned");
+  return CCL_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+ccl_status ccl_plan_matrix_layout(ccl_plan_t plan, int64_t cols, ccl_layout* out) {
+  if (!plan || !out) return fail(CCL_ERR_INVALID_ARG, "NULL argument");
+  if (cols < 1 || cols > kMaxGrid || cols % plan->plan.Gc != 0)
+    return fail(CCL_ERR_INVALID_ARG, "cols must be a positive multiple of the grid's columns below 2^31");
+  const ccl::Layout l = ccl::matrix_layout(plan->plan, cols);
+  out->rows = l.rows;
+  out->cols = l.cols;
+  out->grid_r = l.grid_r;
+  out->grid_c = l.grid_c;
+  out->block_rows = l.block_rows;
+  out->block_cols = l.block_cols;
+  out->strip_bytes = l.strip_bytes;
+  out->strip_stride_bytes = l.strip_stride_bytes;
+  out->total_bytes = l.total_bytes;
+  out->elem_bytes = l.elem_bytes;
+  return ok();
+}
+
+ccl_status ccl_gemm_fused_workspace(ccl_plan_t plan, ccl_operand_layout layout, int* splits,
+                                    int64_t* workspace_bytes) {
+  if (!plan || !splits || !workspace_bytes) return fail(CCL_ERR_INVALID_ARG, "NULL argument");
+  if (*splits < 0 || *splits > ccl::kMaxSplits)
+    return fail(CCL_ERR_INVALID_ARG, "splits must be 0 (choose) or in 1..16");
+  const int s = *splits == 0 ? ccl::recommended_splits(plan->plan) : *splits;
+  ccl::FusedForm f;
+  if (ccl_status st = check_fused(plan, layout, CCL_ACT_NONE, 0, 0, s, false, false, &f)) return st;
+  *splits = f.gemm.splits;
+  *workspace_bytes = f.workspace_bytes;
+  return ok();
+}
+
+ccl_status ccl_gemm_fused(ccl_plan_t plan, const ccl_epilogue* e, const void* A, const void* B, void* C,
+                          int splits, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!plan || !e || !A || !B || !C) return fail(CCL_ERR_INVALID_ARG, "NULL argument");
+  ccl::FusedForm f;
+  if (ccl_status s = check_fused(plan, e->layout, e->activation, e->gated, e->rows, splits, false, false, &f)) return s;
+  if (e->bias && e->bias_type != CCL_DT_FP32 && e->bias_type != CCL_DT_BF16)
+    return fail(CCL_ERR_INVALID_ARG, "the bias must be fp32 or bf16");
+  if (!aligned16(A) || !aligned16(B) || !aligned16(C) || !aligned16(e->bias) || !aligned16(e->residual) ||
+      !aligned16(e->preact))
+    return fail(CCL_ERR_MISALIGNED_POINTER, "A, B, C, bias, residual and preact must be 16-byte aligned");
+  if (ccl_status s = check_workspace(f.workspace_bytes, workspace, workspace_bytes)) return s;
+  if (ccl_status s = check_device()) return s;
+  ccl::FusedCall c;
+  c.A = A;
+  c.B = B;
+  c.C = C;
+  c.bias = e->bias;
+  c.bias_f32 = e->bias_type == CCL_DT_FP32;
+  c.R = e->residual;
+  c.Zout = e->preact;
+  c.rowmajor = e->layout == CCL_LAYOUT_ROWMAJOR;
+  c.gated = e->gated == 1;
+  c.act = e->activation;
+  c.alpha = e->alpha;
+  c.beta = e->beta;
+  c.rows = e->rows;
+  return hip_status(ccl::launch_gemm_fused(plan->plan, c, splits, workspace, static_cast<hipStream_t>(stream)),
+                    "fused gemm launch");
+}
+
+ccl_status ccl_gemm_fused_grad_workspace(ccl_plan_t plan, ccl_operand_layout layout, int gated, int dbias,
+                                         int64_t* workspace_bytes) {
+  if (!plan || !workspace_bytes) return fail(CCL_ERR_INVALID_ARG, "NULL argument");
+  if (dbias != 0 && dbias != 1) return fail(CCL_ERR_INVALID_ARG, "dbias must be 0 or 1");
+  ccl::FusedForm f;
+  if (ccl_status s = check_fused(plan, layout, CCL_ACT_NONE, gated, 0, 1, true, dbias == 1, &f)) return s;
+  *workspace_bytes = f.workspace_bytes;
+  return ok();
+}
+
+ccl_status ccl_gemm_fused_grad(ccl_plan_t plan, const ccl_epilogue_grad* e, const void* A, const void* B, void* dZ,
+                               void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!plan || !e || !A || !B || !dZ) return fail(CCL_ERR_INVALID_ARG, "NULL argument");
+  ccl::FusedForm f;
+  if (ccl_status s = check_fused(plan, e->layout, e->activation, e->gated, e->rows, 1, true, e->dbias != nullptr, &f))
+    return s;
+  const bool linear = e->activation == CCL_ACT_NONE && e->gated == 0;
+  if (!e->preact && !linear) return fail(CCL_ERR_INVALID_ARG, "NULL preact");
+  if (!aligned16(A) || !aligned16(B) || !aligned16(dZ) || !aligned16(e->preact) || !aligned16(e->dbias))
+    return fail(CCL_ERR_MISALIGNED_POINTER, "A, B, dZ, preact and dbias must be 16-byte aligned");
+  if (ccl_status s = check_workspace(f.workspace_bytes, workspace, workspace_bytes)) return s;
+  if (ccl_status s = check_device()) return s;
+  ccl::FusedCall c;
+  c.A = A;
+  c.B = B;
+  c.C = dZ;
+  c.Zin = linear ? nullptr : e->preact;
+  c.dbias = e->dbias;
+  c.rowmajor = e->layout == CCL_LAYOUT_ROWMAJOR;
+  c.grad = true;
+  c.gated = e->gated == 1;
+  c.act = e->activation;
+  c.alpha = e->alpha;
+  c.rows = e->rows;
+  return hip_status(ccl::launch_gemm_fused(plan->plan, c, 1, workspace, static_cast<hipStream_t>(stream)),
+                    "fused gradient gemm launch");
+}
+
+}  // extern "C"

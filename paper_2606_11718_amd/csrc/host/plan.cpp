@@ -700,4 +700,34 @@ GemmForm gemm_form(const Plan& p, const OperandAddr& a, const OperandAddr& b, bo
   return f;
 }
 
+Layout matrix_layout(const Plan& p, int64_t cols) {
+  return make_layout(p.M, cols, p.Gr, p.Gc, p.page, 2);
+}
+
+OperandAddr matrix_addressing(const Plan& p, int64_t cols, bool rowmajor) {
+  if (rowmajor) return {p.part_rows() * cols, cols / p.Gc, (int32_t)cols, 0};
+  const int64_t s = matrix_layout(p, cols).strip_stride_bytes / 2;
+  return {p.Gc * s, s, (int32_t)(cols / p.Gc), 0};
+}
+
+FusedForm fused_form(const Plan& plan, bool rowmajor, int splits, bool grad, bool gated, bool dbias) {
+  Plan p = plan;
+  p.gemm.wide_n = 0;      // the workspace and the reduce are the plan tile's
+  FusedForm f;
+  OperandAddr c;
+  if (rowmajor) rowmajor_addressing(p, &f.a, &f.b, &c);
+  else ccl_addressing(p, &f.a, &f.b, &c);
+  f.gemm = gemm_form(p, f.a, f.b, true, splits);
+  f.z_cols = grad && gated ? 2 * p.N : p.N;
+  f.c_cols = grad ? f.z_cols : gated ? p.N / 2 : p.N;
+  f.z = matrix_addressing(p, f.z_cols, rowmajor);
+  f.c = matrix_addressing(p, f.c_cols, rowmajor);
+  f.c_nt = f.gemm.c_nt;
+  const int md = f.gemm.kernel == GemmKernel::FP8 ? 32 : 16;
+  f.sum_rows = md;
+  f.partial_bytes = (int64_t)p.G * p.gemm.tiles_m * p.gemm.tiles_n * f.gemm.splits * p.gemm.tile_m * p.gemm.tile_n * 4;
+  f.workspace_bytes = f.partial_bytes + (dbias ? p.M / f.sum_rows * f.z_cols * 4 : 0);
+  return f;
+}
+
 }  // namespace ccl

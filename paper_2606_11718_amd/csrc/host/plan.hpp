@@ -167,6 +167,30 @@ GemmForm gemm_form(const Plan& p, const OperandAddr& a, const OperandAddr& b, bo
                    bool reads_c = false);
 const char* kernel_name(GemmKernel k);
 
+// Activations of the FFN operators.
+enum Activation { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };
+inline bool valid_act(int a) { return a >= ACT_NONE && a <= ACT_SILU; }
+
+// Layout of a bf16 M x cols matrix on the plan's grid and pages (cols a
+// multiple of the grid's columns), and its addressing by the kernels, in CCL
+// or row-major.
+Layout matrix_layout(const Plan& p, int64_t cols);
+OperandAddr matrix_addressing(const Plan& p, int64_t cols, bool rowmajor);
+
+// What a fused GEMM launches: the GEMM's form, the operands' addressing and
+// the workspace. c: C (N columns, N / 2 gated) or dZ; z: the pre-activations,
+// z_cols columns (N; 2 N for a gated gradient).
+struct FusedForm {
+  GemmForm gemm;
+  OperandAddr a, b, c, z;
+  int64_t z_cols = 0, c_cols = 0;
+  int sum_rows = 0;                 // rows of one block of column sums
+  bool c_nt = false;
+  int64_t partial_bytes = 0;        // fp32 partial tiles
+  int64_t workspace_bytes = 0;      // with the column sums
+};
+FusedForm fused_form(const Plan& p, bool rowmajor, int splits, bool grad, bool gated, bool dbias);
+
 // tile_of_wg of an unsplit ccl_gemm's own launch.
 void launch_tile_of_wg(const Plan& p, int64_t wg, int* xcd, int64_t* tile_m, int64_t* tile_n);
 

@@ -46,6 +46,7 @@
 #include <mutex>
 #include <type_traits>
 
+#include "activation.hpp"
 #include "kernels.hpp"
 
 namespace ccl {
@@ -680,6 +681,8 @@ __global__ void __launch_bounds__(256) splitk_reduce_kernel(GemmParams p) {
   const int64_t c_tile = pr * p.c.part + pc * p.c.slice + (int64_t)(ti * BM) * p.c.ld + tj * BN;
   store4(p, c_tile + (int64_t)m * p.c.ld + n, o);
 }
+
+#include "fused_epilogue.hpp"
 
 // Writes one wave's phase timeline once its C stores have been issued (not
 // waited for, as in the ordinary launch): words 0-3 real-time counter
@@ -2853,15 +2856,12 @@ static hipError_t launch_splitk_reduce(const Plan& p, GemmParams gp, int md, int
   return hipGetLastError();
 }
 
-hipError_t launch_gemm(const Plan& p, const void* A, const void* B, void* C,
-                       const OperandAddr& a, const OperandAddr& b, const OperandAddr& c,
-                       bool remap, float alpha, float beta, int splits, float* ws,
-                       hipStream_t stream, uint64_t* timeline) {
-  if (splits < 1 || (splits > 1 && (!remap || !ws))) return hipErrorInvalidValue;
-  const GemmForm f = gemm_form(p, a, b, remap, splits, beta != 0.f);
-  if (timeline && (p.ab_type != DT_BF16 || f.splits > 1)) return hipErrorInvalidValue;   // bf16 kernels only
-  GemmParams gp;
-  gp.timeline = timeline;
+// The kernel arguments of launch form f.
+static void gemm_params(const Plan& p, const GemmForm& f, const void* A, const void* B, void* C,
+                        const OperandAddr& a, const OperandAddr& b, const OperandAddr& c, bool remap,
+                        GemmParams* out) {
+  GemmParams& gp = *out;
+  gp.timeline = nullptr;
   gp.A = static_cast<const uint16_t*>(A);
   gp.B = static_cast<const uint16_t*>(B);
   gp.C = C;
@@ -2886,15 +2886,23 @@ hipError_t launch_gemm(const Plan& p, const void* A, const void* B, void* C,
   }
   gp.splits_total = f.splits;
   gp.c_nt = f.c_nt ? 1 : 0;
-  gp.ws = f.splits > 1 ? ws : nullptr;
+  gp.ws = nullptr;
   gp.remap = remap ? 1 : 0;
   gp.grid_r = p.Gr;
-  gp.alpha = alpha;
-  gp.beta = beta;
-  gp.epi = beta != 0.f ? 2 : (alpha != 1.f ? 1 : 0);
+  gp.alpha = 1.f;
+  gp.beta = 0.f;
+  gp.epi = 0;
+}
+
+// The launch of form f's kernel. On return md and wgm are its MFMA tile and
+// the rows of its wave grid, for the reduce of its partials.
+static hipError_t launch_form(const GemmForm& f, const GemmParams& gp, hipStream_t stream, int* md_out,
+                              int* wgm_out) {
   const dim3 grid((unsigned)f.workgroups);
   // MFMA tile and rows of the wave grid, for the reduce of split-K partials
-  int md = 16, wgm = 2;
+  int &md = *md_out, &wgm = *wgm_out;
+  md = 16;
+  wgm = 2;
   const auto tile = [&](int m, int n) { return f.tile_m == m && f.tile_n == n; };
   switch (f.kernel) {
     case GemmKernel::FP8P:
@@ -2981,8 +2989,101 @@ hipError_t launch_gemm(const Plan& p, const void* A, const void* B, void* C,
 #undef CCL_LAUNCH
       break;
   }
-  return f.splits > 1 ? launch_splitk_reduce(p, gp, md, f.waves, stream, wgm) : hipGetLastError();
+  return hipGetLastError();
 }
+
+hipError_t launch_gemm(const Plan& p, const void* A, const void* B, void* C,
+                       const OperandAddr& a, const OperandAddr& b, const OperandAddr& c,
+                       bool remap, float alpha, float beta, int splits, float* ws,
+                       hipStream_t stream, uint64_t* timeline) {
+  if (splits < 1 || (splits > 1 && (!remap || !ws))) return hipErrorInvalidValue;
+  const GemmForm f = gemm_form(p, a, b, remap, splits, beta != 0.f);
+  if (timeline && (p.ab_type != DT_BF16 || f.splits > 1)) return hipErrorInvalidValue;   // bf16 kernels only
+  GemmParams gp;
+  gemm_params(p, f, A, B, C, a, b, c, remap, &gp);
+  gp.timeline = timeline;
+  gp.ws = f.splits > 1 ? ws : nullptr;
+  gp.alpha = alpha;
+  gp.beta = beta;
+  gp.epi = beta != 0.f ? 2 : (alpha != 1.f ? 1 : 0);
+  int md, wgm;
+  const hipError_t e = launch_form(f, gp, stream, &md, &wgm);
+  if (e != hipSuccess || f.splits == 1) return e;
+  return launch_splitk_reduce(p, gp, md, f.waves, stream, wgm);
+}
+
+// The workspace form of the fused epilogue: partials, then the reduce.
+template <bool GRAD>
+static hipError_t launch_fused_reduce(const Plan& p, FusedParams fp, int md, int waves, int wgm,
+                                      hipStream_t stream) {
+  fp.map = tile_map(p, 1);
+  const dim3 grid((unsigned)splitk_reduce_workgroups(p));
+  const GemmConfig& g = p.gemm;
+  const auto tile = [&](int m, int n) { return g.tile_m == m && g.tile_n == n; };
+#define CCL_FUSED_REDUCE(BM_, BN_, WGN_, MD_, WGM_) \
+  hipLaunchKernelGGL((fused_reduce_kernel<BM_, BN_, WGN_, MD_, WGM_, GRAD>), grid, dim3(256), 0, stream, fp)
+  if (waves == 8 && md == 16) {
+    if (tile(256, 256)) CCL_FUSED_REDUCE(256, 256, 4, 16, 2);
+    else if (tile(256, 128) && wgm == 4) CCL_FUSED_REDUCE(256, 128, 2, 16, 4);
+    else if (tile(256, 128)) CCL_FUSED_REDUCE(256, 128, 4, 16, 2);
+    else if (tile(128, 256)) CCL_FUSED_REDUCE(128, 256, 4, 16, 2);
+    else if (tile(128, 128)) CCL_FUSED_REDUCE(128, 128, 4, 16, 2);
+    else return hipErrorInvalidValue;
+  } else if (waves == 8) {
+    if (tile(256, 256)) CCL_FUSED_REDUCE(256, 256, 4, 32, 2);
+    else return hipErrorInvalidValue;
+  } else if (md == 16) {
+    if (tile(256, 256)) CCL_FUSED_REDUCE(256, 256, 2, 16, 2);
+    else if (tile(256, 128)) CCL_FUSED_REDUCE(256, 128, 2, 16, 2);
+    else if (tile(128, 256)) CCL_FUSED_REDUCE(128, 256, 2, 16, 2);
+    else if (tile(128, 128)) CCL_FUSED_REDUCE(128, 128, 2, 16, 2);
+    else return hipErrorInvalidValue;
+  } else {
+    if (tile(256, 256)) CCL_FUSED_REDUCE(256, 256, 2, 32, 2);
+    else if (tile(256, 128)) CCL_FUSED_REDUCE(256, 128, 2, 32, 2);
+    else if (tile(128, 256)) CCL_FUSED_REDUCE(128, 256, 2, 32, 2);
+    else if (tile(128, 128)) CCL_FUSED_REDUCE(128, 128, 2, 32, 2);
+    else return hipErrorInvalidValue;
+  }
+#undef CCL_FUSED_REDUCE
+  return hipGetLastError();
+}
+
+hipError_t launch_gemm_fused(const Plan& plan, const FusedCall& call, int splits, void* ws, hipStream_t stream) {
+  const FusedForm ff = fused_form(plan, call.rowmajor, splits, call.grad, call.gated, call.dbias != nullptr);
+  const GemmForm& f = ff.gemm;
+  Plan p = plan;
+  p.gemm.wide_n = 0;
+  FusedParams fp;
+  gemm_params(p, f, call.A, call.B, call.C, ff.a, ff.b, ff.c, true, &fp);
+  fp.alpha = call.alpha;
+  fp.c_nt = ff.c_nt ? 1 : 0;
+  fp.e.bias = call.bias;
+  fp.e.R = static_cast<const uint16_t*>(call.R);
+  fp.e.Zin = static_cast<const uint16_t*>(call.Zin);
+  fp.e.Zout = static_cast<uint16_t*>(call.Zout);
+  fp.e.colsum = call.dbias ? reinterpret_cast<float*>(static_cast<char*>(ws) + ff.partial_bytes) : nullptr;
+  fp.e.z = ff.z;
+  fp.e.rows = call.rows;
+  fp.e.part_rows = p.part_rows();
+  fp.e.z_cols = ff.z_cols;
+  fp.e.part_cols = (int32_t)p.part_cols();
+  fp.e.act = call.act;
+  fp.e.gated = call.gated ? 1 : 0;
+  fp.e.bias_f32 = call.bias_f32 ? 1 : 0;
+  fp.e.beta = call.beta;
+  int md, wgm;
+  fp.ws = static_cast<float*>(ws);
+  hipError_t e = launch_form(f, fp, stream, &md, &wgm);
+  if (e != hipSuccess) return e;
+  e = call.grad ? launch_fused_reduce<true>(p, fp, md, f.waves, wgm, stream)
+                : launch_fused_reduce<false>(p, fp, md, f.waves, wgm, stream);
+  if (e != hipSuccess || !call.dbias) return e;
+  hipLaunchKernelGGL(bias_reduce_kernel, dim3((unsigned)((ff.z_cols + 63) / 64)), dim3(256), 0, stream, fp.e.colsum,
+                     (call.rows + ff.sum_rows - 1) / ff.sum_rows, ff.z_cols, call.dbias);
+  return hipGetLastError();
+}
+
 
 hipError_t launch_dispatch_probe(const Plan& p, int32_t* out, hipStream_t stream) {
   OperandAddr a, b, c;

@@ -25,6 +25,22 @@ hipError_t launch_gemm(const Plan& p, const void* A, const void* B, void* C,
                        bool remap, float alpha, float beta, int splits, float* ws,
                        hipStream_t stream, uint64_t* timeline = nullptr);
 constexpr int kTimelineWords = 8;
+// One ccl_gemm_fused (grad false) or ccl_gemm_fused_grad call. ws: the
+// workspace of fused_form's size for the same arguments.
+struct FusedCall {
+  const void *A = nullptr, *B = nullptr;
+  void* C = nullptr;               // C, or dZ
+  const void* bias = nullptr;
+  const void* R = nullptr;         // residual
+  const void* Zin = nullptr;       // pre-activations read (grad)
+  void* Zout = nullptr;            // pre-activations kept
+  float* dbias = nullptr;          // column sums of dZ (grad)
+  bool rowmajor = false, grad = false, gated = false, bias_f32 = false;
+  int act = ACT_NONE;
+  float alpha = 1.f, beta = 0.f;
+  int64_t rows = 0;
+};
+hipError_t launch_gemm_fused(const Plan& p, const FusedCall& call, int splits, void* ws, hipStream_t stream);
 // Split-K workspace for callers that cannot allocate device memory: a
 // static device array of kScratchBytes in the library (one per GPU, held
 // until the process ends). Returns its address on the current device,
