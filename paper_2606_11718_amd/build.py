@@ -33,6 +33,7 @@ SOURCES = [
     ("ccl_ops.cpp", "hip"),
     ("kernels/pack.hip", "hip"),
     ("kernels/gemm.hip", "hip"),
+    ("kernels/gemm_fused.hip", "hip"),
 ]
 
 

@@ -723,9 +723,16 @@ FusedForm fused_form(const Plan& plan, bool rowmajor, int splits, bool grad, boo
   f.z = matrix_addressing(p, f.z_cols, rowmajor);
   f.c = matrix_addressing(p, f.c_cols, rowmajor);
   f.c_nt = f.gemm.c_nt;
-  const int md = f.gemm.kernel == GemmKernel::FP8 ? 32 : 16;
-  f.sum_rows = md;
-  f.partial_bytes = (int64_t)p.G * p.gemm.tiles_m * p.gemm.tiles_n * f.gemm.splits * p.gemm.tile_m * p.gemm.tile_n * 4;
+  // The kernels whose accumulators are in 16x16 MFMA order under 8 waves take
+  // the epilogue themselves; split-K sums its ranges first, and the rest (plans
+  // whose K blocks are odd multiples of the K step, 4 waves, operands of 2 GiB
+  // and more) pass through one range's partials.
+  const GemmKernel k = f.gemm.kernel;
+  f.direct = f.gemm.splits == 1 && f.gemm.waves == 8 &&
+             (k == GemmKernel::A2 || k == GemmKernel::FP8P || k == GemmKernel::FP8S ||
+              (k == GemmKernel::K64 && !f.gemm.far));
+  f.sum_rows = f.direct ? f.gemm.tile_m : k == GemmKernel::FP8 ? 32 : 16;
+  f.partial_bytes = f.direct ? 0 : (int64_t)p.G * p.gemm.tiles_m * p.gemm.tiles_n * f.gemm.splits * p.gemm.tile_m * p.gemm.tile_n * 4;
   f.workspace_bytes = f.partial_bytes + (dbias ? p.M / f.sum_rows * f.z_cols * 4 : 0);
   return f;
 }

@@ -52,125 +52,292 @@ __device__ __forceinline__ f32x4 bias4(const FusedEpi& e, int64_t n) {
 // wide_col(n) and its up at wide_col(n) + 16; n and n + 3 lie in one group.
 __device__ __forceinline__ int wide_col(int n) { return ((n & ~15) << 1) | (n & 15); }
 
-// The simple form: the product's fp32 partial tiles (split-K ranges, or one
-// range of the whole K) are read back from the workspace and summed in
-// ascending range order, one float4 per thread, as splitk_reduce_kernel does.
-// Bound by reading the partials; used for split-K and for the plans whose
-// GEMM kernel has no fused epilogue of its own.
-template <int BM, int BN, int WGN, int MD, int WGM, bool GRAD>
-__global__ void __launch_bounds__(256) fused_reduce_kernel(FusedParams p) {
-  using L = AccLayout<MD>;
-  constexpr int WM = BM / WGM, WN = BN / WGN;
-  constexpr int TM = WM / MD, TN = WN / MD;
-  constexpr int kChunks = BM * BN / (4 * 256);
-  const int64_t slot = blockIdx.x >> 3;
-  const int32_t chunk = (int32_t)(slot % kChunks);
-  int32_t pr, pc, ti, tj, split;
-  if (!map_tile(p.map, ((slot / kChunks) << 3) | (blockIdx.x & 7), &pr, &pc, &ti, &tj, &split)) return;
-  const int32_t f = chunk * 256 + threadIdx.x;
-  const int lane = f & 63;
-  int r = f >> 6;
-  const int q = r % L::Q;
-  r /= L::Q;
-  const int nt = r % TN;
-  r /= TN;
-  const int mt = r % TM;
-  const int wave = r / TM;
-  const int wm = wave / (BN / WN), wn = wave % (BN / WN);
-  const int64_t m = ti * BM + wm * WM + mt * MD + L::row(lane);   // row in the partition
-  const int n = tj * BN + wn * WN + nt * MD + L::col(lane, q);    // column of D in the partition
-  const FusedEpi& e = p.e;
-  const bool live = pr * e.part_rows + m < e.rows;
-  const int32_t S = p.splits_total;
-  const float4* part = reinterpret_cast<const float4*>(p.ws + tile_id(p, pr, pc, ti, tj) * S * (BM * BN));
-  auto sum = [&](int32_t at) {
-    f32x4 o{0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < S; ++s) o += *reinterpret_cast<const f32x4*>(part + at + (int64_t)s * (BM * BN / 4));
-    return o * p.alpha;
-  };
-  const int64_t c_at = pr * p.c.part + pc * p.c.slice + m * p.c.ld;
-  const int64_t z_at = pr * e.z.part + pc * e.z.slice + m * e.z.ld;
-  auto put = [](uint16_t* base, int64_t at, f32x4 v) { *reinterpret_cast<uint2*>(base + at) = f32_to_bf16x4(v); };
-  uint16_t* C = static_cast<uint16_t*>(p.C);
-  const f32x4 zero{0.f, 0.f, 0.f, 0.f};
-  if constexpr (!GRAD) {
-    // The up columns' threads leave: the gate columns' threads read both. The
-    // up's float4 lies in the next MFMA tile (16 wide) or two groups on (32).
-    constexpr int kUp = MD == 16 ? 64 * L::Q : 2 * 64;
-    if (e.gated && (n & 16)) return;
-    f32x4 z = live ? sum(f) + bias4(e, pc * (int64_t)e.part_cols + n) : zero;
-    f32x4 u = e.gated && live ? sum(f + kUp) + bias4(e, pc * (int64_t)e.part_cols + n + 16) : zero;
-    if (e.Zout) {
-      put(e.Zout, z_at + n, z);
-      if (e.gated) put(e.Zout, z_at + n + 16, u);
+// ---------------------------------------------------------------------------
+// The epilogue in the GEMM kernel itself (kernels with 16x16 MFMA tiles and 8
+// waves). Lane l holds rows wm WM + 16 mt + l % 16 and columns wn WN + 16 nt +
+// 4 (l / 16) .. + 3 of D in acc[mt][nt]; a gate and its up are acc[mt][2 i] and
+// acc[mt][2 i + 1] of one lane, so the formulas stay in registers. Matrices
+// cross between this order and whole 128-byte lines of memory through the
+// stage buffers, idle after the K loop: what is read (R, Z) is copied in line
+// by line and picked up 8 bytes a lane, the result replaces it in place, and
+// lines are copied out.
+// ---------------------------------------------------------------------------
+
+// A bf16 matrix of ROWS x COLS in the two stage arrays, half of its rows in
+// each, 16-byte chunks XORed with the row so that the 16 rows of one access
+// fall in distinct banks.
+template <int ROWS, int COLS>
+struct StagedTile {
+  static constexpr int HALF = ROWS / 2, PITCH = COLS * 2, CPR = COLS / 8;
+  static_assert(CPR == 8 || CPR % 16 == 0, "the swizzle is defined for rows of 8 or 16 i chunks");
+  char *lo, *hi;
+  __device__ __forceinline__ char* chunk(int r, int c) const {
+    const int h = r < HALF ? r : r - HALF;
+    return (r < HALF ? lo : hi) + h * PITCH + ((c ^ (CPR == 8 ? (h >> 1) & 7 : h & 15)) << 4);
+  }
+  // Four columns from column n (a multiple of 4) of row r.
+  __device__ __forceinline__ uint2* at(int r, int n) const {
+    return reinterpret_cast<uint2*>(chunk(r, n >> 3) + ((n >> 2) & 1) * 8);
+  }
+};
+
+// Every LDS access of the workgroup before this is done after it.
+__device__ __forceinline__ void staged_barrier() {
+  __builtin_amdgcn_s_waitcnt(waitcnt_imm(63, 0));
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Staged row r is row `row(r)` of the matrix at m (leading dimension ld).
+template <int ROWS, int COLS, int THREADS, typename Row>
+__device__ __forceinline__ void copy_in(const StagedTile<ROWS, COLS>& t, const uint16_t* m, int32_t ld, int tid, Row&& row) {
+  constexpr int CPR = COLS / 8, N = ROWS * CPR / THREADS;
+  static_assert(ROWS * CPR % THREADS == 0, "whole accesses");
+  constexpr int B = N < 8 ? N : 8;            // loads in flight per thread
+  for (int i = 0; i < N; i += B) {
+    uint4 v[B];
+#pragma unroll
+    for (int j = 0; j < B; ++j) {
+      const int at = (i + j) * THREADS + tid;
+      v[j] = *reinterpret_cast<const uint4*>(m + (int64_t)row(at / CPR) * ld + at % CPR * 8);
     }
-    f32x4 o;
-    with_act(e.act, [&](auto act) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] = act_value<decltype(act)::value>(z[j]);
-    });
-    if (e.gated) o *= u;
-    const int cn = e.gated ? ((n >> 5) << 4) | (n & 15) : n;
-    if (!live) {
-      o = zero;
-    } else if (e.R) {
-      const f32x4 res = bf16x4_to_f32(*reinterpret_cast<const uint2*>(e.R + c_at + cn));
-#pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] = __builtin_fmaf(e.beta, res[j], o[j]);
-    }
-    put(C, c_at + cn, o);
-  } else {
-    const int zn = e.gated ? wide_col(n) : n;
-    f32x4 g = zero, u = zero;
-    if (live) {
-      const f32x4 d = sum(f);
-      const f32x4 z = e.Zin ? bf16x4_to_f32(*reinterpret_cast<const uint2*>(e.Zin + z_at + zn)) : zero;
-      const f32x4 zu = e.gated ? bf16x4_to_f32(*reinterpret_cast<const uint2*>(e.Zin + z_at + zn + 16)) : zero;
-      with_act(e.act, [&](auto act) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float grad;
-          const float value = act_value_grad<decltype(act)::value>(z[j], &grad);
-          g[j] = d[j] * grad;
-          if (e.gated) {
-            g[j] *= zu[j];
-            u[j] = d[j] * value;
-          }
-        }
-      });
-    }
-    put(C, c_at + zn, g);
-    if (e.gated) put(C, c_at + zn + 16, u);
-    if (e.colsum) {
-      // The MD lanes of a column group hold MD rows of four columns.
-      const int64_t block = (pr * e.part_rows + m) / MD;
-      float* to = e.colsum + block * e.z_cols + (e.gated ? 2 : 1) * pc * (int64_t)e.part_cols + zn;
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        if (half && !e.gated) break;
-        f32x4 v = half ? u : g;
-#pragma unroll
-        for (int x = 1; x < MD; x <<= 1)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) v[j] += __shfl_xor(v[j], x);
-        if ((lane & (MD - 1)) == 0) *reinterpret_cast<f32x4*>(to + 16 * half) = v;
-      }
+    for (int j = 0; j < B; ++j) {
+      const int at = (i + j) * THREADS + tid;
+      *reinterpret_cast<uint4*>(t.chunk(at / CPR, at % CPR)) = v[j];
     }
   }
 }
 
-// Column sums over the row blocks, in a fixed order: thread (g, c) adds the
-// blocks g, g + 4, ... of its column, then the four are added.
-__global__ void __launch_bounds__(256) bias_reduce_kernel(const float* part, int64_t blocks, int64_t cols, float* out) {
-  __shared__ float sm[4][64];
-  const int c = threadIdx.x & 63, g = threadIdx.x >> 6;
-  const int64_t col = (int64_t)blockIdx.x * 64 + c;
-  float v = 0.f;
-  if (col < cols) {
-#pragma unroll 8
-    for (int64_t b = g; b < blocks; b += 4) v += part[b * cols + col];
+template <int ROWS, int COLS, int THREADS, typename Row>
+__device__ __forceinline__ void copy_out(const StagedTile<ROWS, COLS>& t, uint16_t* m, int32_t ld, int32_t nt, int tid,
+                                         Row&& row) {
+  constexpr int CPR = COLS / 8, N = ROWS * CPR / THREADS;
+  choose_nt(nt, [&](auto past) __attribute__((always_inline)) {
+#pragma unroll 4
+    for (int i = 0; i < N; ++i) {
+      const int at = i * THREADS + tid;
+      const i32x4 v = *reinterpret_cast<const i32x4*>(t.chunk(at / CPR, at % CPR));
+      i32x4* dst = reinterpret_cast<i32x4*>(m + (int64_t)row(at / CPR) * ld + at % CPR * 8);
+      if constexpr (decltype(past)::value) __builtin_nontemporal_store(v, dst);
+      else *dst = v;
+    }
+  });
+}
+
+template <int COLS, int THREADS>
+__device__ __forceinline__ void zero_rows(uint16_t* m, int32_t ld, int rows, int tid) {
+  constexpr int CPR = COLS / 8;
+  for (int at = tid; at < rows * CPR; at += THREADS)
+    *reinterpret_cast<uint4*>(m + (int64_t)(at / CPR) * ld + at % CPR * 8) = make_uint4(0, 0, 0, 0);
+}
+
+// Corners of a tile (or of its 2 BN or BN / 2 columns) in a matrix.
+template <int BM>
+__device__ __forceinline__ int64_t tile_corner(const OperandAddr& o, int32_t pr, int32_t pc, int32_t ti, int64_t col) {
+  return pr * o.part + pc * o.slice + (int64_t)(ti * BM) * o.ld + col;
+}
+
+// A tile wholly past the valid rows: zeros, and no column sums (the reduce
+// does not read its block). Whether it was one.
+template <int BM, int BN, int THREADS, bool GRAD>
+__device__ __forceinline__ bool dead_tile(const FusedParams& p, int32_t pr, int32_t pc, int32_t ti, int32_t tj) {
+  const FusedEpi& e = p.e;
+  if (pr * e.part_rows + (int64_t)ti * BM < e.rows) return false;
+  const int tid = threadIdx.x;
+  uint16_t* C = static_cast<uint16_t*>(p.C);
+  const auto zero = [&](uint16_t* m, const OperandAddr& o, auto cols) {
+    constexpr int W = decltype(cols)::value;
+    zero_rows<W, THREADS>(m + tile_corner<BM>(o, pr, pc, ti, (int64_t)tj * W), o.ld, BM, tid);
+  };
+  if (!e.gated) zero(C, p.c, std::integral_constant<int, BN>{});
+  else zero(C, p.c, std::integral_constant<int, GRAD ? 2 * BN : BN / 2>{});
+  if (!GRAD && e.Zout) zero(e.Zout, e.z, std::integral_constant<int, BN>{});
+  return true;
+}
+
+template <int BM, int BN, int NW, int TM, int TN, int WM, int WN>
+__device__ __forceinline__ void fused_forward(const FusedParams& p, f32x4 (&acc)[TM][TN], char* lo, char* hi,
+                                              int32_t pr, int32_t pc, int32_t ti, int32_t tj, int wm, int wn, int tid) {
+  const FusedEpi& e = p.e;
+  constexpr int THREADS = 64 * NW;
+  const int lane = tid & 63;
+  const int r0 = wm * WM + (lane & 15), n0 = wn * WN + 4 * (lane >> 4);
+  const int64_t left = e.rows - (pr * e.part_rows + (int64_t)ti * BM);   // valid rows from the tile's first on
+  const auto same = [](int r) { return r; };
+  const f32x4 zero{0.f, 0.f, 0.f, 0.f};
+  // Z, in place of D
+#pragma unroll
+  for (int nt = 0; nt < TN; ++nt) {
+    const f32x4 b = bias4(e, pc * (int64_t)e.part_cols + tj * BN + n0 + 16 * nt);
+#pragma unroll
+    for (int mt = 0; mt < TM; ++mt) {
+      const bool live = r0 + 16 * mt < left;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[mt][nt][j] = live ? __builtin_fmaf(p.alpha, acc[mt][nt][j], b[j]) : 0.f;
+    }
   }
-  sm[g][c] = v;
-  __syncthreads();
-  if (g == 0 && col < cols) out[col] = ((sm[0][c] + sm[1][c]) + sm[2][c]) + sm[3][c];
+  if (e.Zout) {
+    const StagedTile<BM, BN> t{lo, hi};
+#pragma unroll
+    for (int mt = 0; mt < TM; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < TN; ++nt) *t.at(r0 + 16 * mt, n0 + 16 * nt) = f32_to_bf16x4(acc[mt][nt]);
+    staged_barrier();
+    copy_out<BM, BN, THREADS>(t, e.Zout + tile_corner<BM>(e.z, pr, pc, ti, tj * BN), e.z.ld, p.c_nt, tid, same);
+    staged_barrier();
+  }
+  const ActCoef k = act_coef(e.act);
+  const auto finish = [&](auto gated) __attribute__((always_inline)) {
+    constexpr bool GATED = decltype(gated)::value;
+    constexpr int W = GATED ? BN / 2 : BN;
+    const StagedTile<BM, W> t{lo, hi};
+    const int64_t corner = tile_corner<BM>(p.c, pr, pc, ti, (int64_t)tj * W);
+    if (e.R) {
+      copy_in<BM, W, THREADS>(t, e.R + corner, p.c.ld, tid, same);
+      staged_barrier();
+    }
+    with_act(e.act, [&](auto cls) __attribute__((always_inline)) {
+#pragma unroll
+      for (int mt = 0; mt < TM; ++mt) {
+        const bool live = r0 + 16 * mt < left;
+#pragma unroll
+        for (int nt = 0; nt < TN; nt += GATED ? 2 : 1) {
+          uint2* at = t.at(r0 + 16 * mt, GATED ? wn * (WN / 2) + 4 * (lane >> 4) + 8 * nt : n0 + 16 * nt);
+          f32x4 o;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            o[j] = act_value<decltype(cls)::value>(k, acc[mt][nt][j]);
+            if constexpr (GATED) o[j] *= acc[mt][nt + 1][j];
+          }
+          if (e.R) {
+            const f32x4 r = bf16x4_to_f32(*at);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = __builtin_fmaf(e.beta, r[j], o[j]);
+          }
+          *at = f32_to_bf16x4(live ? o : zero);
+        }
+      }
+    });
+    staged_barrier();
+    copy_out<BM, W, THREADS>(t, static_cast<uint16_t*>(p.C) + corner, p.c.ld, p.c_nt, tid, same);
+  };
+  if (e.gated) finish(std::true_type{});
+  else finish(std::false_type{});
+}
+
+template <int BM, int BN, int NW, int TM, int TN, int WM, int WN>
+__device__ __forceinline__ void fused_backward(const FusedParams& p, const f32x4 (&acc)[TM][TN], char* lo, char* hi,
+                                               int32_t pr, int32_t pc, int32_t ti, int32_t tj, int wm, int wn, int tid) {
+  const FusedEpi& e = p.e;
+  constexpr int THREADS = 64 * NW;
+  const int lane = tid & 63;
+  const int64_t left = e.rows - (pr * e.part_rows + (int64_t)ti * BM);
+  const ActCoef k = act_coef(e.act);
+  const f32x4 zero{0.f, 0.f, 0.f, 0.f};
+  const auto finish = [&](auto gated) __attribute__((always_inline)) {
+    constexpr bool GATED = decltype(gated)::value;
+    // A gated Z and dZ have 2 BN columns: two passes of half of every wave's rows.
+    constexpr int PASSES = GATED ? 2 : 1;
+    constexpr int W = GATED ? 2 * BN : BN, PM = WM / PASSES;
+    const StagedTile<BM / PASSES, W> t{lo, hi};
+    const int64_t corner = tile_corner<BM>(p.c, pr, pc, ti, (int64_t)tj * W);
+    f32x4 sums[TN][PASSES];
+#pragma unroll
+    for (int nt = 0; nt < TN; ++nt)
+#pragma unroll
+      for (int h = 0; h < PASSES; ++h) sums[nt][h] = zero;
+#pragma unroll
+    for (int ps = 0; ps < PASSES; ++ps) {
+      const auto row = [&](int r) { return r / PM * WM + ps * PM + r % PM; };
+      if (ps) staged_barrier();               // the pass before has been copied out
+      if (e.Zin) {
+        copy_in<BM / PASSES, W, THREADS>(t, e.Zin + corner, p.c.ld, tid, row);
+        staged_barrier();
+      }
+      with_act(e.act, [&](auto cls) __attribute__((always_inline)) {
+#pragma unroll
+        for (int m = 0; m < TM / PASSES; ++m) {
+          const int mt = ps * (TM / PASSES) + m;
+          const bool live = wm * WM + 16 * mt + (lane & 15) < left;
+          const int r = wm * PM + 16 * m + (lane & 15);
+#pragma unroll
+          for (int nt = 0; nt < TN; ++nt) {
+            const int n = wn * (W / (BN / WN)) + 4 * (lane >> 4) + (GATED ? 32 : 16) * nt;
+            const f32x4 z = e.Zin ? bf16x4_to_f32(*t.at(r, n)) : zero;
+            f32x4 zu = zero, u = zero, g;
+            if constexpr (GATED) zu = bf16x4_to_f32(*t.at(r, n + 16));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float d = p.alpha * acc[mt][nt][j];
+              float grad;
+              const float value = act_value_grad<decltype(cls)::value>(k, z[j], &grad);
+              g[j] = d * grad;
+              if constexpr (GATED) {
+                g[j] *= zu[j];
+                u[j] = d * value;
+              }
+            }
+            g = live ? g : zero;
+            *t.at(r, n) = f32_to_bf16x4(g);
+            sums[nt][0] += g;
+            if constexpr (GATED) {
+              u = live ? u : zero;
+              *t.at(r, n + 16) = f32_to_bf16x4(u);
+              sums[nt][PASSES - 1] += u;
+            }
+          }
+        }
+      });
+      staged_barrier();
+      copy_out<BM / PASSES, W, THREADS>(t, static_cast<uint16_t*>(p.C) + corner, p.c.ld, p.c_nt, tid, row);
+    }
+    if (!e.colsum) return;
+    // Over the 16 rows of a lane group, then over the rows of waves in order.
+    staged_barrier();
+    float* part = reinterpret_cast<float*>(lo);       // [BM / WM][W]
+#pragma unroll
+    for (int nt = 0; nt < TN; ++nt)
+#pragma unroll
+      for (int h = 0; h < PASSES; ++h) {
+        f32x4 v = sums[nt][h];
+#pragma unroll
+        for (int x = 1; x < 16; x <<= 1)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] += __shfl_xor(v[j], x);
+        const int n = wn * (W / (BN / WN)) + 4 * (lane >> 4) + (GATED ? 32 : 16) * nt + 16 * h;
+        if ((lane & 15) == 0) *reinterpret_cast<f32x4*>(part + wm * W + n) = v;
+      }
+    staged_barrier();
+    float* to = e.colsum + (pr * e.part_rows + (int64_t)ti * BM) / BM * e.z_cols +
+                (W / BN) * pc * (int64_t)e.part_cols + (int64_t)tj * W;
+    for (int n = tid; n < W; n += THREADS) {
+      float v = part[n];
+#pragma unroll
+      for (int w = 1; w < BM / WM; ++w) v += part[w * W + n];
+      to[n] = v;
+    }
+  };
+  if (e.gated) finish(std::true_type{});
+  else finish(std::false_type{});
+}
+
+// The parameters of a kernel with one direction's epilogue.
+template <bool GRAD>
+struct FusedTileParams : FusedParams {
+  static constexpr bool kGrad = GRAD;
+};
+
+template <int BM, int BN, int NW, int TM, int TN, int WM, int WN, bool GRAD>
+__device__ __forceinline__ void fused_epilogue(const FusedTileParams<GRAD>& p, f32x4 (&acc)[TM][TN], char* lo, char* hi,
+                                               int32_t pr, int32_t pc, int32_t ti, int32_t tj, int wm, int wn, int tid) {
+  // No wave reads the stage buffers any more and no load into them is in
+  // flight (the direct-to-LDS loads of the last steps included).
+  __builtin_amdgcn_s_waitcnt(0);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  if constexpr (GRAD) fused_backward<BM, BN, NW, TM, TN, WM, WN>(p, acc, lo, hi, pr, pc, ti, tj, wm, wn, tid);
+  else fused_forward<BM, BN, NW, TM, TN, WM, WN>(p, acc, lo, hi, pr, pc, ti, tj, wm, wn, tid);
 }

@@ -25,6 +25,12 @@ hipError_t launch_gemm(const Plan& p, const void* A, const void* B, void* C,
                        bool remap, float alpha, float beta, int splits, float* ws,
                        hipStream_t stream, uint64_t* timeline = nullptr);
 constexpr int kTimelineWords = 8;
+// The GEMM of form f with every tile's fp32 partials written to ws. md and
+// wgm: the MFMA tile and the rows of the wave grid of the kernel that wrote
+// them, which set their order.
+hipError_t launch_gemm_partials(const Plan& p, const GemmForm& f, const void* A, const void* B,
+                                const OperandAddr& a, const OperandAddr& b, float* ws, hipStream_t stream,
+                                int* md, int* wgm);
 // One ccl_gemm_fused (grad false) or ccl_gemm_fused_grad call. ws: the
 // workspace of fused_form's size for the same arguments.
 struct FusedCall {
