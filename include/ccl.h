@@ -369,6 +369,57 @@ ccl_status ccl_gemm_fused_grad(ccl_plan_t plan, const ccl_epilogue_grad* epilogu
                                const void* B, void* dZ, void* workspace, int64_t workspace_bytes,
                                void* stream);
 
+/*
+ * A whole mixture-of-experts FFN layer for a few tokens (a decoding step):
+ *   p = softmax(logits) over the experts; the top_k largest logits are chosen,
+ *   the lowest expert first among equals; with normalize the chosen p are
+ *   divided by their sum;
+ *   y = sum over the chosen e of p_e * down_scale_e * Wd_e h_e,
+ *   h_e = act(gate_up_scale_e * Wg_e x) * (gate_up_scale_e * Wu_e x).
+ * Experts whose logit is -inf (masked) or NaN are never chosen and take no part
+ * in the softmax; a token with fewer than top_k others leaves ids of -1 and
+ * probabilities of 0 in its last slots, and one with none has y = 0.
+ * Everything up to y is fp32 (h crosses between the launches to 16 bits), y is
+ * rounded to bf16 once, and the order of every sum is fixed. A dense FFN is
+ * the case of one expert.
+ */
+typedef struct ccl_moe {
+  int64_t hidden, ffn;          /* multiples of 16 */
+  int32_t experts, top_k;       /* 1..512, 1..min(16, experts) */
+  ccl_activation activation;
+  int32_t normalize;            /* 0 or 1 */
+  ccl_dtype weight_type;        /* CCL_DT_BF16 or CCL_DT_FP8_E4M3 */
+  /* Weights as a checkpoint stores them, output-major: gate_up is
+   * (experts, 2 ffn, hidden), the gate rows first; down is (experts, hidden,
+   * ffn). Elements between rows and between experts; 0: no gaps. Multiples of
+   * 16 bytes. */
+  int64_t gate_up_ld, gate_up_stride, down_ld, down_stride;
+} ccl_moe;
+
+#define CCL_MOE_MAX_TOKENS 64
+
+/*
+ * Device workspace of ccl_moe_decode for up to `tokens` tokens (0..64), and the
+ * call. x is tokens x hidden bf16 with rows x_ld apart, logits tokens x experts
+ * fp32 (rows logits_ld apart), y as x; ids (int32) and probs (fp32), both
+ * tokens x top_k, take the choice, or are NULL. The scales are fp32, one per
+ * expert, or NULL (1). x, gate_up, down and the workspace are 16-byte aligned,
+ * x_ld a multiple of 8. y may overlap x only if it is a call of no tokens; the
+ * workspace's contents on entry do not matter, and calls that share one must
+ * be ordered on one stream. No tokens: nothing is launched.
+ * Errors: CCL_ERR_INVALID_ARG (NULL argument, sizes outside the ranges above,
+ * an unknown activation or weight type, a leading dimension or stride smaller
+ * than what it spans, workspace missing or too small); CCL_ERR_UNSUPPORTED
+ * (hidden or ffn not a multiple of 16, or above 2^24; a launch too large; device
+ * not gfx950); CCL_ERR_MISALIGNED_POINTER; CCL_ERR_HIP.
+ */
+ccl_status ccl_moe_workspace(const ccl_moe* moe, int64_t tokens, int64_t* workspace_bytes);
+ccl_status ccl_moe_decode(const ccl_moe* moe, int64_t tokens, const void* x, int64_t x_ld,
+                          const float* logits, int64_t logits_ld, const void* gate_up,
+                          const float* gate_up_scale, const void* down, const float* down_scale,
+                          void* y, int64_t y_ld, int32_t* ids, float* probs, void* workspace,
+                          int64_t workspace_bytes, void* stream);
+
 /* Flags of ccl_remote_bytes and ccl_remote_bytes_l2. */
 #define CCL_TRAFFIC_A_TRANS 1   /* A is stored transposed (e.g. H held for A = H^T) */
 #define CCL_TRAFFIC_B_TRANS 2   /* B is stored transposed */

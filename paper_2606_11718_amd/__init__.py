@@ -12,5 +12,6 @@ from .ccl import (CCL_A, CCL_B, CCL_C, CCL_PLACE_RR, CCL_PLACE_COARSE, CCL_PLACE
                   CCL_ACT_NONE, CCL_ACT_RELU, CCL_ACT_GELU, CCL_ACT_SILU, CCL_LAYOUT_CCL, CCL_LAYOUT_ROWMAJOR,
                   ccl_plan_matrix_layout, ccl_gemm_fused_workspace, ccl_gemm_fused,
                   ccl_gemm_fused_grad_workspace, ccl_gemm_fused_grad,
+                  CCL_MOE_MAX_TOKENS, ccl_moe, ccl_moe_workspace, ccl_moe_decode,
                   ccl_gemm_rowmajor, ccl_remote_bytes, ccl_remote_bytes_l2, ccl_status_string,
                   ccl_last_error)

@@ -34,6 +34,7 @@ SOURCES = [
     ("kernels/pack.hip", "hip"),
     ("kernels/gemm.hip", "hip"),
     ("kernels/gemm_fused.hip", "hip"),
+    ("kernels/moe.hip", "hip"),
 ]
 
 

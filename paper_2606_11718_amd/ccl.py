@@ -29,7 +29,7 @@ EXPORTED = ("ccl_plan", "ccl_plan_typed", "ccl_plan_destroy", "ccl_plan_grid", "
             "ccl_pack", "ccl_unpack", "ccl_gemm", "ccl_gemm_scaled", "ccl_gemm_splitk_workspace",
             "ccl_gemm_splitk", "ccl_gemm_splitk_noalloc", "ccl_gemm_rowmajor",
             "ccl_plan_matrix_layout", "ccl_gemm_fused_workspace", "ccl_gemm_fused", "ccl_gemm_fused_grad_workspace",
-            "ccl_gemm_fused_grad", "ccl_remote_bytes", "ccl_remote_bytes_l2", "ccl_status_string", "ccl_last_error",
+            "ccl_gemm_fused_grad", "ccl_moe_workspace", "ccl_moe_decode", "ccl_remote_bytes", "ccl_remote_bytes_l2", "ccl_status_string", "ccl_last_error",
             "ccl_debug_tile_of_wg", "ccl_debug_gemm_config", "ccl_debug_dispatch",
             "ccl_debug_gemm_timeline", "ccl_debug_launch", "ccl_debug_launch_tile_of_wg",
             "ccl_debug_launch_dispatch", "ccl_debug_launch_timeline")
@@ -84,6 +84,13 @@ class _EpilogueGrad(ctypes.Structure):
                 ("dbias", ctypes.c_void_p)]
 
 
+class _Moe(ctypes.Structure):
+    _fields_ = [("hidden", ctypes.c_int64), ("ffn", ctypes.c_int64), ("experts", ctypes.c_int32),
+                ("top_k", ctypes.c_int32), ("activation", ctypes.c_int), ("normalize", ctypes.c_int32),
+                ("weight_type", ctypes.c_int)] + \
+               [(n, ctypes.c_int64) for n in ("gate_up_ld", "gate_up_stride", "down_ld", "down_stride")]
+
+
 _lib = None
 
 
@@ -121,6 +128,8 @@ def library() -> ctypes.CDLL:
         "ccl_gemm_fused": [vp, ctypes.POINTER(_Epilogue), vp, vp, vp, i32, vp, i64, vp],
         "ccl_gemm_fused_grad_workspace": [vp, i32, i32, i32, ctypes.POINTER(i64)],
         "ccl_gemm_fused_grad": [vp, ctypes.POINTER(_EpilogueGrad), vp, vp, vp, vp, i64, vp],
+        "ccl_moe_workspace": [ctypes.POINTER(_Moe), i64, ctypes.POINTER(i64)],
+        "ccl_moe_decode": [ctypes.POINTER(_Moe), i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp],
         "ccl_remote_bytes": [vp, i32, i32, ctypes.POINTER(_Traffic)],
         "ccl_remote_bytes_l2": [vp, i32, i32, ctypes.POINTER(_L2Config), ctypes.POINTER(_L2Traffic)],
         "ccl_debug_tile_of_wg": [vp, i64, ctypes.POINTER(i32), ctypes.POINTER(i64), ctypes.POINTER(i64)],
@@ -329,6 +338,42 @@ def ccl_gemm_fused_grad(plan: Plan, A, B, preact, dZ, *, activation: int = CCL_A
                       _ptr(dbias))
     _check(library().ccl_gemm_fused_grad(plan, ctypes.byref(e), _ptr(A), _ptr(B), _ptr(dZ), _ptr(workspace),
                                          workspace_bytes, _stream(stream)))
+
+
+CCL_MOE_MAX_TOKENS = 64
+
+
+def ccl_moe(*, hidden: int, ffn: int, experts: int, top_k: int, activation: int = CCL_ACT_SILU,
+            normalize: bool = True, weight_type: int = CCL_DT_BF16, gate_up_ld: int = 0, gate_up_stride: int = 0,
+            down_ld: int = 0, down_stride: int = 0) -> _Moe:
+    """Description of a mixture-of-experts FFN layer for ccl_moe_decode."""
+    return _Moe(hidden, ffn, experts, top_k, activation, int(normalize), weight_type, gate_up_ld, gate_up_stride,
+                down_ld, down_stride)
+
+
+def ccl_moe_workspace(moe: _Moe, tokens: int) -> int:
+    """Workspace bytes of ccl_moe_decode for up to `tokens` tokens."""
+    nbytes = ctypes.c_int64(0)
+    _check(library().ccl_moe_workspace(ctypes.byref(moe), tokens, ctypes.byref(nbytes)))
+    return nbytes.value
+
+
+def _row_stride(t, ld, width: int) -> int:
+    """Elements between rows: as given, else a 2-d tensor's own (its row length for an address)."""
+    if ld is not None:
+        return ld
+    return width if t is None or isinstance(t, int) or t.dim() < 2 else t.stride(0)
+
+
+def ccl_moe_decode(moe: _Moe, tokens: int, x, logits, gate_up, down, y, *, ids=None, probs=None, gate_up_scale=None,
+                   down_scale=None, workspace=None, workspace_bytes: int = 0, x_ld: int | None = None,
+                   logits_ld: int | None = None, y_ld: int | None = None, stream=None) -> None:
+    """y = the layer on `tokens` rows of x, routed by logits; ids and probs take the choice."""
+    _check(library().ccl_moe_decode(
+        ctypes.byref(moe), tokens, _ptr(x), _row_stride(x, x_ld, moe.hidden), _ptr(logits),
+        _row_stride(logits, logits_ld, moe.experts), _ptr(gate_up), _ptr(gate_up_scale), _ptr(down), _ptr(down_scale),
+        _ptr(y), _row_stride(y, y_ld, moe.hidden), _ptr(ids), _ptr(probs), _ptr(workspace), workspace_bytes,
+        _stream(stream)))
 
 
 CCL_TRAFFIC_A_TRANS, CCL_TRAFFIC_B_TRANS, CCL_TRAFFIC_C_READ = 1, 2, 4

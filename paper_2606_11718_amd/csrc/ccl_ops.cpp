@@ -2,6 +2,7 @@
 // include/ccl.h).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <string>
 
@@ -43,6 +44,49 @@ ccl_status check_workspace(int64_t need, const void* workspace, int64_t bytes) {
   if (!workspace) return fail(CCL_ERR_INVALID_ARG, "NULL workspace");
   if (bytes < need) return fail(CCL_ERR_INVALID_ARG, "workspace smaller than the " + std::to_string(need) + " bytes reported");
   if (!aligned16(workspace)) return fail(CCL_ERR_MISALIGNED_POINTER, "the workspace must be 16-byte aligned");
+  return CCL_OK;
+}
+
+// The checked shape of a layer for a number of tokens.
+ccl_status check_moe(const ccl_moe* m, int64_t tokens, ccl::MoeShape* out) {
+  if (!m) return fail(CCL_ERR_INVALID_ARG, "NULL argument");
+  if (tokens < 0 || tokens > ccl::kMoeMaxTokens) return fail(CCL_ERR_INVALID_ARG, "tokens must be in 0..64");
+  if (m->hidden < 1 || m->ffn < 1) return fail(CCL_ERR_INVALID_ARG, "hidden and ffn must be positive");
+  if (m->experts < 1 || m->experts > ccl::kMoeMaxExperts) return fail(CCL_ERR_INVALID_ARG, "experts must be in 1..512");
+  if (m->top_k < 1 || m->top_k > ccl::kMoeMaxTopK || m->top_k > m->experts)
+    return fail(CCL_ERR_INVALID_ARG, "top_k must be in 1..16 and at most the experts");
+  if (!ccl::valid_act(m->activation)) return fail(CCL_ERR_INVALID_ARG, "unknown activation");
+  if (m->normalize != 0 && m->normalize != 1) return fail(CCL_ERR_INVALID_ARG, "normalize must be 0 or 1");
+  if (m->weight_type != CCL_DT_BF16 && m->weight_type != CCL_DT_FP8_E4M3)
+    return fail(CCL_ERR_INVALID_ARG, "weights must be bf16 or fp8 E4M3");
+  constexpr int64_t kMaxSide = 1 << 24, kMaxStride = (int64_t)1 << 48;
+  if (m->hidden % 16 || m->ffn % 16 || m->hidden > kMaxSide || m->ffn > kMaxSide)
+    return fail(CCL_ERR_UNSUPPORTED, "hidden and ffn must be multiples of 16 up to 2^24");
+  ccl::MoeShape s;
+  s.hidden = m->hidden;
+  s.ffn = m->ffn;
+  s.experts = m->experts;
+  s.top_k = m->top_k;
+  s.act = m->activation;
+  s.normalize = m->normalize == 1;
+  s.fp8 = m->weight_type == CCL_DT_FP8_E4M3;
+  const int64_t per = s.fp8 ? 16 : 8;
+  s.gu_ld = m->gate_up_ld ? m->gate_up_ld : m->hidden;
+  s.down_ld = m->down_ld ? m->down_ld : m->ffn;
+  if (s.gu_ld < m->hidden || s.down_ld < m->ffn || s.gu_ld > kMaxSide || s.down_ld > kMaxSide)
+    return fail(CCL_ERR_INVALID_ARG, "a weight's leading dimension is smaller than its rows, or above 2^24");
+  s.gu_stride = m->gate_up_stride ? m->gate_up_stride : 2 * m->ffn * s.gu_ld;
+  s.down_stride = m->down_stride ? m->down_stride : m->hidden * s.down_ld;
+  // an expert's last row need not be followed by a gap
+  if (s.gu_stride < (2 * m->ffn - 1) * s.gu_ld + m->hidden || s.down_stride < (m->hidden - 1) * s.down_ld + m->ffn ||
+      s.gu_stride > kMaxStride || s.down_stride > kMaxStride)
+    return fail(CCL_ERR_INVALID_ARG, "experts overlap, or lie more than 2^48 elements apart");
+  if (s.gu_ld % per || s.gu_stride % per || s.down_ld % per || s.down_stride % per)
+    return fail(CCL_ERR_MISALIGNED_POINTER, "weight rows and experts must lie whole 16 bytes apart");
+  const ccl::MoeForm f = ccl::moe_form(s, tokens);
+  if (f.up_workgroups > kMaxGrid || (int64_t)f.down_tiles * f.splits > kMaxGrid)
+    return fail(CCL_ERR_UNSUPPORTED, "launch too large");
+  *out = s;
   return CCL_OK;
 }
 
@@ -147,6 +191,52 @@ ccl_status ccl_gemm_fused_grad(ccl_plan_t plan, const ccl_epilogue_grad* e, cons
   c.rows = e->rows;
   return hip_status(ccl::launch_gemm_fused(plan->plan, c, 1, workspace, static_cast<hipStream_t>(stream)),
                     "fused gradient gemm launch");
+}
+
+ccl_status ccl_moe_workspace(const ccl_moe* moe, int64_t tokens, int64_t* workspace_bytes) {
+  if (!workspace_bytes) return fail(CCL_ERR_INVALID_ARG, "NULL argument");
+  ccl::MoeShape s;
+  if (ccl_status st = check_moe(moe, tokens, &s)) return st;
+  // a smaller number of tokens may need more (it may be launched otherwise)
+  int64_t most = 0;
+  for (int64_t t = 0; t <= tokens; ++t) most = std::max(most, ccl::moe_form(s, t).workspace_bytes);
+  *workspace_bytes = most;
+  return ok();
+}
+
+ccl_status ccl_moe_decode(const ccl_moe* moe, int64_t tokens, const void* x, int64_t x_ld, const float* logits,
+                          int64_t logits_ld, const void* gate_up, const float* gate_up_scale, const void* down,
+                          const float* down_scale, void* y, int64_t y_ld, int32_t* ids, float* probs,
+                          void* workspace, int64_t workspace_bytes, void* stream) {
+  ccl::MoeShape s;
+  if (ccl_status st = check_moe(moe, tokens, &s)) return st;
+  if (tokens == 0) return ok();
+  if (!x || !logits || !gate_up || !down || !y) return fail(CCL_ERR_INVALID_ARG, "NULL argument");
+  constexpr int64_t kMaxLd = (int64_t)1 << 48;
+  if (x_ld < s.hidden || y_ld < s.hidden || logits_ld < s.experts || x_ld > kMaxLd || y_ld > kMaxLd || logits_ld > kMaxLd)
+    return fail(CCL_ERR_INVALID_ARG, "a leading dimension is smaller than its row");
+  if (!aligned16(x) || x_ld % 8 || !aligned16(gate_up) || !aligned16(down))
+    return fail(CCL_ERR_MISALIGNED_POINTER, "x (and its rows) and the weights must be 16-byte aligned");
+  if (!aligned(logits, 4) || !aligned(gate_up_scale, 4) || !aligned(down_scale, 4) || !aligned(y, 2) ||
+      !aligned(ids, 4) || !aligned(probs, 4))
+    return fail(CCL_ERR_MISALIGNED_POINTER, "a pointer is not aligned to its elements");
+  if (ccl_status st = check_workspace(ccl::moe_form(s, tokens).workspace_bytes, workspace, workspace_bytes)) return st;
+  if (ccl_status st = check_device()) return st;
+  ccl::MoeCall c;
+  c.tokens = tokens;
+  c.x = x;
+  c.logits = logits;
+  c.gate_up = gate_up;
+  c.down = down;
+  c.gate_up_scale = gate_up_scale;
+  c.down_scale = down_scale;
+  c.y = y;
+  c.ids = ids;
+  c.probs = probs;
+  c.x_ld = x_ld;
+  c.logits_ld = logits_ld;
+  c.y_ld = y_ld;
+  return hip_status(ccl::launch_moe(s, c, workspace, static_cast<hipStream_t>(stream)), "moe launch");
 }
 
 }  // extern "C"

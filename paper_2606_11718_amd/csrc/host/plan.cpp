@@ -737,4 +737,23 @@ FusedForm fused_form(const Plan& plan, bool rowmajor, int splits, bool grad, boo
   return f;
 }
 
+MoeForm moe_form(const MoeShape& s, int64_t tokens) {
+  MoeForm f;
+  const int64_t slots = tokens * s.top_k;
+  f.up_tiles = (int)((s.ffn + 15) / 16);
+  f.down_tiles = (int)((s.hidden + 15) / 16);
+  // Fewer chosen slots than experts: a workgroup per slot, which routes every
+  // token itself. Otherwise one per expert, which ranks that expert alone, and
+  // workgroups in front that route.
+  f.list = slots < s.experts;
+  f.up_workgroups = f.list ? slots * f.up_tiles : (int64_t)s.experts * f.up_tiles + (tokens + 7) / 8;
+  f.splits = 1;
+  const auto up16 = [](int64_t n) { return (n + 15) / 16 * 16; };
+  f.probs_at = up16(slots * 4);
+  f.h_at = f.probs_at + up16(slots * 4);
+  f.part_at = f.h_at + up16(slots * s.ffn * 4);
+  f.workspace_bytes = f.part_at + (f.splits > 1 ? f.splits * tokens * s.hidden * 4 : 0);
+  return f;
+}
+
 }  // namespace ccl

@@ -195,4 +195,24 @@ FusedForm fused_form(const Plan& p, bool rowmajor, int splits, bool grad, bool g
 // tile_of_wg of an unsplit ccl_gemm's own launch.
 void launch_tile_of_wg(const Plan& p, int64_t wg, int* xcd, int64_t* tile_m, int64_t* tile_n);
 
+// A mixture-of-experts FFN layer for a few tokens.
+constexpr int kMoeMaxTokens = 64, kMoeMaxExperts = 512, kMoeMaxTopK = 16;
+struct MoeShape {
+  int64_t hidden = 0, ffn = 0;
+  int experts = 0, top_k = 0, act = ACT_SILU;
+  bool normalize = true, fp8 = false;
+  // elements between experts and between rows
+  int64_t gu_stride = 0, gu_ld = 0, down_stride = 0, down_ld = 0;
+};
+// Its launches for a number of tokens, and the workspace: ids, probabilities,
+// the activations h (bf16 value and rest) and the down product's partial sums.
+struct MoeForm {
+  bool list = false;                // up workgroups per chosen slot instead of per expert
+  int up_tiles = 0, down_tiles = 0; // 16-row tiles of ffn and hidden
+  int64_t up_workgroups = 0;
+  int splits = 1;                   // ranges of the down product
+  int64_t probs_at = 0, h_at = 0, part_at = 0, workspace_bytes = 0;
+};
+MoeForm moe_form(const MoeShape& s, int64_t tokens);
+
 }  // namespace ccl

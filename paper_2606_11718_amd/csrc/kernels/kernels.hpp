@@ -56,4 +56,20 @@ hipError_t scratch_workspace(float** ws);
 // Dispatch probe with an unsplit ccl_gemm's grid (4 int32 per workgroup).
 hipError_t launch_dispatch_probe(const Plan& p, int32_t* out, hipStream_t stream);
 
+// One ccl_moe_decode call; ws: moe_form's workspace.
+struct MoeCall {
+  int64_t tokens = 0;
+  const void* x = nullptr;
+  const float* logits = nullptr;
+  const void* gate_up = nullptr;
+  const void* down = nullptr;
+  const float* gate_up_scale = nullptr;
+  const float* down_scale = nullptr;
+  void* y = nullptr;
+  int32_t* ids = nullptr;
+  float* probs = nullptr;
+  int64_t x_ld = 0, logits_ld = 0, y_ld = 0;
+};
+hipError_t launch_moe(const MoeShape& s, const MoeCall& c, void* ws, hipStream_t stream);
+
 }  // namespace ccl
