@@ -420,6 +420,42 @@ ccl_status ccl_moe_decode(const ccl_moe* moe, int64_t tokens, const void* x, int
                           void* y, int64_t y_ld, int32_t* ids, float* probs, void* workspace,
                           int64_t workspace_bytes, void* stream);
 
+/*
+ * Orthogonalised updates: for each of `batch` rows x cols matrices G (weight
+ * gradients or momenta),
+ *   X = G / (|G|_F + eps), transposed if rows > cols;
+ *   `steps` times: S = X X^T, X <- a X + (b S + c S S) X;
+ *   O = X, transposed back.
+ * The defaults (steps 5, (a, b, c) = 3.4445, -4.7750, 2.0315, eps 1e-7) bring
+ * every singular value that is not tiny to around 1. The norm is summed in 64
+ * bits; X, S and S S are held in fp16 times 2^13 with 32-bit sums, which is
+ * about 1.3e-3 of the result, and O is rounded to bf16 once. Other
+ * coefficients must keep the elements of X, S and b S + c S S below 8: past
+ * that fp16 overflows to infinity. A zero G gives zeros; an infinity or a NaN
+ * in G gives NaNs in its own matrix only. steps 0: the scaled G.
+ */
+
+/* Device workspace of ccl_orthogonalize in bytes, and the call. G is bf16 or
+ * fp32 with elements ld apart between rows and stride between matrices, at any
+ * alignment of its elements; O is bf16 with o_ld and o_stride; O may be G
+ * itself (bf16, the same layout). coeffs: three floats on the host, or NULL for
+ * the defaults. The workspace is 256-byte aligned; its contents on entry do not
+ * matter, and calls that share one must be ordered on one stream. An empty batch
+ * or matrix: nothing is launched.
+ * Errors: CCL_ERR_INVALID_ARG (NULL argument; negative sizes; a leading
+ * dimension or, in a batch, a stride smaller than what it spans; a type other
+ * than bf16 and fp32; steps outside 0..32; a coefficient or eps that is not
+ * finite, a negative eps; workspace missing or too small);
+ * CCL_ERR_UNSUPPORTED (a side above 65536, 2^30 padded elements or more a
+ * matrix, more than 2^31 workgroups; device not gfx950);
+ * CCL_ERR_MISALIGNED_POINTER; CCL_ERR_HIP. */
+ccl_status ccl_orthogonalize_workspace(int64_t batch, int64_t rows, int64_t cols,
+                                       int64_t* workspace_bytes);
+ccl_status ccl_orthogonalize(int64_t batch, int64_t rows, int64_t cols, const void* G,
+                             ccl_dtype g_type, int64_t ld, int64_t stride, int steps,
+                             const float* coeffs, float eps, void* O, int64_t o_ld, int64_t o_stride,
+                             void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Flags of ccl_remote_bytes and ccl_remote_bytes_l2. */
 #define CCL_TRAFFIC_A_TRANS 1   /* A is stored transposed (e.g. H held for A = H^T) */
 #define CCL_TRAFFIC_B_TRANS 2   /* B is stored transposed */

@@ -13,5 +13,6 @@ from .ccl import (CCL_A, CCL_B, CCL_C, CCL_PLACE_RR, CCL_PLACE_COARSE, CCL_PLACE
                   ccl_plan_matrix_layout, ccl_gemm_fused_workspace, ccl_gemm_fused,
                   ccl_gemm_fused_grad_workspace, ccl_gemm_fused_grad,
                   CCL_MOE_MAX_TOKENS, ccl_moe, ccl_moe_workspace, ccl_moe_decode,
+                  ccl_orthogonalize_workspace, ccl_orthogonalize,
                   ccl_gemm_rowmajor, ccl_remote_bytes, ccl_remote_bytes_l2, ccl_status_string,
                   ccl_last_error)

@@ -35,6 +35,7 @@ SOURCES = [
     ("kernels/gemm.hip", "hip"),
     ("kernels/gemm_fused.hip", "hip"),
     ("kernels/moe.hip", "hip"),
+    ("kernels/newton_schulz.hip", "hip"),
 ]
 
 

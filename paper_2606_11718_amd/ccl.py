@@ -29,7 +29,8 @@ EXPORTED = ("ccl_plan", "ccl_plan_typed", "ccl_plan_destroy", "ccl_plan_grid", "
             "ccl_pack", "ccl_unpack", "ccl_gemm", "ccl_gemm_scaled", "ccl_gemm_splitk_workspace",
             "ccl_gemm_splitk", "ccl_gemm_splitk_noalloc", "ccl_gemm_rowmajor",
             "ccl_plan_matrix_layout", "ccl_gemm_fused_workspace", "ccl_gemm_fused", "ccl_gemm_fused_grad_workspace",
-            "ccl_gemm_fused_grad", "ccl_moe_workspace", "ccl_moe_decode", "ccl_remote_bytes", "ccl_remote_bytes_l2", "ccl_status_string", "ccl_last_error",
+            "ccl_gemm_fused_grad", "ccl_moe_workspace", "ccl_moe_decode",
+            "ccl_orthogonalize_workspace", "ccl_orthogonalize", "ccl_remote_bytes", "ccl_remote_bytes_l2", "ccl_status_string", "ccl_last_error",
             "ccl_debug_tile_of_wg", "ccl_debug_gemm_config", "ccl_debug_dispatch",
             "ccl_debug_gemm_timeline", "ccl_debug_launch", "ccl_debug_launch_tile_of_wg",
             "ccl_debug_launch_dispatch", "ccl_debug_launch_timeline")
@@ -130,6 +131,9 @@ def library() -> ctypes.CDLL:
         "ccl_gemm_fused_grad": [vp, ctypes.POINTER(_EpilogueGrad), vp, vp, vp, vp, i64, vp],
         "ccl_moe_workspace": [ctypes.POINTER(_Moe), i64, ctypes.POINTER(i64)],
         "ccl_moe_decode": [ctypes.POINTER(_Moe), i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp],
+        "ccl_orthogonalize_workspace": [i64, i64, i64, ctypes.POINTER(i64)],
+        "ccl_orthogonalize": [i64, i64, i64, vp, i32, i64, i64, i32, ctypes.POINTER(ctypes.c_float), ctypes.c_float,
+                              vp, i64, i64, vp, i64, vp],
         "ccl_remote_bytes": [vp, i32, i32, ctypes.POINTER(_Traffic)],
         "ccl_remote_bytes_l2": [vp, i32, i32, ctypes.POINTER(_L2Config), ctypes.POINTER(_L2Traffic)],
         "ccl_debug_tile_of_wg": [vp, i64, ctypes.POINTER(i32), ctypes.POINTER(i64), ctypes.POINTER(i64)],
@@ -374,6 +378,24 @@ def ccl_moe_decode(moe: _Moe, tokens: int, x, logits, gate_up, down, y, *, ids=N
         _row_stride(logits, logits_ld, moe.experts), _ptr(gate_up), _ptr(gate_up_scale), _ptr(down), _ptr(down_scale),
         _ptr(y), _row_stride(y, y_ld, moe.hidden), _ptr(ids), _ptr(probs), _ptr(workspace), workspace_bytes,
         _stream(stream)))
+
+
+def ccl_orthogonalize_workspace(batch: int, rows: int, cols: int) -> int:
+    """Workspace bytes of ccl_orthogonalize."""
+    nbytes = ctypes.c_int64(0)
+    _check(library().ccl_orthogonalize_workspace(batch, rows, cols, ctypes.byref(nbytes)))
+    return nbytes.value
+
+
+def ccl_orthogonalize(batch: int, rows: int, cols: int, G, g_type: int, ld: int, stride: int, O, *,
+                      o_ld: int | None = None, o_stride: int | None = None, steps: int = 5, coeffs=None,
+                      eps: float = 1e-7, workspace=None, workspace_bytes: int = 0, stream=None) -> None:
+    """O = the Newton-Schulz orthogonalisation of each of the batch's matrices (O without gaps by default)."""
+    c = None if coeffs is None else (ctypes.c_float * 3)(*coeffs)
+    o_ld = cols if o_ld is None else o_ld
+    _check(library().ccl_orthogonalize(batch, rows, cols, _ptr(G), g_type, ld, stride, steps, c, eps, _ptr(O), o_ld,
+                                       rows * o_ld if o_stride is None else o_stride, _ptr(workspace), workspace_bytes,
+                                       _stream(stream)))
 
 
 CCL_TRAFFIC_A_TRANS, CCL_TRAFFIC_B_TRANS, CCL_TRAFFIC_C_READ = 1, 2, 4

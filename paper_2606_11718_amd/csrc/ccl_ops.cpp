@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <string>
 
@@ -87,6 +88,19 @@ ccl_status check_moe(const ccl_moe* m, int64_t tokens, ccl::MoeShape* out) {
   if (f.up_workgroups > kMaxGrid || (int64_t)f.down_tiles * f.splits > kMaxGrid)
     return fail(CCL_ERR_UNSUPPORTED, "launch too large");
   *out = s;
+  return CCL_OK;
+}
+
+ccl_status check_ortho(int64_t batch, int64_t rows, int64_t cols) {
+  if (batch < 0 || rows < 0 || cols < 0) return fail(CCL_ERR_INVALID_ARG, "negative size");
+  if (rows > 65536 || cols > 65536) return fail(CCL_ERR_UNSUPPORTED, "a side above 65536");
+  if (batch > kMaxGrid) return fail(CCL_ERR_UNSUPPORTED, "launch too large");
+  const ccl::OrthoForm f = ccl::ortho_form({batch, rows, cols});
+  if (f.x_elems >= (int64_t)1 << 30) return fail(CCL_ERR_UNSUPPORTED, "a matrix of 2^30 padded elements or more");
+  // the launches of most workgroups: 64x64 pieces, elements without steps, 128x128 tiles
+  if (batch * ((rows * cols + 255) / 256) > kMaxGrid || batch * (f.x_elems / 4096) > kMaxGrid ||
+      batch * f.chunks > kMaxGrid)
+    return fail(CCL_ERR_UNSUPPORTED, "launch too large");
   return CCL_OK;
 }
 
@@ -237,6 +251,52 @@ ccl_status ccl_moe_decode(const ccl_moe* moe, int64_t tokens, const void* x, int
   c.logits_ld = logits_ld;
   c.y_ld = y_ld;
   return hip_status(ccl::launch_moe(s, c, workspace, static_cast<hipStream_t>(stream)), "moe launch");
+}
+
+ccl_status ccl_orthogonalize_workspace(int64_t batch, int64_t rows, int64_t cols, int64_t* workspace_bytes) {
+  if (!workspace_bytes) return fail(CCL_ERR_INVALID_ARG, "NULL argument");
+  if (ccl_status s = check_ortho(batch, rows, cols)) return s;
+  *workspace_bytes = batch && rows && cols ? ccl::ortho_form({batch, rows, cols}).workspace_bytes : 0;
+  return ok();
+}
+
+ccl_status ccl_orthogonalize(int64_t batch, int64_t rows, int64_t cols, const void* G, ccl_dtype g_type, int64_t ld,
+                             int64_t stride, int steps, const float* coeffs, float eps, void* O, int64_t o_ld,
+                             int64_t o_stride, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (ccl_status s = check_ortho(batch, rows, cols)) return s;
+  if (g_type != CCL_DT_BF16 && g_type != CCL_DT_FP32) return fail(CCL_ERR_INVALID_ARG, "G must be bf16 or fp32");
+  if (steps < 0 || steps > 32) return fail(CCL_ERR_INVALID_ARG, "steps must be in 0..32");
+  ccl::OrthoCall c;
+  const float defaults[3] = {3.4445f, -4.7750f, 2.0315f};
+  for (int i = 0; i < 3; ++i) {
+    c.coeffs[i] = coeffs ? coeffs[i] : defaults[i];
+    if (!std::isfinite(c.coeffs[i])) return fail(CCL_ERR_INVALID_ARG, "coefficients must be finite");
+  }
+  if (!std::isfinite(eps) || eps < 0.f) return fail(CCL_ERR_INVALID_ARG, "eps must be finite and not negative");
+  if (batch == 0 || rows == 0 || cols == 0) return ok();
+  if (!G || !O) return fail(CCL_ERR_INVALID_ARG, "NULL argument");
+  constexpr int64_t kMaxStride = (int64_t)1 << 40;
+  const int64_t span = (rows - 1) * std::max<int64_t>(ld, 0) + cols, o_span = (rows - 1) * std::max<int64_t>(o_ld, 0) + cols;
+  if (ld < cols || o_ld < cols || ld > kMaxStride || o_ld > kMaxStride)
+    return fail(CCL_ERR_INVALID_ARG, "a leading dimension is smaller than the row");
+  if (batch > 1 && (stride < span || o_stride < o_span || stride > kMaxStride || o_stride > kMaxStride))
+    return fail(CCL_ERR_INVALID_ARG, "matrices of the batch overlap");
+  if (!aligned(G, g_type == CCL_DT_FP32 ? 4 : 2) || !aligned(O, 2))
+    return fail(CCL_ERR_MISALIGNED_POINTER, "G and O must be aligned to their elements");
+  const ccl::OrthoShape s{batch, rows, cols};
+  if (ccl_status st = check_workspace(ccl::ortho_form(s).workspace_bytes, workspace, workspace_bytes)) return st;
+  if (!aligned(workspace, 256)) return fail(CCL_ERR_MISALIGNED_POINTER, "the workspace must be 256-byte aligned");
+  if (ccl_status st = check_device()) return st;
+  c.G = G;
+  c.f32 = g_type == CCL_DT_FP32;
+  c.ld = ld;
+  c.stride = batch > 1 ? stride : 0;
+  c.O = O;
+  c.o_ld = o_ld;
+  c.o_stride = batch > 1 ? o_stride : 0;
+  c.steps = steps;
+  c.eps = eps;
+  return hip_status(ccl::launch_orthogonalize(s, c, workspace, static_cast<hipStream_t>(stream)), "orthogonalize launch");
 }
 
 }  // extern "C"

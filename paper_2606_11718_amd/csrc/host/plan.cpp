@@ -756,4 +756,31 @@ MoeForm moe_form(const MoeShape& s, int64_t tokens) {
   return f;
 }
 
+OrthoForm ortho_form(const OrthoShape& s) {
+  OrthoForm f;
+  const auto up = [](int64_t n, int64_t m) { return (n + m - 1) / m * m; };
+  f.pp = (int32_t)up(std::min(s.rows, s.cols), 128);
+  f.qp = (int32_t)up(std::max(s.rows, s.cols), 128);
+  f.chunks = (int32_t)std::min<int64_t>(1024, std::max<int64_t>(1, s.rows * s.cols / 16384));
+  // 256x256 tiles where they still give every CU one.
+  const auto tiles = [&](int64_t m, int64_t n, int b) { return ((m + b - 1) / b) * ((n + b - 1) / b); };
+  const int64_t t256 = (f.pp + 255) / 256;
+  f.tile_s = f.pp >= 256 && t256 * (t256 + 1) / 2 * s.batch >= 256 ? 256 : 128;
+  f.tile_x = f.pp >= 256 && tiles(f.pp, f.qp, 256) * s.batch >= 256 ? 256 : 128;
+  f.x_elems = (int64_t)f.pp * f.qp;
+  f.s_elems = (int64_t)f.pp * f.pp;
+  int64_t at = up(s.batch * f.chunks * 8, 256);
+  const auto take = [&](int64_t elems) {
+    const int64_t a = at;
+    at += up(s.batch * elems * 2, 256);
+    return a;
+  };
+  f.x_at[0] = take(f.x_elems);
+  f.x_at[1] = take(f.x_elems);
+  f.s_at = take(f.s_elems);
+  f.b_at = take(f.s_elems);
+  f.workspace_bytes = at;
+  return f;
+}
+
 }  // namespace ccl

@@ -215,4 +215,18 @@ struct MoeForm {
 };
 MoeForm moe_form(const MoeShape& s, int64_t tokens);
 
+// Newton-Schulz orthogonalisation of a batch of rows x cols matrices: padded
+// sides, tiles and the workspace (sums of squares; X twice, S and B in fp16).
+struct OrthoShape {
+  int64_t batch = 0, rows = 0, cols = 0;
+};
+struct OrthoForm {
+  int32_t pp = 0, qp = 0;           // padded smaller and larger side
+  int32_t chunks = 0;               // partial sums of squares per matrix
+  int tile_s = 0, tile_x = 0;       // tiles of the p x p products and of the last one
+  int64_t x_elems = 0, s_elems = 0; // per matrix
+  int64_t x_at[2] = {0, 0}, s_at = 0, b_at = 0, workspace_bytes = 0;
+};
+OrthoForm ortho_form(const OrthoShape& s);
+
 }  // namespace ccl

@@ -72,4 +72,17 @@ struct MoeCall {
 };
 hipError_t launch_moe(const MoeShape& s, const MoeCall& c, void* ws, hipStream_t stream);
 
+// One ccl_orthogonalize call; ws: ortho_form's workspace.
+struct OrthoCall {
+  const void* G = nullptr;
+  bool f32 = false;
+  int64_t ld = 0, stride = 0;
+  void* O = nullptr;
+  int64_t o_ld = 0, o_stride = 0;
+  int steps = 0;
+  float coeffs[3] = {0.f, 0.f, 0.f};
+  float eps = 0.f;
+};
+hipError_t launch_orthogonalize(const OrthoShape& s, const OrthoCall& c, void* ws, hipStream_t stream);
+
 }  // namespace ccl
