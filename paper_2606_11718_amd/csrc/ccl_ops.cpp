@@ -60,9 +60,9 @@ ccl_status check_moe(const ccl_moe* m, int64_t tokens, ccl::MoeShape* out) {
   if (m->normalize != 0 && m->normalize != 1) return fail(CCL_ERR_INVALID_ARG, "normalize must be 0 or 1");
   if (m->weight_type != CCL_DT_BF16 && m->weight_type != CCL_DT_FP8_E4M3)
     return fail(CCL_ERR_INVALID_ARG, "weights must be bf16 or fp8 E4M3");
-  constexpr int64_t kMaxSide = 1 << 24, kMaxStride = (int64_t)1 << 48;
+  constexpr int64_t kMaxSide = 1 << 22, kMaxStride = (int64_t)1 << 48;
   if (m->hidden % 16 || m->ffn % 16 || m->hidden > kMaxSide || m->ffn > kMaxSide)
-    return fail(CCL_ERR_UNSUPPORTED, "hidden and ffn must be multiples of 16 up to 2^24");
+    return fail(CCL_ERR_UNSUPPORTED, "hidden and ffn must be multiples of 16 up to 2^22");
   ccl::MoeShape s;
   s.hidden = m->hidden;
   s.ffn = m->ffn;
@@ -75,7 +75,7 @@ ccl_status check_moe(const ccl_moe* m, int64_t tokens, ccl::MoeShape* out) {
   s.gu_ld = m->gate_up_ld ? m->gate_up_ld : m->hidden;
   s.down_ld = m->down_ld ? m->down_ld : m->ffn;
   if (s.gu_ld < m->hidden || s.down_ld < m->ffn || s.gu_ld > kMaxSide || s.down_ld > kMaxSide)
-    return fail(CCL_ERR_INVALID_ARG, "a weight's leading dimension is smaller than its rows, or above 2^24");
+    return fail(CCL_ERR_INVALID_ARG, "a weight's leading dimension is smaller than its rows, or above 2^22");
   s.gu_stride = m->gate_up_stride ? m->gate_up_stride : 2 * m->ffn * s.gu_ld;
   s.down_stride = m->down_stride ? m->down_stride : m->hidden * s.down_ld;
   // an expert's last row need not be followed by a gap
@@ -84,8 +84,10 @@ ccl_status check_moe(const ccl_moe* m, int64_t tokens, ccl::MoeShape* out) {
     return fail(CCL_ERR_INVALID_ARG, "experts overlap, or lie more than 2^48 elements apart");
   if (s.gu_ld % per || s.gu_stride % per || s.down_ld % per || s.down_stride % per)
     return fail(CCL_ERR_MISALIGNED_POINTER, "weight rows and experts must lie whole 16 bytes apart");
+  if (tokens * s.top_k * s.ffn >= (int64_t)1 << 29)
+    return fail(CCL_ERR_UNSUPPORTED, "tokens * top_k * ffn must be below 2^29");
   const ccl::MoeForm f = ccl::moe_form(s, tokens);
-  if (f.up_workgroups > kMaxGrid || (int64_t)f.down_tiles * f.splits > kMaxGrid)
+  if (f.up_workgroups > kMaxGrid || (int64_t)f.down_groups * f.splits > kMaxGrid)
     return fail(CCL_ERR_UNSUPPORTED, "launch too large");
   *out = s;
   return CCL_OK;
@@ -226,9 +228,9 @@ ccl_status ccl_moe_decode(const ccl_moe* moe, int64_t tokens, const void* x, int
   if (ccl_status st = check_moe(moe, tokens, &s)) return st;
   if (tokens == 0) return ok();
   if (!x || !logits || !gate_up || !down || !y) return fail(CCL_ERR_INVALID_ARG, "NULL argument");
-  constexpr int64_t kMaxLd = (int64_t)1 << 48;
+  constexpr int64_t kMaxLd = (int64_t)1 << 22;    // 64 rows stay within 31-bit offsets
   if (x_ld < s.hidden || y_ld < s.hidden || logits_ld < s.experts || x_ld > kMaxLd || y_ld > kMaxLd || logits_ld > kMaxLd)
-    return fail(CCL_ERR_INVALID_ARG, "a leading dimension is smaller than its row");
+    return fail(CCL_ERR_INVALID_ARG, "a leading dimension is smaller than its row, or above 2^22");
   if (!aligned16(x) || x_ld % 8 || !aligned16(gate_up) || !aligned16(down))
     return fail(CCL_ERR_MISALIGNED_POINTER, "x (and its rows) and the weights must be 16-byte aligned");
   if (!aligned(logits, 4) || !aligned(gate_up_scale, 4) || !aligned(down_scale, 4) || !aligned(y, 2) ||

@@ -746,8 +746,17 @@ MoeForm moe_form(const MoeShape& s, int64_t tokens) {
   // token itself. Otherwise one per expert, which ranks that expert alone, and
   // workgroups in front that route.
   f.list = slots < s.experts;
-  f.up_workgroups = f.list ? slots * f.up_tiles : (int64_t)s.experts * f.up_tiles + (tokens + 7) / 8;
-  f.splits = 1;
+  // Up to two tiles per CU: a workgroup each. More: workgroups that stream their
+  // tiles, about three rounds of one per CU (some find no tokens).
+  const int64_t used = f.list ? slots : s.experts;
+  f.up_group = (int)std::max<int64_t>(1, used * f.up_tiles / 768);
+  const int64_t groups = (f.up_tiles + f.up_group - 1) / f.up_group;
+  f.up_workgroups = used * groups + (f.list ? 0 : (tokens + 7) / 8);
+  // The down product: ranges until every CU has a workgroup, of at least a
+  // 128-byte line of each row for every wave.
+  const int64_t lines = used * ((s.ffn * (s.fp8 ? 1 : 2) + 127) / 128);
+  f.down_groups = (f.down_tiles + kMoeDownTiles - 1) / kMoeDownTiles;
+  f.splits = (int)std::max<int64_t>(1, std::min<int64_t>(16, std::min<int64_t>(256 / f.down_groups, lines / 8)));
   const auto up16 = [](int64_t n) { return (n + 15) / 16 * 16; };
   f.probs_at = up16(slots * 4);
   f.h_at = f.probs_at + up16(slots * 4);

@@ -197,6 +197,7 @@ void launch_tile_of_wg(const Plan& p, int64_t wg, int* xcd, int64_t* tile_m, int
 
 // A mixture-of-experts FFN layer for a few tokens.
 constexpr int kMoeMaxTokens = 64, kMoeMaxExperts = 512, kMoeMaxTopK = 16;
+constexpr int kMoeDownTiles = 4;    // 16-column tiles of y per workgroup
 struct MoeShape {
   int64_t hidden = 0, ffn = 0;
   int experts = 0, top_k = 0, act = ACT_SILU;
@@ -209,7 +210,9 @@ struct MoeShape {
 struct MoeForm {
   bool list = false;                // up workgroups per chosen slot instead of per expert
   int up_tiles = 0, down_tiles = 0; // 16-row tiles of ffn and hidden
+  int up_group = 1;                 // up tiles per workgroup
   int64_t up_workgroups = 0;
+  int down_groups = 0;              // workgroups of a range of the down product
   int splits = 1;                   // ranges of the down product
   int64_t probs_at = 0, h_at = 0, part_at = 0, workspace_bytes = 0;
 };
