@@ -765,29 +765,81 @@ MoeForm moe_form(const MoeShape& s, int64_t tokens) {
   return f;
 }
 
+// The tiles of an m x n product of `steps` K steps of 64, and about how long it
+// takes in microseconds, by what was measured: rounds of workgroups over the
+// CUs, in each of which a tile takes `fixed` besides its K steps.
+//   256x256: one to a CU, 16 + 1.5 a step (3 rounds of 24 steps 157, 14 of 128
+//   2900, one of 64 115).
+//   128x128 with four LDS stages: one to a CU, up to one round, 6.4 + 0.3 a step
+//   (21 tiles of 12 and 32 steps 9.8 and 15.5; 136 tiles 0.4 a step).
+//   128x128 with two stages: two to a CU, 7 + 1.0 a step, or 0.6 alone (1248
+//   tiles of 24 steps 84, with four stages 90; 512 of 32 38).
+// The tiles past whole rounds may be cut into K ranges, of 4 steps at least,
+// which a further launch adds up (5, and reading the partials).
+static double ortho_split(int64_t m, int64_t n, int64_t steps, int64_t batch, bool sym, int tile, OrthoSplit* out) {
+  constexpr int64_t kCus = 256;
+  const auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+  const int64_t tm = up(m, tile), tn = up(n, tile);
+  const int64_t total = (sym ? tm * (tm + 1) / 2 : tm * tn) * batch;
+  out->tile = tile;
+  out->paired = tile == 128 && total > kCus;
+  out->whole = (int32_t)total;
+  out->splits = 1;
+  out->ksplit = (int32_t)steps;
+  out->part_elems = 0;
+  const int64_t slots = out->paired ? 2 * kCus : kCus;
+  const double fixed = tile == 256 ? 16.0 : out->paired ? 7.0 : 6.4;
+  const double step = tile == 256 ? 1.5 : out->paired ? 1.0 : total > 64 ? 0.4 : 0.3;
+  const int64_t whole = total / slots * slots, rest = total - whole;
+  const double rounds = (double)(whole / slots) * (fixed + step * (double)steps);
+  if (rest == 0) return rounds;
+  const double last = out->paired && rest <= kCus ? 0.6 : step;
+  double best = rounds + fixed + last * (double)steps;
+  const int64_t s = std::min<int64_t>(std::min<int64_t>(slots / rest, steps / 4), 16);
+  if (s < 2) return best;
+  const int64_t per = up(steps, s), ranges = up(steps, per), elems = rest * ranges * tile * tile;
+  const double split = rounds + fixed + step * (double)per + 5.0 + (double)elems * 4 / 4e6;
+  if (split < best) {
+    best = split;
+    out->whole = (int32_t)whole;
+    out->splits = (int32_t)ranges;
+    out->ksplit = (int32_t)per;
+    out->part_elems = elems;
+  }
+  return best;
+}
+
 OrthoForm ortho_form(const OrthoShape& s) {
   OrthoForm f;
   const auto up = [](int64_t n, int64_t m) { return (n + m - 1) / m * m; };
   f.pp = (int32_t)up(std::min(s.rows, s.cols), 128);
   f.qp = (int32_t)up(std::max(s.rows, s.cols), 128);
   f.chunks = (int32_t)std::min<int64_t>(1024, std::max<int64_t>(1, s.rows * s.cols / 16384));
-  // 256x256 tiles where they still give every CU one.
-  const auto tiles = [&](int64_t m, int64_t n, int b) { return ((m + b - 1) / b) * ((n + b - 1) / b); };
-  const int64_t t256 = (f.pp + 255) / 256;
-  f.tile_s = f.pp >= 256 && t256 * (t256 + 1) / 2 * s.batch >= 256 ? 256 : 128;
-  f.tile_x = f.pp >= 256 && tiles(f.pp, f.qp, 256) * s.batch >= 256 ? 256 : 128;
-  f.x_elems = (int64_t)f.pp * f.qp;
-  f.s_elems = (int64_t)f.pp * f.pp;
+  // Each product on the tiles that take least.
+  const auto best = [&](int64_t m, int64_t n, int64_t k, bool sym, OrthoSplit* out) {
+    const double t = ortho_split(m, n, k / 64, s.batch, sym, 128, out);
+    OrthoSplit large;
+    if (f.pp >= 256 && ortho_split(m, n, k / 64, s.batch, sym, 256, &large) < t) *out = large;
+  };
+  best(f.pp, f.pp, f.qp, true, &f.gram);
+  best(f.pp, f.pp, f.pp, true, &f.square);
+  best(f.pp, f.qp, f.pp, false, &f.update);
+  // Rows an odd number of 128-byte lines apart.
+  f.ld_p = f.pp + 64;
+  f.ld_q = f.qp + 64;
+  f.x_elems = (int64_t)f.pp * f.ld_q;
+  f.s_elems = (int64_t)f.pp * f.ld_p;
   int64_t at = up(s.batch * f.chunks * 8, 256);
-  const auto take = [&](int64_t elems) {
+  const auto take = [&](int64_t bytes) {
     const int64_t a = at;
-    at += up(s.batch * elems * 2, 256);
+    at += up(bytes, 256);
     return a;
   };
-  f.x_at[0] = take(f.x_elems);
-  f.x_at[1] = take(f.x_elems);
-  f.s_at = take(f.s_elems);
-  f.b_at = take(f.s_elems);
+  f.x_at[0] = take(s.batch * f.x_elems * 2);
+  f.x_at[1] = take(s.batch * f.x_elems * 2);
+  f.s_at = take(s.batch * f.s_elems * 2);
+  f.b_at = take(s.batch * f.s_elems * 2);
+  f.part_at = take(std::max({f.gram.part_elems, f.square.part_elems, f.update.part_elems}) * 4);
   f.workspace_bytes = at;
   return f;
 }

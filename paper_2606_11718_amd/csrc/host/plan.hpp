@@ -223,12 +223,21 @@ MoeForm moe_form(const MoeShape& s, int64_t tokens);
 struct OrthoShape {
   int64_t batch = 0, rows = 0, cols = 0;
 };
+// One product's tiles over the batch: the first `whole` by a workgroup each, the
+// rest cut into `splits` K ranges of ksplit steps of 64.
+struct OrthoSplit {
+  int tile = 0;                     // 128 or 256 squared
+  bool paired = false;              // 128: two workgroups of two LDS stages share a CU
+  int32_t whole = 0, splits = 1, ksplit = 0;
+  int64_t part_elems = 0;           // fp32 values of the ranges' partial tiles
+};
 struct OrthoForm {
   int32_t pp = 0, qp = 0;           // padded smaller and larger side
+  int32_t ld_p = 0, ld_q = 0;       // leading dimensions of rows that long
   int32_t chunks = 0;               // partial sums of squares per matrix
-  int tile_s = 0, tile_x = 0;       // tiles of the p x p products and of the last one
+  OrthoSplit gram, square, update;  // S = X X^T, B = b S + c S S, a X + B X
   int64_t x_elems = 0, s_elems = 0; // per matrix
-  int64_t x_at[2] = {0, 0}, s_at = 0, b_at = 0, workspace_bytes = 0;
+  int64_t x_at[2] = {0, 0}, s_at = 0, b_at = 0, part_at = 0, workspace_bytes = 0;
 };
 OrthoForm ortho_form(const OrthoShape& s);
 

@@ -34,6 +34,7 @@ struct NsParams {
   const uint16_t* D;        // addend, laid out as out (null: none)
   uint16_t* out;            // fp16 M x N
   uint16_t* O;              // the last product: bf16 result instead of out (else null)
+  float* part;              // fp32 tiles of the ranges of the split ones, in fragment order
   int64_t u_stride, v_stride, out_stride, o_stride;   // elements between matrices (D: out's)
   int64_t o_ld;
   int32_t M, N, K;          // padded
@@ -42,11 +43,14 @@ struct NsParams {
   int32_t o_trans;
   int32_t tiles_m, tiles_n; // per matrix; symmetric: tiles_m (tiles_m + 1) / 2 tiles
   int32_t tiles, total;     // per matrix, of the launch
-  int32_t per_xcd, group;
+  int32_t group;
+  int32_t whole;            // tiles computed by one workgroup each (a multiple of 8, or all)
+  int32_t splits, ksplit;   // the other tiles' K ranges, of ksplit steps
+  int32_t whole_xcd, split_xcd;   // workgroups of each kind per XCD
   float alpha, beta;
 };
 
-template <int BM, int BN, bool NT>
+template <int BM, int BN, bool NT, int NS_>
 struct NsTile {
   static constexpr int WGN = 4, NW = 8, THREADS = 512;
   static constexpr int WM = BM / 2, WN = BN / WGN;
@@ -54,27 +58,19 @@ struct NsTile {
   static constexpr int U_BYTES = BM * 128, V_BYTES = BN * 128;   // a stage of 64 K
   static constexpr int NU = U_BYTES / (1024 * NW), NV = V_BYTES / (1024 * NW), NL = NU + NV;
   static constexpr int CPR_V = BN / 8, RPI_V = 64 / CPR_V;       // 16-byte chunks and rows of a load (not NT)
-  static constexpr int kFit = (160 * 1024) / (U_BYTES + V_BYTES);
-  static constexpr int NS = kFit >= 4 ? 4 : 2;
+  static constexpr int NS = NS_;
   // With two stage buffers a step's loads go out behind its barrier, into the
   // buffer it has just read; otherwise NS - 1 stages ahead of it.
   static constexpr bool kLate = NS == 2;
   static constexpr int AHEAD = kLate ? 2 : NS - 1;
+  static_assert(NS == 2 || NS == 4, "the waits of a step are written for these");
   static_assert(NU >= 1 && NV >= 1 && NU <= 4 && NV <= 4, "a run of loads shares one M0");
   static_assert((BM / 2) * BN * 2 <= NS * U_BYTES && (BM / 2) * BN * 2 <= NS * V_BYTES, "the tile is staged in both");
 };
 
-// Workgroup -> matrix and tile. The tiles of all matrices are numbered matrix
-// by matrix and each XCD (workgroup mod 8) takes a contiguous range of them, so
-// that what is resident on one XCD together shares operands in its L2. Inside
-// a matrix: tile rows in groups, column by column.
+// Tile t of a matrix: tile rows in groups, column by column.
 template <bool SYM>
-__device__ __forceinline__ bool ns_tile_of(const NsParams& p, int32_t* mat, int32_t* ti, int32_t* tj) {
-  const int32_t xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
-  const int32_t id = xcd * p.per_xcd + slot;
-  if (slot >= p.per_xcd || id >= p.total) return false;
-  const int32_t m = id / p.tiles, t = id - m * p.tiles;
-  int32_t i, j;
+__device__ __forceinline__ void ns_tile(const NsParams& p, int32_t t, int32_t* ti, int32_t* tj) {
   const int32_t G = p.group;
   if constexpr (SYM) {
     // rows G r .. G r + G - 1 have G r (G r + 1) / 2 tiles before them
@@ -83,23 +79,55 @@ __device__ __forceinline__ bool ns_tile_of(const NsParams& p, int32_t* mat, int3
     const int32_t first = G * r, h = min(G, p.tiles_m - first);
     int32_t w = t - first * (first + 1) / 2;
     if (w < h * (first + 1)) {          // columns that every row of the group has
-      j = w / h;
-      i = first + w - j * h;
+      *tj = w / h;
+      *ti = first + w - *tj * h;
     } else {                            // the group's own triangle, below the diagonal's first column
       w -= h * (first + 1);
-      j = first + 1;
+      int32_t j = first + 1;
       while (w >= h - (j - first)) {
         w -= h - (j - first);
         ++j;
       }
-      i = j + w;
+      *tj = j;
+      *ti = j + w;
     }
   } else {
     const int32_t per = G * p.tiles_n, r = t / per, first = r * G, h = min(G, p.tiles_m - first);
     const int32_t w = t - r * per;
-    j = w / h;
-    i = first + w - j * h;
+    *tj = w / h;
+    *ti = first + w - *tj * h;
   }
+}
+
+// Workgroup -> matrix, tile and K steps [*k0, *k1). The tiles of all matrices
+// are numbered matrix by matrix and each XCD (workgroup mod 8) takes a
+// contiguous range of them, so that what is resident on one XCD together shares
+// operands in its L2. The tiles past p.whole are cut along K: with them, the
+// last round of workgroups fills the CUs (*part: where the range's partial
+// tile goes, else -1).
+template <bool SYM>
+__device__ __forceinline__ bool ns_work(const NsParams& p, int32_t* mat, int32_t* ti, int32_t* tj, int32_t* k0,
+                                        int32_t* k1, int32_t* part) {
+  const int32_t xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
+  int32_t id;
+  if (slot < p.whole_xcd) {
+    id = xcd * p.whole_xcd + slot;
+    if (id >= p.whole) return false;
+    *k0 = 0;
+    *k1 = p.K / 64;
+    *part = -1;
+  } else {
+    const int32_t v = xcd * p.split_xcd + slot - p.whole_xcd;
+    if (v >= (p.total - p.whole) * p.splits) return false;
+    const int32_t tile = v / p.splits, range = v - tile * p.splits;
+    id = p.whole + tile;
+    *k0 = __builtin_amdgcn_readfirstlane(range * p.ksplit);
+    *k1 = __builtin_amdgcn_readfirstlane(min(p.K / 64, range * p.ksplit + p.ksplit));
+    *part = __builtin_amdgcn_readfirstlane(v);
+  }
+  const int32_t m = id / p.tiles;
+  int32_t i, j;
+  ns_tile<SYM>(p, id - m * p.tiles, &i, &j);
   *mat = __builtin_amdgcn_readfirstlane(m);
   *ti = __builtin_amdgcn_readfirstlane(i);
   *tj = __builtin_amdgcn_readfirstlane(j);
@@ -151,23 +179,76 @@ __device__ __forceinline__ void ns_copy_out_trans(const StagedTile<BM, BN>& t, u
   }
 }
 
+// D's ROWS x COLS from row r0, column c0 into the staged tile. (Accumulators
+// that started from D instead, loaded in their own order with the first stages,
+// took 1 to 5 % longer: 32-byte pieces.)
+template <int ROWS, int COLS, int THREADS>
+__device__ __forceinline__ void ns_copy_in(const NsParams& p, const StagedTile<ROWS, COLS>& t, int mat, int r0, int c0,
+                                           int tid) {
+  constexpr int CPR = COLS / 8, N = ROWS * CPR / THREADS, B = N < 8 ? N : 8;
+  const uint16_t* d = p.D + mat * p.out_stride;
+  for (int i = 0; i < N; i += B) {
+    uint4 v[B];
+#pragma unroll
+    for (int j = 0; j < B; ++j) {
+      const int at = (i + j) * THREADS + tid, r = r0 + at / CPR, c = c0 + at % CPR * 8;
+      v[j] = make_uint4(0, 0, 0, 0);
+      if (r < p.M && c < p.N) v[j] = *reinterpret_cast<const uint4*>(d + (int64_t)r * p.ld_out + c);
+    }
+#pragma unroll
+    for (int j = 0; j < B; ++j) {
+      const int at = (i + j) * THREADS + tid;
+      *reinterpret_cast<uint4*>(t.chunk(at / CPR, at % CPR)) = v[j];
+    }
+  }
+}
+
+// alpha acc + beta D on four staged values, in place.
+__device__ __forceinline__ void ns_combine(const NsParams& p, uint2* at, f32x4 acc) {
+  f32x4 o = acc * p.alpha;
+  if (p.D) {
+    const f16x4 d = __builtin_bit_cast(f16x4, *at);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] = __builtin_fmaf(p.beta, (float)d[j], o[j]);
+  }
+  *at = p.O ? f32_to_bf16x4(o) : __builtin_bit_cast(uint2, __builtin_convertvector(o, f16x4));
+}
+
+// The staged tile (corner r0, c0) to where it goes: the result, or out, and off
+// the diagonal of a symmetric out to its mirror image.
+template <int ROWS, int COLS, bool SYM>
+__device__ __forceinline__ void ns_store(const NsParams& p, const StagedTile<ROWS, COLS>& t, int mat, int r0, int c0,
+                                         bool off_diagonal, int tid) {
+  const int wave = tid >> 6, lane = tid & 63;
+  if (p.O) {
+    uint16_t* O = p.O + mat * p.o_stride;
+    if (p.o_trans) ns_copy_out_trans<ROWS, COLS, 8>(t, O, p.o_ld, c0, r0, p.o_rows, p.o_cols, wave, lane);
+    else ns_copy_out<ROWS, COLS, 512>(t, O, p.o_ld, r0, c0, p.o_rows, p.o_cols, tid);
+    return;
+  }
+  uint16_t* out = p.out + mat * p.out_stride;
+  ns_copy_out<ROWS, COLS, 512>(t, out, p.ld_out, r0, c0, p.M, p.N, tid);
+  if (SYM && off_diagonal) ns_copy_out_trans<ROWS, COLS, 8>(t, out, p.ld_out, c0, r0, p.N, p.M, wave, lane);
+}
+
 // out = alpha U V' + beta D. The K loop is that of the GEMM's 64-K tiles: a
 // stage's two halves of 32 K around one barrier, the next half's fragments read
 // behind the MFMAs. U rows are 128 bytes with chunk c of row r at c ^
 // swz_a64(r), V's the same (NT) or 64 rows of BN with the transposing reads.
-template <int BM, int BN, bool NT, bool SYM>
-__global__ void __launch_bounds__(512, 2) ns_product_kernel(NsParams p) {
+// The symmetric products have K contiguous in both operands (NT).
+template <int BM, int BN, bool SYM, int NS>
+__global__ void __launch_bounds__(512, NS * (BM + BN) * 128 <= 80 * 1024 ? 4 : 2) ns_product_kernel(NsParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  using T = NsTile<BM, BN, NT>;
-  constexpr int NS = T::NS;
+  constexpr bool NT = SYM;
+  using T = NsTile<BM, BN, NT, NS>;
   __shared__ __attribute__((aligned(1024))) char smU[NS][T::U_BYTES];
   __shared__ __attribute__((aligned(1024))) char smV[NS][T::V_BYTES];
-  int32_t mat, ti, tj;
-  if (!ns_tile_of<SYM>(p, &mat, &ti, &tj)) return;
+  int32_t mat, ti, tj, k0, k1, part;
+  if (!ns_work<SYM>(p, &mat, &ti, &tj, &k0, &k1, &part)) return;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / T::WGN, wn = wave % T::WGN;
-  const int32_t ksteps = p.K / 64;
+  const int32_t ksteps = k1 - k0;
 
   // Per-lane byte offsets of the loads, minus the instruction offset of load i
   // of its run (rows are at least 128 elements: never negative).
@@ -220,8 +301,8 @@ __global__ void __launch_bounds__(512, 2) ns_product_kernel(NsParams p) {
   auto load_one = [&](int32_t s, int i) __attribute__((always_inline)) {
     char* su = smU[0] + (s % NS) * T::U_BYTES;
     char* sv = smV[0] + (s % NS) * T::V_BYTES;
-    if (i < T::NU) lds_dma16_run<false>(u_desc, u_voff[i], (uint32_t)s * 128u, su + (wave * T::NU + i) * 1024, i);
-    else lds_dma16_run<false>(v_desc, v_voff[i - T::NU], (uint32_t)s * v_adv, sv + (wave * T::NV + i - T::NU) * 1024, i - T::NU);
+    if (i < T::NU) lds_dma16_run<false>(u_desc, u_voff[i], (uint32_t)(k0 + s) * 128u, su + (wave * T::NU + i) * 1024, i);
+    else lds_dma16_run<false>(v_desc, v_voff[i - T::NU], (uint32_t)(k0 + s) * v_adv, sv + (wave * T::NV + i - T::NU) * 1024, i - T::NU);
   };
   // Loads past the last stage must not touch memory, but keep the count.
   auto end_loads = [&](int32_t s) __attribute__((always_inline)) {
@@ -270,8 +351,8 @@ __global__ void __launch_bounds__(512, 2) ns_product_kernel(NsParams p) {
     end_loads(s + T::AHEAD);
     const auto load = [&](int i) __attribute__((always_inline)) {
       const int at = (ph + T::AHEAD) % NS;
-      if (i < T::NU) lds_dma16_run<false>(u_desc, u_voff[i], (uint32_t)(s + T::AHEAD) * 128u, smU[at] + (wave * T::NU + i) * 1024, i);
-      else lds_dma16_run<false>(v_desc, v_voff[i - T::NU], (uint32_t)(s + T::AHEAD) * v_adv, smV[at] + (wave * T::NV + i - T::NU) * 1024, i - T::NU);
+      if (i < T::NU) lds_dma16_run<false>(u_desc, u_voff[i], (uint32_t)(k0 + s + T::AHEAD) * 128u, smU[at] + (wave * T::NU + i) * 1024, i);
+      else lds_dma16_run<false>(v_desc, v_voff[i - T::NU], (uint32_t)(k0 + s + T::AHEAD) * v_adv, smV[at] + (wave * T::NV + i - T::NU) * 1024, i - T::NU);
     };
 #pragma unroll
     for (int i = 0; i < kAll1; ++i) {
@@ -321,56 +402,64 @@ __global__ void __launch_bounds__(512, 2) ns_product_kernel(NsParams p) {
   for (int j = 0; j < NS - 1; ++j)
     if (s + j < ksteps) step(j, s + j);
 
-  // Epilogue: D line by line into the stage buffers, combined in place.
+  if (part >= 0) {
+    f32x4* to = reinterpret_cast<f32x4*>(p.part + (int64_t)part * (BM * BN));
+#pragma unroll
+    for (int mt = 0; mt < T::TM; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < T::TN; ++nt) to[frag_index<T::TM, T::TN, 1>(wave, mt, nt, 0, lane)] = acc[mt][nt];
+    return;
+  }
+  // Epilogue: through the stage buffers, so that whole lines are stored.
   __builtin_amdgcn_s_waitcnt(0);
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   const StagedTile<BM, BN> t{smU[0], smV[0]};
   if (p.D) {
-    constexpr int CPR = BN / 8, N = BM * CPR / T::THREADS, B = N < 8 ? N : 8;
-    const uint16_t* d = p.D + mat * p.out_stride;
-    for (int i = 0; i < N; i += B) {
-      uint4 v[B];
-#pragma unroll
-      for (int j = 0; j < B; ++j) {
-        const int at = (i + j) * T::THREADS + tid, r = ti * BM + at / CPR, c = tj * BN + at % CPR * 8;
-        v[j] = make_uint4(0, 0, 0, 0);
-        if (r < p.M && c < p.N) v[j] = *reinterpret_cast<const uint4*>(d + (int64_t)r * p.ld_out + c);
-      }
-#pragma unroll
-      for (int j = 0; j < B; ++j) {
-        const int at = (i + j) * T::THREADS + tid;
-        *reinterpret_cast<uint4*>(t.chunk(at / CPR, at % CPR)) = v[j];
-      }
-    }
+    ns_copy_in<BM, BN, T::THREADS>(p, t, mat, ti * BM, tj * BN, tid);
     staged_barrier();
   }
 #pragma unroll
   for (int mt = 0; mt < T::TM; ++mt)
 #pragma unroll
-    for (int nt = 0; nt < T::TN; ++nt) {
-      uint2* at = t.at(wm * T::WM + 16 * mt + (lane & 15), wn * T::WN + 16 * nt + 4 * (lane >> 4));
-      f32x4 o = acc[mt][nt] * p.alpha;
-      if (p.D) {
-        const f16x4 d = __builtin_bit_cast(f16x4, *at);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) o[j] = __builtin_fmaf(p.beta, (float)d[j], o[j]);
-      }
-      *at = p.O ? f32_to_bf16x4(o) : __builtin_bit_cast(uint2, __builtin_convertvector(o, f16x4));
-    }
+    for (int nt = 0; nt < T::TN; ++nt)
+      ns_combine(p, t.at(wm * T::WM + 16 * mt + (lane & 15), wn * T::WN + 16 * nt + 4 * (lane >> 4)), acc[mt][nt]);
   staged_barrier();
-  if (p.O) {
-    uint16_t* O = p.O + mat * p.o_stride;
-    if (p.o_trans) ns_copy_out_trans<BM, BN, T::NW>(t, O, p.o_ld, tj * BN, ti * BM, p.o_rows, p.o_cols, wave, lane);
-    else ns_copy_out<BM, BN, T::THREADS>(t, O, p.o_ld, ti * BM, tj * BN, p.o_rows, p.o_cols, tid);
-    return;
-  }
-  uint16_t* out = p.out + mat * p.out_stride;
-  ns_copy_out<BM, BN, T::THREADS>(t, out, p.ld_out, ti * BM, tj * BN, p.M, p.N, tid);
-  if constexpr (SYM)
-    if (ti != tj) ns_copy_out_trans<BM, BN, T::NW>(t, out, p.ld_out, tj * BN, ti * BM, p.M, p.N, wave, lane);
+  ns_store<BM, BN, SYM>(p, t, mat, ti * BM, tj * BN, ti != tj, tid);
 #endif
+}
+
+// The split tiles: ranges summed in order. A workgroup takes 32 rows of a tile
+// (two rows of 16x16 tiles of one row of waves).
+template <int B, bool SYM>
+__global__ void __launch_bounds__(512) ns_split_sum_kernel(NsParams p) {
+  using T = NsTile<B, B, true, 2>;
+  constexpr int PARTS = B / 32, FRAGS = 2 * B / 16;          // 16x16 tiles of a part
+  __shared__ __attribute__((aligned(16))) char sm[32 * B * 2];
+  const int32_t tile = blockIdx.x / PARTS, row0 = blockIdx.x % PARTS * 32;
+  const int32_t id = p.whole + tile, mat = id / p.tiles;
+  int32_t ti, tj;
+  ns_tile<SYM>(p, id - mat * p.tiles, &ti, &tj);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const StagedTile<32, B> t{sm, sm + 32 * B};
+  if (p.D) {
+    ns_copy_in<32, B, 512>(p, t, mat, ti * B + row0, tj * B, tid);
+    __syncthreads();
+  }
+  const f32x4* from = reinterpret_cast<const f32x4*>(p.part + (int64_t)tile * p.splits * (B * B));
+#pragma unroll
+  for (int i = 0; i < FRAGS / 8; ++i) {
+    const int f = wave * (FRAGS / 8) + i, sub = f % 2, col = f / 2;          // 16-row half, 16-column tile
+    const int w = row0 / T::WM * T::WGN + col / T::TN;                       // the wave that computed it
+    const int at = frag_index<T::TM, T::TN, 1>(w, row0 % T::WM / 16 + sub, col % T::TN, 0, lane);
+    f32x4 v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int r = 0; r < p.splits; ++r) v += from[(int64_t)r * (B * B / 4) + at];
+    ns_combine(p, t.at(16 * sub + (lane & 15), 16 * col + 4 * (lane >> 4)), v);
+  }
+  __syncthreads();
+  ns_store<32, B, SYM>(p, t, mat, ti * B + row0, tj * B, ti != tj, tid);
 }
 
 // ---- the norm and the first X ----
@@ -384,7 +473,7 @@ struct NsInput {
   int32_t chunks;
   uint16_t* X;              // fp16 pp x qp
   int64_t x_stride;
-  int32_t pp, qp, tall;
+  int32_t pp, qp, ld_x, tall;
   float eps;
 };
 
@@ -455,7 +544,7 @@ __global__ void __launch_bounds__(256) ns_first_kernel(NsInput p) {
   const float scale = (float)(kScale / (sqrt(block_sum(sum, sm)) + (double)p.eps));
   // the tile in G: rows g_r .., columns g_c ..
   const int64_t g_r = 64 * (int64_t)(p.tall ? tc : tr), g_c = 64 * (int64_t)(p.tall ? tr : tc);
-  uint16_t* X = p.X + mat * p.x_stride;
+  uint16_t* X = p.X + mat * p.x_stride + 64 * (int64_t)tr * p.ld_x + 64 * tc;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int at = i * 256 + threadIdx.x, r = at >> 3, c = (at & 7) * 8;
@@ -465,7 +554,7 @@ __global__ void __launch_bounds__(256) ns_first_kernel(NsInput p) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) o[j] = (_Float16)(v[j] * scale);
     if (!p.tall) {
-      *reinterpret_cast<f16x8*>(X + (64 * (int64_t)tr + r) * p.qp + 64 * tc + c) = o;
+      *reinterpret_cast<f16x8*>(X + (int64_t)r * p.ld_x + c) = o;
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -479,7 +568,7 @@ __global__ void __launch_bounds__(256) ns_first_kernel(NsInput p) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int at = i * 256 + threadIdx.x, r = at >> 3, c = (at & 7) * 8;
-    *reinterpret_cast<uint4*>(X + (64 * (int64_t)tr + r) * p.qp + 64 * tc + c) = *reinterpret_cast<const uint4*>(&st[r][c]);
+    *reinterpret_cast<uint4*>(X + (int64_t)r * p.ld_x + c) = *reinterpret_cast<const uint4*>(&st[r][c]);
   }
 }
 
@@ -495,15 +584,30 @@ __global__ void __launch_bounds__(256) ns_copy_kernel(const uint16_t* X, int64_t
   O[mat * o_stride + r * o_ld + c] = __builtin_bit_cast(uint16_t, (__bf16)(v / kScale));
 }
 
-template <int B, bool NT, bool SYM>
-void ns_launch(NsParams p, int64_t batch, hipStream_t stream) {
-  p.tiles_m = (p.M + B - 1) / B;
-  p.tiles_n = (p.N + B - 1) / B;
+// One product of the batch.
+template <bool SYM>
+hipError_t ns_launch(NsParams p, int64_t batch, const OrthoSplit& f, hipStream_t stream) {
+  const int b = f.tile;
+  p.tiles_m = (p.M + b - 1) / b;
+  p.tiles_n = (p.N + b - 1) / b;
   p.tiles = SYM ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
   p.total = (int32_t)(p.tiles * batch);
-  p.per_xcd = (p.total + 7) / 8;
   p.group = p.tiles_m < 8 ? p.tiles_m : 8;
-  hipLaunchKernelGGL((ns_product_kernel<B, B, NT, SYM>), dim3((unsigned)(8 * p.per_xcd)), dim3(512), 0, stream, p);
+  p.whole = f.whole;
+  p.splits = f.splits;
+  p.ksplit = f.ksplit;
+  p.whole_xcd = (f.whole + 7) / 8;
+  const int32_t rest = p.total - p.whole;
+  p.split_xcd = (rest * f.splits + 7) / 8;
+  const dim3 grid((unsigned)(8 * (p.whole_xcd + p.split_xcd))), block(512);
+  if (b == 128 && f.paired) hipLaunchKernelGGL((ns_product_kernel<128, 128, SYM, 2>), grid, block, 0, stream, p);
+  else if (b == 128) hipLaunchKernelGGL((ns_product_kernel<128, 128, SYM, 4>), grid, block, 0, stream, p);
+  else hipLaunchKernelGGL((ns_product_kernel<256, 256, SYM, 2>), grid, block, 0, stream, p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || rest == 0) return e;
+  if (b == 128) hipLaunchKernelGGL((ns_split_sum_kernel<128, SYM>), dim3((unsigned)(rest * 4)), block, 0, stream, p);
+  else hipLaunchKernelGGL((ns_split_sum_kernel<256, SYM>), dim3((unsigned)(rest * 8)), block, 0, stream, p);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -511,9 +615,9 @@ void ns_launch(NsParams p, int64_t batch, hipStream_t stream) {
 hipError_t launch_orthogonalize(const OrthoShape& s, const OrthoCall& c, void* ws, hipStream_t stream) {
   const OrthoForm f = ortho_form(s);
   char* base = static_cast<char*>(ws);
-  uint16_t* x[2] = {reinterpret_cast<uint16_t*>(base + f.x_at[0]), reinterpret_cast<uint16_t*>(base + f.x_at[1])};
-  uint16_t* S = reinterpret_cast<uint16_t*>(base + f.s_at);
-  uint16_t* B = reinterpret_cast<uint16_t*>(base + f.b_at);
+  const auto at = [&](int64_t offset) { return reinterpret_cast<uint16_t*>(base + offset); };
+  uint16_t *S = at(f.s_at), *B = at(f.b_at);
+  uint16_t* x[2] = {at(f.x_at[0]), at(f.x_at[1])};
   const bool tall = s.rows > s.cols;
 
   NsInput in;
@@ -529,6 +633,7 @@ hipError_t launch_orthogonalize(const OrthoShape& s, const OrthoCall& c, void* w
   in.x_stride = f.x_elems;
   in.pp = f.pp;
   in.qp = f.qp;
+  in.ld_x = f.ld_q;
   in.tall = tall ? 1 : 0;
   in.eps = c.eps;
   hipLaunchKernelGGL(ns_square_kernel, dim3((unsigned)(f.chunks * s.batch)), dim3(256), 0, stream, in);
@@ -539,7 +644,7 @@ hipError_t launch_orthogonalize(const OrthoShape& s, const OrthoCall& c, void* w
   if (e != hipSuccess) return e;
   if (c.steps == 0) {
     const int64_t blocks = (s.rows * s.cols + 255) / 256 * s.batch;
-    hipLaunchKernelGGL(ns_copy_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, x[0], f.x_elems, f.qp,
+    hipLaunchKernelGGL(ns_copy_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, x[0], f.x_elems, f.ld_q,
                        static_cast<uint16_t*>(c.O), c.o_stride, c.o_ld, s.rows, s.cols, in.tall);
     return hipGetLastError();
   }
@@ -547,50 +652,46 @@ hipError_t launch_orthogonalize(const OrthoShape& s, const OrthoCall& c, void* w
     const uint16_t* X = x[step & 1];
     const bool last = step + 1 == c.steps;
     NsParams p{};
+    p.part = reinterpret_cast<float*>(base + f.part_at);
     p.o_ld = c.o_ld;
     p.o_stride = c.o_stride;
     p.o_rows = (int32_t)s.rows;
     p.o_cols = (int32_t)s.cols;
-    p.o_trans = in.tall;
     // S = X X^T
     p.U = p.V = X;
     p.u_stride = p.v_stride = f.x_elems;
-    p.ldu = p.ldv = f.qp;
+    p.ldu = p.ldv = f.ld_q;
     p.out = S;
     p.out_stride = f.s_elems;
-    p.ld_out = f.pp;
+    p.ld_out = f.ld_p;
     p.M = p.N = f.pp;
     p.K = f.qp;
     p.alpha = 1.f / kScale;
-    if (f.tile_s == 256) ns_launch<256, true, true>(p, s.batch, stream);
-    else ns_launch<128, true, true>(p, s.batch, stream);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if ((e = ns_launch<true>(p, s.batch, f.gram, stream)) != hipSuccess) return e;
     // B = b S + c S S (S is its own transpose)
     p.U = p.V = p.D = S;
     p.u_stride = p.v_stride = f.s_elems;
-    p.ldu = p.ldv = f.pp;
+    p.ldu = p.ldv = f.ld_p;
     p.out = B;
     p.K = f.pp;
     p.alpha = c.coeffs[2] / kScale;
     p.beta = c.coeffs[1];
-    if (f.tile_s == 256) ns_launch<256, true, true>(p, s.batch, stream);
-    else ns_launch<128, true, true>(p, s.batch, stream);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if ((e = ns_launch<true>(p, s.batch, f.square, stream)) != hipSuccess) return e;
     // X <- a X + B X
     p.U = B;
     p.V = p.D = X;
     p.v_stride = f.x_elems;
-    p.ldv = f.qp;
+    p.ldv = f.ld_q;
     p.out = x[(step + 1) & 1];
     p.out_stride = f.x_elems;
-    p.ld_out = f.qp;
+    p.ld_out = f.ld_q;
     p.N = f.qp;
+    p.o_trans = in.tall;
     p.O = last ? static_cast<uint16_t*>(c.O) : nullptr;
     p.alpha = last ? 1.f / (kScale * kScale) : 1.f / kScale;
     p.beta = last ? c.coeffs[0] / kScale : c.coeffs[0];
-    if (f.tile_x == 256) ns_launch<256, false, false>(p, s.batch, stream);
-    else ns_launch<128, false, false>(p, s.batch, stream);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    e = ns_launch<false>(p, s.batch, f.update, stream);
+    if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
