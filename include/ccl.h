@@ -317,11 +317,12 @@ typedef struct ccl_epilogue {
 } ccl_epilogue;
 
 /*
- * ccl_gemm_fused_workspace: in: *splits = K ranges per tile (1..16, or 0 to
- * choose, as ccl_gemm_splitk_workspace); out: the ranges used and the device
- * workspace of ccl_gemm_fused for that request in bytes, which is not zero
- * with one range either where the plan's GEMM kernel has no fused epilogue
- * (the product's fp32 tiles then pass through it).
+ * ccl_gemm_fused_workspace: in: *splits = the most K ranges per tile (1..16, or
+ * 0 to choose); out: the ranges used, which are no more than give each of an
+ * XCD's compute units a workgroup (as ccl_gemm_splitk_workspace chooses them),
+ * and the device workspace of ccl_gemm_fused for that request in bytes, which is
+ * not zero with one range either where the plan's GEMM kernel has no fused
+ * epilogue (the product's fp32 tiles then pass through it).
  *
  * ccl_gemm_fused: the product and epilogue above, for plans with a bf16 C
  * (A and B bf16 or fp8 E4M3). All matrices 16-byte aligned; none may overlap

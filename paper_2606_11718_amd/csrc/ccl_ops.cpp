@@ -176,7 +176,7 @@ ccl_status ccl_gemm_fused_grad_workspace(ccl_plan_t plan, ccl_operand_layout lay
   if (!plan || !workspace_bytes) return fail(CCL_ERR_INVALID_ARG, "NULL argument");
   if (dbias != 0 && dbias != 1) return fail(CCL_ERR_INVALID_ARG, "dbias must be 0 or 1");
   ccl::FusedForm f;
-  if (ccl_status s = check_fused(plan, layout, CCL_ACT_NONE, gated, 0, 1, true, dbias == 1, &f)) return s;
+  if (ccl_status s = check_fused(plan, layout, CCL_ACT_NONE, gated, 0, ccl::kMaxSplits, true, dbias == 1, &f)) return s;
   *workspace_bytes = f.workspace_bytes;
   return ok();
 }
@@ -185,7 +185,8 @@ ccl_status ccl_gemm_fused_grad(ccl_plan_t plan, const ccl_epilogue_grad* e, cons
                                void* workspace, int64_t workspace_bytes, void* stream) {
   if (!plan || !e || !A || !B || !dZ) return fail(CCL_ERR_INVALID_ARG, "NULL argument");
   ccl::FusedForm f;
-  if (ccl_status s = check_fused(plan, e->layout, e->activation, e->gated, e->rows, 1, true, e->dbias != nullptr, &f))
+  if (ccl_status s = check_fused(plan, e->layout, e->activation, e->gated, e->rows, ccl::kMaxSplits, true,
+                                 e->dbias != nullptr, &f))
     return s;
   const bool linear = e->activation == CCL_ACT_NONE && e->gated == 0;
   if (!e->preact && !linear) return fail(CCL_ERR_INVALID_ARG, "NULL preact");
@@ -205,7 +206,7 @@ ccl_status ccl_gemm_fused_grad(ccl_plan_t plan, const ccl_epilogue_grad* e, cons
   c.act = e->activation;
   c.alpha = e->alpha;
   c.rows = e->rows;
-  return hip_status(ccl::launch_gemm_fused(plan->plan, c, 1, workspace, static_cast<hipStream_t>(stream)),
+  return hip_status(ccl::launch_gemm_fused(plan->plan, c, ccl::kMaxSplits, workspace, static_cast<hipStream_t>(stream)),
                     "fused gradient gemm launch");
 }
 

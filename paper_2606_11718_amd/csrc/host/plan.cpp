@@ -717,6 +717,10 @@ FusedForm fused_form(const Plan& plan, bool rowmajor, int splits, bool grad, boo
   OperandAddr c;
   if (rowmajor) rowmajor_addressing(p, &f.a, &f.b, &c);
   else ccl_addressing(p, &f.a, &f.b, &c);
+  // K ranges only while there are CUs without a tile: past that they add traffic
+  // (896x5120x768: 4 ranges 38 us, 1 range 12). The gradient takes as many by
+  // itself where K is long.
+  splits = std::min(grad && p.K < 2048 ? 1 : splits, recommended_splits(p));
   f.gemm = gemm_form(p, f.a, f.b, true, splits);
   f.z_cols = grad && gated ? 2 * p.N : p.N;
   f.c_cols = grad ? f.z_cols : gated ? p.N / 2 : p.N;
@@ -728,9 +732,9 @@ FusedForm fused_form(const Plan& plan, bool rowmajor, int splits, bool grad, boo
   // whose K blocks are odd multiples of the K step, 4 waves, operands of 2 GiB
   // and more) pass through one range's partials.
   const GemmKernel k = f.gemm.kernel;
-  f.direct = f.gemm.splits == 1 && f.gemm.waves == 8 &&
-             (k == GemmKernel::A2 || k == GemmKernel::FP8P || k == GemmKernel::FP8S ||
-              (k == GemmKernel::K64 && !f.gemm.far));
+  f.own = f.gemm.waves == 8 && (k == GemmKernel::A2 || k == GemmKernel::FP8P || k == GemmKernel::FP8S ||
+                                (k == GemmKernel::K64 && !f.gemm.far));
+  f.direct = f.own && f.gemm.splits == 1;
   f.sum_rows = f.direct ? f.gemm.tile_m : k == GemmKernel::FP8 ? 32 : 16;
   f.partial_bytes = f.direct ? 0 : (int64_t)p.G * p.gemm.tiles_m * p.gemm.tiles_n * f.gemm.splits * p.gemm.tile_m * p.gemm.tile_n * 4;
   f.workspace_bytes = f.partial_bytes + (dbias ? p.M / f.sum_rows * f.z_cols * 4 : 0);

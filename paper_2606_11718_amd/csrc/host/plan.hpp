@@ -185,6 +185,7 @@ struct FusedForm {
   OperandAddr a, b, c, z;
   int64_t z_cols = 0, c_cols = 0;
   bool direct = false;              // the GEMM's kernel has the epilogue itself (else: by way of partials)
+  bool own = false;                 // the GEMM's kernel knows the valid rows
   int sum_rows = 0;                 // rows of one block of column sums
   bool c_nt = false;
   int64_t partial_bytes = 0;        // fp32 partial tiles

@@ -139,12 +139,14 @@ __device__ __forceinline__ int64_t tile_corner(const OperandAddr& o, int32_t pr,
   return pr * o.part + pc * o.slice + (int64_t)(ti * BM) * o.ld + col;
 }
 
-// A tile wholly past the valid rows: zeros, and no column sums (the reduce
-// does not read its block). Whether it was one.
+// A tile wholly past the valid rows: zeros, and no column sums or partials (the
+// reduces do not read them; with partials, theirs writes the zeros). Whether it
+// was one.
 template <int BM, int BN, int THREADS, bool GRAD>
 __device__ __forceinline__ bool dead_tile(const FusedParams& p, int32_t pr, int32_t pc, int32_t ti, int32_t tj) {
   const FusedEpi& e = p.e;
   if (pr * e.part_rows + (int64_t)ti * BM < e.rows) return false;
+  if (p.ws) return true;
   const int tid = threadIdx.x;
   uint16_t* C = static_cast<uint16_t*>(p.C);
   const auto zero = [&](uint16_t* m, const OperandAddr& o, auto cols) {

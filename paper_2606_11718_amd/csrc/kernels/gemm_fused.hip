@@ -200,9 +200,10 @@ static hipError_t launch_fused_reduce(const Plan& p, FusedParams fp, int md, int
   return hipGetLastError();
 }
 
-// The kernel of a form with an epilogue of its own (FusedForm::direct).
+// A form with kernels of its own here (FusedForm::own): with the epilogue, or,
+// with a workspace, the partials of the tiles that have valid rows.
 template <bool GRAD>
-static hipError_t launch_direct(const GemmForm& f, const FusedParams& fp, hipStream_t stream) {
+static hipError_t launch_own(const GemmForm& f, const FusedParams& fp, hipStream_t stream) {
   FusedTileParams<GRAD> p;
   static_cast<FusedParams&>(p) = fp;
   const dim3 grid((unsigned)f.workgroups), block(512);
@@ -253,12 +254,13 @@ hipError_t launch_gemm_fused(const Plan& plan, const FusedCall& call, int splits
   fp.e.bias_f32 = call.bias_f32 ? 1 : 0;
   fp.e.beta = call.beta;
   hipError_t e;
+  if (!ff.direct) fp.ws = static_cast<float*>(ws);
+  if (ff.own) e = call.grad ? launch_own<true>(f, fp, stream) : launch_own<false>(f, fp, stream);
   if (ff.direct) {
-    e = call.grad ? launch_direct<true>(f, fp, stream) : launch_direct<false>(f, fp, stream);
+    if (e != hipSuccess) return e;
   } else {
-    int md, wgm;
-    fp.ws = static_cast<float*>(ws);
-    e = launch_gemm_partials(p, f, call.A, call.B, ff.a, ff.b, fp.ws, stream, &md, &wgm);
+    int md = 16, wgm = f.kernel == GemmKernel::FP8S && f.tile_m == 256 ? 4 : 2;
+    if (!ff.own) e = launch_gemm_partials(p, f, call.A, call.B, ff.a, ff.b, fp.ws, stream, &md, &wgm);
     if (e != hipSuccess) return e;
     e = call.grad ? launch_fused_reduce<true>(p, fp, md, f.waves, wgm, stream)
                   : launch_fused_reduce<false>(p, fp, md, f.waves, wgm, stream);

@@ -1354,9 +1354,10 @@ __device__ __forceinline__ void k64_tile(const P& p) {
   constexpr int kBuf = kInB ? NS * T::B_BYTES / 2
                             : NS * T::A_BYTES < NS * T::B_BYTES ? NS * T::A_BYTES : NS * T::B_BYTES;
   char* const lo = kInB ? &smB[0][0] + kBuf : &smA[0][0];
-  if constexpr (kFused<P>)
-    fused_epilogue<BM, BN, T::NW, T::TM, T::TN, T::WM, T::WN>(p, acc, lo, &smB[0][0], pr, pc, ti, tj, wm, wn, tid);
-  else
+  if constexpr (kFused<P>) {
+    if (p.ws) store_tile<BM, BN, 16, T::TM, T::TN, T::WM, T::WN>(p, acc, pr, pc, ti, tj, split, wm, wn, lane);
+    else fused_epilogue<BM, BN, T::NW, T::TM, T::TN, T::WM, T::WN>(p, acc, lo, &smB[0][0], pr, pc, ti, tj, wm, wn, tid);
+  } else
     epilogue16<BM, BN, T::NW, T::TM, T::TN, T::WM, T::WN, kBuf, BNT ? 2 : 1>(p, acc, lo, &smB[0][0], pr, pc,
                                                                     ti, tj, split, wm, wn, wave, lane);
   if (tl_on) record_timeline(p.timeline + ((int64_t)blockIdx.x * T::NW + wave) * kTimelineWords,
@@ -2778,9 +2779,10 @@ __device__ __forceinline__ void fp8s_tile(const P& p) {
   int ln = lane;
   asm volatile("" : "+v"(ln));
   constexpr int kBuf = NS * T::A_BYTES < NS * T::B_BYTES ? NS * T::A_BYTES : NS * T::B_BYTES;
-  if constexpr (kFused<P>)
-    fused_epilogue<BM, BN, T::NW, T::TM, T::TN, T::WM, T::WN>(p, acc, &smA[0][0], &smB[0][0], pr, pc, ti, tj, wm, wn, tid);
-  else
+  if constexpr (kFused<P>) {
+    if (p.ws) store_tile<BM, BN, 16, T::TM, T::TN, T::WM, T::WN>(p, acc, pr, pc, ti, tj, split, wm, wn, lane);
+    else fused_epilogue<BM, BN, T::NW, T::TM, T::TN, T::WM, T::WN>(p, acc, &smA[0][0], &smB[0][0], pr, pc, ti, tj, wm, wn, tid);
+  } else
     epilogue16<BM, BN, T::NW, T::TM, T::TN, T::WM, T::WN, kBuf, 1>(p, acc, &smA[0][0], &smB[0][0], pr, pc,
                                                                     ti, tj, split, wm, wn, wave, ln);
 }

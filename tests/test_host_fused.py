@@ -72,9 +72,11 @@ def test_fp32_results_and_operands_are_refused():
 
 def test_queries():
     plan = _plan()
-    ranges, need = ccl.ccl_gemm_fused_workspace(plan, 4)
-    assert ranges == 4 and need == ccl.ccl_gemm_splitk_workspace(plan, 4)[1]
-    assert ccl.ccl_gemm_fused_workspace(plan, 0)[0] == ccl.ccl_gemm_splitk_workspace(plan, 0)[0]
+    chosen = ccl.ccl_gemm_splitk_workspace(plan, 0)[0]
+    assert chosen == 2                               # 16 K steps in ranges of 8
+    for asked in (0, 2, 4):                          # no more than the CUs have use for
+        assert ccl.ccl_gemm_fused_workspace(plan, asked) == ccl.ccl_gemm_splitk_workspace(plan, chosen)
+    assert ccl.ccl_gemm_fused_workspace(plan, 1) == (1, 0)
     _refused("CCL_ERR_INVALID_ARG", ccl.ccl_gemm_fused_workspace, plan, 17)
     _refused("CCL_ERR_INVALID_ARG", ccl.ccl_gemm_fused_workspace, plan, -1)
     _refused("CCL_ERR_INVALID_ARG", ccl.ccl_gemm_fused_workspace, plan, 1, layout=5)
