@@ -710,7 +710,7 @@ OperandAddr matrix_addressing(const Plan& p, int64_t cols, bool rowmajor) {
   return {p.Gc * s, s, (int32_t)(cols / p.Gc), 0};
 }
 
-FusedForm fused_form(const Plan& plan, bool rowmajor, int splits, bool grad, bool gated, bool dbias) {
+FusedForm fused_form(const Plan& plan, bool rowmajor, int splits, bool grad, bool gated, bool dbias, int64_t rows) {
   Plan p = plan;
   p.gemm.wide_n = 0;      // the workspace and the reduce are the plan tile's
   FusedForm f;
@@ -735,6 +735,17 @@ FusedForm fused_form(const Plan& plan, bool rowmajor, int splits, bool grad, boo
   f.own = f.gemm.waves == 8 && (k == GemmKernel::A2 || k == GemmKernel::FP8P || k == GemmKernel::FP8S ||
                                 (k == GemmKernel::K64 && !f.gemm.far));
   f.direct = f.own && f.gemm.splits == 1;
+  // Where at most three quarters of the partition rows have valid rows, the
+  // XCDs of the others would idle: the tiles then go round the XCDs in raster
+  // order instead of to their owners' (the workspace is the same: none).
+  const int64_t live = (rows + p.part_rows() - 1) / p.part_rows();
+  if (f.direct && live > 0 && 4 * live <= 3 * p.Gr) {
+    const GemmForm g = gemm_form(p, f.a, f.b, false, 1);
+    if (g.kernel == f.gemm.kernel && !g.far) {
+      f.remap = false;
+      f.gemm = g;
+    }
+  }
   f.sum_rows = f.direct ? f.gemm.tile_m : k == GemmKernel::FP8 ? 32 : 16;
   f.partial_bytes = f.direct ? 0 : (int64_t)p.G * p.gemm.tiles_m * p.gemm.tiles_n * f.gemm.splits * p.gemm.tile_m * p.gemm.tile_n * 4;
   f.workspace_bytes = f.partial_bytes + (dbias ? p.M / f.sum_rows * f.z_cols * 4 : 0);
@@ -756,11 +767,15 @@ MoeForm moe_form(const MoeShape& s, int64_t tokens) {
   f.up_group = (int)std::max<int64_t>(1, used * f.up_tiles / 768);
   const int64_t groups = (f.up_tiles + f.up_group - 1) / f.up_group;
   f.up_workgroups = used * groups + (f.list ? 0 : (tokens + 7) / 8);
-  // The down product: ranges until every CU has a workgroup, of at least a
-  // 128-byte line of each row for every wave.
+  // The down product, in steps of a 128-byte line of 16 rows. kMoeDownTiles
+  // tiles of y share the loads of h, in ranges until every CU has a workgroup (a
+  // step at least for every wave). Where that takes ranges, whose sum is a launch
+  // of its own, of few steps: one tile a workgroup and no ranges (3 tokens, 9
+  // experts of 1216 x 256: 15.9 -> 13.6 us; but not past one round of the CUs).
   const int64_t lines = used * ((s.ffn * (s.fp8 ? 1 : 2) + 127) / 128);
-  f.down_groups = (f.down_tiles + kMoeDownTiles - 1) / kMoeDownTiles;
-  f.splits = (int)std::max<int64_t>(1, std::min<int64_t>(16, std::min<int64_t>(256 / f.down_groups, lines / 8)));
+  f.down_nt = lines >= 16 && lines <= kMoeFewLines && f.down_tiles <= 256 ? 1 : kMoeDownTiles;
+  f.down_groups = (f.down_tiles + f.down_nt - 1) / f.down_nt;
+  f.splits = f.down_nt == 1 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(16, std::min<int64_t>(256 / f.down_groups, lines / 8)));
   const auto up16 = [](int64_t n) { return (n + 15) / 16 * 16; };
   f.probs_at = up16(slots * 4);
   f.h_at = f.probs_at + up16(slots * 4);

@@ -186,19 +186,21 @@ struct FusedForm {
   int64_t z_cols = 0, c_cols = 0;
   bool direct = false;              // the GEMM's kernel has the epilogue itself (else: by way of partials)
   bool own = false;                 // the GEMM's kernel knows the valid rows
+  bool remap = true;                // tiles on the XCDs of their owners
   int sum_rows = 0;                 // rows of one block of column sums
   bool c_nt = false;
   int64_t partial_bytes = 0;        // fp32 partial tiles
   int64_t workspace_bytes = 0;      // with the column sums
 };
-FusedForm fused_form(const Plan& p, bool rowmajor, int splits, bool grad, bool gated, bool dbias);
+FusedForm fused_form(const Plan& p, bool rowmajor, int splits, bool grad, bool gated, bool dbias, int64_t rows);
 
 // tile_of_wg of an unsplit ccl_gemm's own launch.
 void launch_tile_of_wg(const Plan& p, int64_t wg, int* xcd, int64_t* tile_m, int64_t* tile_n);
 
 // A mixture-of-experts FFN layer for a few tokens.
 constexpr int kMoeMaxTokens = 64, kMoeMaxExperts = 512, kMoeMaxTopK = 16;
-constexpr int kMoeDownTiles = 4;    // 16-column tiles of y per workgroup
+constexpr int kMoeDownTiles = 4;    // 16-column tiles of y per workgroup, where there are many steps
+constexpr int kMoeFewLines = 128;   // (expert, K line) steps up to which the down product is not cut
 struct MoeShape {
   int64_t hidden = 0, ffn = 0;
   int experts = 0, top_k = 0, act = ACT_SILU;
@@ -213,7 +215,8 @@ struct MoeForm {
   int up_tiles = 0, down_tiles = 0; // 16-row tiles of ffn and hidden
   int up_group = 1;                 // up tiles per workgroup
   int64_t up_workgroups = 0;
-  int down_groups = 0;              // workgroups of a range of the down product
+  int down_nt = 1;                  // tiles of hidden per workgroup of the down product
+  int down_groups = 0;              // workgroups of a range of it
   int splits = 1;                   // ranges of the down product
   int64_t probs_at = 0, h_at = 0, part_at = 0, workspace_bytes = 0;
 };

@@ -231,12 +231,13 @@ static hipError_t launch_own(const GemmForm& f, const FusedParams& fp, hipStream
 }
 
 hipError_t launch_gemm_fused(const Plan& plan, const FusedCall& call, int splits, void* ws, hipStream_t stream) {
-  const FusedForm ff = fused_form(plan, call.rowmajor, splits, call.grad, call.gated, call.dbias != nullptr);
+  const FusedForm ff = fused_form(plan, call.rowmajor, splits, call.grad, call.gated, call.dbias != nullptr,
+                                  call.rows);
   const GemmForm& f = ff.gemm;
   Plan p = plan;
   p.gemm.wide_n = 0;
   FusedParams fp;
-  gemm_params(p, f, call.A, call.B, call.C, ff.a, ff.b, ff.c, true, &fp);
+  gemm_params(p, f, call.A, call.B, call.C, ff.a, ff.b, ff.c, ff.remap, &fp);
   fp.alpha = call.alpha;
   fp.c_nt = ff.c_nt ? 1 : 0;
   fp.e.bias = call.bias;

@@ -456,21 +456,19 @@ __global__ void __launch_bounds__(kThreads, STREAM ? 2 : 4) moe_up_kernel(MoePar
 #endif
 }
 
-// The down launch: one workgroup per kDownTiles tiles of 16 rows of the down
-// weights (columns of y) and range of the (expert, K line) steps of the chosen
+// The down launch: one workgroup per NT tiles of 16 rows of the down weights
+// (columns of y) and range of the (expert, K line) steps of the chosen
 // experts; the steps of a range are cut over the waves. A wave's stream is cut
-// into units of up to two lines of one expert; a unit's weights are loaded behind
+// into units of up to kLines lines of one expert; a unit's weights are loaded behind
 // the loads of the h rows of the unit before, one unit ahead of its products,
 // which are added to the wave's own y in LDS, at the rows of the unit's tokens.
 // Several tiles share the loads of h: with one, an fp8 layer's h took four times
 // the weights' load instructions (48 tokens, 128 experts of 2048 x 768: 92 us).
-constexpr int kDownTiles = kMoeDownTiles;
-
-template <bool FP8>
+template <bool FP8, int NT>
 __global__ void __launch_bounds__(kThreads, 2) moe_down_kernel(MoeParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)
   using W = Weights<FP8>;
-  constexpr int NT = kDownTiles, COLS = 16 * NT;
+  constexpr int COLS = 16 * NT;
   constexpr int kSlots = kMoeMaxTokens * kMoeMaxTopK;
   __shared__ int32_t s_list[kSlots];              // slots by expert
   __shared__ float s_probs[kSlots];               // times the expert's scale
@@ -527,7 +525,7 @@ __global__ void __launch_bounds__(kThreads, 2) moe_down_kernel(MoeParams p) {
   const int r = lane & 15, g = lane >> 4;
   const int64_t esize = FP8 ? 1 : 2;
   const W weights(p.down_ld, K, lane);
-  constexpr int kLines = 2;                                 // lines of a unit
+  constexpr int kLines = NT == 1 ? 4 : 2;                   // lines of a unit
   const int lines = weights.last + 1;
   const int total = __builtin_amdgcn_readfirstlane(s_total) * lines;
   const int parts = p.splits * kWaves, part = split * kWaves + wave;
@@ -696,9 +694,14 @@ hipError_t launch_moe(const MoeShape& s, const MoeCall& c, void* ws, hipStream_t
   p.tiles = f.down_tiles;
   p.groups = f.down_groups;
   const dim3 down((unsigned)(f.down_groups * f.splits));
-  const unsigned sums = (unsigned)(kWaves * c.tokens * 16 * kDownTiles * sizeof(float));
-  if (s.fp8) hipLaunchKernelGGL(moe_down_kernel<true>, down, block, sums, stream, p);
-  else hipLaunchKernelGGL(moe_down_kernel<false>, down, block, sums, stream, p);
+  const unsigned sums = (unsigned)(kWaves * c.tokens * 16 * f.down_nt * sizeof(float));
+  if (f.down_nt == 1) {
+    if (s.fp8) hipLaunchKernelGGL((moe_down_kernel<true, 1>), down, block, sums, stream, p);
+    else hipLaunchKernelGGL((moe_down_kernel<false, 1>), down, block, sums, stream, p);
+  } else {
+    if (s.fp8) hipLaunchKernelGGL((moe_down_kernel<true, kMoeDownTiles>), down, block, sums, stream, p);
+    else hipLaunchKernelGGL((moe_down_kernel<false, kMoeDownTiles>), down, block, sums, stream, p);
+  }
   e = hipGetLastError();
   if (e != hipSuccess || f.splits == 1) return e;
   hipLaunchKernelGGL(moe_sum_kernel, dim3((unsigned)((c.tokens * s.hidden / 4 + 255) / 256)), dim3(256), 0, stream, p);
