@@ -711,8 +711,7 @@ OperandAddr matrix_addressing(const Plan& p, int64_t cols, bool rowmajor) {
 }
 
 FusedForm fused_form(const Plan& plan, bool rowmajor, int splits, bool grad, bool gated, bool dbias, int64_t rows) {
-  Plan p = plan;
-  p.gemm.wide_n = 0;      // the workspace and the reduce are the plan tile's
+  const Plan& p = plan;
   FusedForm f;
   OperandAddr c;
   if (rowmajor) rowmajor_addressing(p, &f.a, &f.b, &c);
@@ -728,12 +727,13 @@ FusedForm fused_form(const Plan& plan, bool rowmajor, int splits, bool grad, boo
   f.c = matrix_addressing(p, f.c_cols, rowmajor);
   f.c_nt = f.gemm.c_nt;
   // The kernels whose accumulators are in 16x16 MFMA order under 8 waves take
-  // the epilogue themselves; split-K sums its ranges first, and the rest (plans
-  // whose K blocks are odd multiples of the K step, 4 waves, operands of 2 GiB
-  // and more) pass through one range's partials.
+  // the epilogue themselves; split-K sums its ranges first, and the rest (fp8
+  // plans whose K blocks are odd multiples of 64, 4 waves, operands of 2 GiB and
+  // more) pass through one range's partials.
   const GemmKernel k = f.gemm.kernel;
-  f.own = f.gemm.waves == 8 && (k == GemmKernel::A2 || k == GemmKernel::FP8P || k == GemmKernel::FP8S ||
-                                (k == GemmKernel::K64 && !f.gemm.far));
+  f.own = f.gemm.waves == 8 && !f.gemm.far &&
+          (k == GemmKernel::A2 || k == GemmKernel::K64 || k == GemmKernel::K32 || k == GemmKernel::FP8P ||
+           k == GemmKernel::FP8S);
   f.direct = f.own && f.gemm.splits == 1;
   // Where at most three quarters of the partition rows have valid rows, the
   // XCDs of the others would idle: the tiles then go round the XCDs in raster

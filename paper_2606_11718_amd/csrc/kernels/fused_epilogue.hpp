@@ -65,15 +65,17 @@ __device__ __forceinline__ int wide_col(int n) { return ((n & ~15) << 1) | (n & 
 
 // A bf16 matrix of ROWS x COLS in the two stage arrays, half of its rows in
 // each, 16-byte chunks XORed with the row so that the 16 rows of one access
-// fall in distinct banks.
+// fall in distinct banks: rows of 16 i chunks start in the same bank, of 8 i in
+// two, of 4 i in four.
 template <int ROWS, int COLS>
 struct StagedTile {
   static constexpr int HALF = ROWS / 2, PITCH = COLS * 2, CPR = COLS / 8;
-  static_assert(CPR == 8 || CPR % 16 == 0, "the swizzle is defined for rows of 8 or 16 i chunks");
+  static_assert(CPR % 4 == 0, "the swizzle is defined for rows of 4 i chunks");
+  static constexpr int swizzle(int h) { return CPR % 16 == 0 ? h & 15 : CPR % 8 == 0 ? (h >> 1) & 7 : (h >> 2) & 3; }
   char *lo, *hi;
   __device__ __forceinline__ char* chunk(int r, int c) const {
     const int h = r < HALF ? r : r - HALF;
-    return (r < HALF ? lo : hi) + h * PITCH + ((c ^ (CPR == 8 ? (h >> 1) & 7 : h & 15)) << 4);
+    return (r < HALF ? lo : hi) + h * PITCH + ((c ^ swizzle(h)) << 4);
   }
   // Four columns from column n (a multiple of 4) of row r.
   __device__ __forceinline__ uint2* at(int r, int n) const {
@@ -94,7 +96,9 @@ template <int ROWS, int COLS, int THREADS, typename Row>
 __device__ __forceinline__ void copy_in(const StagedTile<ROWS, COLS>& t, const uint16_t* m, int32_t ld, int tid, Row&& row) {
   constexpr int CPR = COLS / 8, N = ROWS * CPR / THREADS;
   static_assert(ROWS * CPR % THREADS == 0, "whole accesses");
-  constexpr int B = N < 8 ? N : 8;            // loads in flight per thread
+  // loads in flight per thread
+  constexpr int B = N <= 8 ? N : N % 8 == 0 ? 8 : N % 6 == 0 ? 6 : N % 5 == 0 ? 5 : 1;
+  static_assert(N % B == 0 && B > 1, "whole batches");
   for (int i = 0; i < N; i += B) {
     uint4 v[B];
 #pragma unroll
@@ -225,8 +229,15 @@ __device__ __forceinline__ void fused_forward(const FusedParams& p, f32x4 (&acc)
     staged_barrier();
     copy_out<BM, W, THREADS>(t, static_cast<uint16_t*>(p.C) + corner, p.c.ld, p.c_nt, tid, same);
   };
-  if (e.gated) finish(std::true_type{});
-  else finish(std::false_type{});
+  // A wave with an odd number of 16-column tiles splits a pair: those kernels are
+  // not launched on gated products.
+  if constexpr (TN % 2 == 0) {
+    if (e.gated) {
+      finish(std::true_type{});
+      return;
+    }
+  }
+  finish(std::false_type{});
 }
 
 template <int BM, int BN, int NW, int TM, int TN, int WM, int WN>

@@ -6,6 +6,15 @@ namespace ccl {
 
 namespace {
 
+template <int BM, int BN, int WGN>
+__global__ void __launch_bounds__(128 * WGN, WGN / 2) gemm_kernel(GemmParams p) {
+  // The host pass only needs the launch stub; the tile functions use
+  // device-only buffer-resource builtins.
+#if defined(__HIP_DEVICE_COMPILE__)
+  k32_tile<BM, BN, WGN>(p);
+#endif
+}
+
 template <int BM, int BN, bool RAGGED, bool BNT>
 __global__ void __launch_bounds__(512, 2) gemm_k64_kernel(GemmParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)

@@ -8,10 +8,19 @@ namespace ccl {
 namespace {
 
 // The GEMM's tiles with the epilogue behind the K loop.
-template <int BM, int BN, bool RAGGED, bool BNT, bool GRAD>
+// WGN: columns of the wave grid, 4 or 2. A gated product on 192 or 320 columns
+// takes 2, so that a wave's 16-column tiles are whole pairs of gate and up.
+template <int BM, int BN, bool RAGGED, bool BNT, bool GRAD, int WGN = 4>
 __global__ void __launch_bounds__(512, 2) fused_k64_kernel(FusedTileParams<GRAD> p) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  k64_tile<BM, BN, RAGGED, BNT, false>(p);
+  k64_tile<BM, BN, RAGGED, BNT, false, WGN>(p);
+#endif
+}
+
+template <int BM, int BN, bool GRAD>
+__global__ void __launch_bounds__(512, 2) fused_k32_kernel(FusedTileParams<GRAD> p) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  k32_tile<BM, BN, 4>(p);
 #endif
 }
 
@@ -200,6 +209,20 @@ static hipError_t launch_fused_reduce(const Plan& p, FusedParams fp, int md, int
   return hipGetLastError();
 }
 
+// A gated product on 128 x 192 or 128 x 320 tiles.
+template <int BM, int BN>
+static void launch_pairs(const GemmForm& f, const FusedParams& fp, hipStream_t stream) {
+  FusedTileParams<false> p;
+  static_cast<FusedParams&>(p) = fp;
+  const dim3 grid((unsigned)f.workgroups), block(512);
+#define CCL_PAIRS(R_, B_) hipLaunchKernelGGL((fused_k64_kernel<BM, BN, R_, B_, false, 2>), grid, block, 0, stream, p)
+  if (!f.ragged && f.stream_b) CCL_PAIRS(false, true);
+  else if (!f.ragged) CCL_PAIRS(false, false);
+  else if (f.stream_b) CCL_PAIRS(true, true);
+  else CCL_PAIRS(true, false);
+#undef CCL_PAIRS
+}
+
 // A form with kernels of its own here (FusedForm::own): with the epilogue, or,
 // with a workspace, the partials of the tiles that have valid rows.
 template <bool GRAD>
@@ -209,18 +232,27 @@ static hipError_t launch_own(const GemmForm& f, const FusedParams& fp, hipStream
   const dim3 grid((unsigned)f.workgroups), block(512);
   const auto tile = [&](int m, int n) { return f.tile_m == m && f.tile_n == n; };
 #define CCL_FUSED(...) hipLaunchKernelGGL((__VA_ARGS__), grid, block, 0, stream, p)
-#define CCL_FUSED_K64(BM_, BN_)                                                            \
-  do {                                                                                     \
-    if (!f.ragged && f.stream_b) CCL_FUSED(fused_k64_kernel<BM_, BN_, false, true, GRAD>); \
-    else if (!f.ragged) CCL_FUSED(fused_k64_kernel<BM_, BN_, false, false, GRAD>);         \
-    else if (f.stream_b) CCL_FUSED(fused_k64_kernel<BM_, BN_, true, true, GRAD>);          \
-    else CCL_FUSED(fused_k64_kernel<BM_, BN_, true, false, GRAD>);                         \
+#define CCL_FUSED_K64(BM_, BN_, WGN_)                                                            \
+  do {                                                                                           \
+    if (!f.ragged && f.stream_b) CCL_FUSED(fused_k64_kernel<BM_, BN_, false, true, GRAD, WGN_>); \
+    else if (!f.ragged) CCL_FUSED(fused_k64_kernel<BM_, BN_, false, false, GRAD, WGN_>);         \
+    else if (f.stream_b) CCL_FUSED(fused_k64_kernel<BM_, BN_, true, true, GRAD, WGN_>);          \
+    else CCL_FUSED(fused_k64_kernel<BM_, BN_, true, false, GRAD, WGN_>);                         \
   } while (0)
+  const bool pairs = !GRAD && fp.e.gated;
   if (f.kernel == GemmKernel::A2) CCL_FUSED(fused_a2_kernel<GRAD>);
   else if (f.kernel == GemmKernel::FP8P) CCL_FUSED(fused_fp8p_kernel<GRAD>);
-  else if (f.kernel == GemmKernel::K64 && tile(256, 128)) CCL_FUSED_K64(256, 128);
-  else if (f.kernel == GemmKernel::K64 && tile(128, 256)) CCL_FUSED_K64(128, 256);
-  else if (f.kernel == GemmKernel::K64 && tile(128, 128)) CCL_FUSED_K64(128, 128);
+  else if (f.kernel == GemmKernel::K64 && tile(256, 128)) CCL_FUSED_K64(256, 128, 4);
+  else if (f.kernel == GemmKernel::K64 && tile(128, 256)) CCL_FUSED_K64(128, 256, 4);
+  else if (f.kernel == GemmKernel::K64 && tile(128, 128)) CCL_FUSED_K64(128, 128, 4);
+  else if (f.kernel == GemmKernel::K64 && tile(128, 192) && !pairs) CCL_FUSED_K64(128, 192, 4);
+  else if (f.kernel == GemmKernel::K64 && tile(128, 320) && !pairs) CCL_FUSED_K64(128, 320, 4);
+  else if (f.kernel == GemmKernel::K64 && tile(128, 192)) launch_pairs<128, 192>(f, fp, stream);
+  else if (f.kernel == GemmKernel::K64 && tile(128, 320)) launch_pairs<128, 320>(f, fp, stream);
+  else if (f.kernel == GemmKernel::K32 && tile(256, 256)) CCL_FUSED(fused_k32_kernel<256, 256, GRAD>);
+  else if (f.kernel == GemmKernel::K32 && tile(256, 128)) CCL_FUSED(fused_k32_kernel<256, 128, GRAD>);
+  else if (f.kernel == GemmKernel::K32 && tile(128, 256)) CCL_FUSED(fused_k32_kernel<128, 256, GRAD>);
+  else if (f.kernel == GemmKernel::K32 && tile(128, 128)) CCL_FUSED(fused_k32_kernel<128, 128, GRAD>);
   else if (f.kernel == GemmKernel::FP8S && tile(256, 128)) CCL_FUSED(fused_fp8s_kernel<256, 128, 4, 2, GRAD>);
   else if (f.kernel == GemmKernel::FP8S && tile(128, 256)) CCL_FUSED(fused_fp8s_kernel<128, 256, 2, 4, GRAD>);
   else if (f.kernel == GemmKernel::FP8S && tile(128, 128)) CCL_FUSED(fused_fp8s_kernel<128, 128, 2, 4, GRAD>);

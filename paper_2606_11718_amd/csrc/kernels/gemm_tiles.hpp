@@ -706,11 +706,9 @@ __device__ __forceinline__ void record_timeline(uint64_t* o, const uint64_t (&rt
   }
 }
 
-template <int BM, int BN, int WGN>
-__global__ void __launch_bounds__(128 * WGN, WGN / 2) gemm_kernel(GemmParams p) {
-  // The host pass only needs the launch stub; the body uses device-only
-  // buffer-resource builtins.
 #if defined(__HIP_DEVICE_COMPILE__)
+template <int BM, int BN, int WGN, typename P>
+__device__ __forceinline__ void k32_tile(const P& p) {
   using T = Tile<BM, BN, WGN>;
   constexpr int NS = kStagesBf16;
   __shared__ __attribute__((aligned(1024))) char smA[NS][T::A_BYTES];
@@ -728,6 +726,8 @@ __global__ void __launch_bounds__(128 * WGN, WGN / 2) gemm_kernel(GemmParams p) 
   }
   int32_t pr, pc, ti, tj, split;
   if (!tile_of_block(p, &pr, &pc, &ti, &tj, &split)) return;
+  if constexpr (kFused<P>)
+    if (dead_tile<BM, BN, T::THREADS, P::kGrad>(p, pr, pc, ti, tj)) return;
   // K range of this workgroup: steps [k0, k0 + ksteps) (all of K without split-K)
   const int32_t k0 = __builtin_amdgcn_readfirstlane(split * p.ksteps_per_split);
   const int32_t ksteps = __builtin_amdgcn_readfirstlane(min(p.ksteps, k0 + p.ksteps_per_split) - k0);
@@ -997,12 +997,16 @@ __global__ void __launch_bounds__(128 * WGN, WGN / 2) gemm_kernel(GemmParams p) 
     tl_clk[1] = __builtin_amdgcn_s_memtime();
   }
   constexpr int kBuf = NS * T::A_BYTES < NS * T::B_BYTES ? NS * T::A_BYTES : NS * T::B_BYTES;
-  epilogue16<BM, BN, T::NW, T::TM, T::TN, T::WM, T::WN, kBuf, 0>(p, acc, &smA[0][0], &smB[0][0], pr, pc,
+  if constexpr (kFused<P>) {
+    if (p.ws) store_tile<BM, BN, 16, T::TM, T::TN, T::WM, T::WN>(p, acc, pr, pc, ti, tj, split, wm, wn, lane);
+    else fused_epilogue<BM, BN, T::NW, T::TM, T::TN, T::WM, T::WN>(p, acc, &smA[0][0], &smB[0][0], pr, pc, ti, tj, wm, wn, tid);
+  } else
+    epilogue16<BM, BN, T::NW, T::TM, T::TN, T::WM, T::WN, kBuf, 0>(p, acc, &smA[0][0], &smB[0][0], pr, pc,
                                                                     ti, tj, split, wm, wn, wave, lane);
   if (tl_on) record_timeline(p.timeline + ((int64_t)blockIdx.x * T::NW + wave) * kTimelineWords,
                              tl_rt, tl_clk, lane);
-#endif
 }
+#endif
 
 // ---------------------------------------------------------------------------
 // bf16 with 64-K stages, for the output tiles below 256x256 (8 waves). A
@@ -1037,12 +1041,12 @@ constexpr int kBK64 = 64;        // K extent of one stage of gemm_k64_kernel
 
 __device__ __forceinline__ int swz_a64(int row) { return (row >> 1) & 7; }
 
-template <int BM, int BN>
+template <int BM, int BN, int WGN_ = 4>
 struct Tile64 {
-  static constexpr int WGN = 4;
+  static constexpr int WGN = WGN_;
   static constexpr int NW = 8;                         // waves per workgroup
   static constexpr int THREADS = 64 * NW;
-  static constexpr int WM = BM / 2, WN = BN / WGN;     // wave tile
+  static constexpr int WM = BM * WGN / NW, WN = BN / WGN;   // wave tile
   static constexpr int TM = WM / 16, TN = WN / 16;     // MFMA tiles per wave
   static constexpr int A_BYTES = BM * kBK64 * 2;       // one stage
   static constexpr int B_BYTES = kBK64 * BN * 2;
@@ -1070,10 +1074,10 @@ struct Tile64 {
 };
 
 #if defined(__HIP_DEVICE_COMPILE__)
-template <int BM, int BN, bool RAGGED, bool BNT, bool FAR, typename P>
+template <int BM, int BN, bool RAGGED, bool BNT, bool FAR, int WGN = 4, typename P>
 __device__ __forceinline__ void k64_tile(const P& p) {
   static_assert(!(RAGGED && FAR), "a ragged stage's jump to the next K block is a 31-bit offset");
-  using T = Tile64<BM, BN>;
+  using T = Tile64<BM, BN, WGN>;
   constexpr int NS = T::NS;
   __shared__ __attribute__((aligned(1024))) char smA[NS][T::A_BYTES];
   __shared__ __attribute__((aligned(1024))) char smB[NS][T::B_BYTES];

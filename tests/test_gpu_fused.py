@@ -164,6 +164,38 @@ def test_every_tile(monkeypatch, tile, waves, fp8, K):
                  alpha=0.05 if fp8 else 1.0, layout=ccl.CCL_LAYOUT_ROWMAJOR)
 
 
+# plans whose launch takes 128-row tiles of 192 or 320 columns, whole and odd K
+# blocks (K / 8 of 64 i and of 32)
+WIDE_TILES = [((256, 1920, 512, 1, 1, 4096), 192), ((256, 1920, 512, 1, 1, 4096), 320),
+              ((256, 15360, 768, 8, 1, 4096), 192), ((256, 15360, 768, 8, 1, 4096), 320)]
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("shape,cols", WIDE_TILES)
+def test_wide_tiles(monkeypatch, shape, cols, grad, gated):
+    monkeypatch.setenv("CCL_GEMM_WIDE", str(cols))
+    plan = ccl.ccl_plan(*shape)
+    assert ccl.ccl_debug_launch(plan).tile_cols == cols
+    if grad:
+        _backward(shape, ccl.CCL_ACT_SILU, gated, rows=200, spoil=True)
+    else:
+        _forward(shape, ccl.CCL_ACT_SILU, gated, bias="f32", residual=True, rows=200, spoil=True)
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("tile", ["256x256", "256x128", "128x256", "128x128"])
+def test_odd_k_blocks(monkeypatch, tile, grad, gated):
+    """K blocks that are odd multiples of 32: the 32-K kernels and the ragged 64-K ones."""
+    monkeypatch.setenv("CCL_GEMM_TILE", tile)
+    shape = (512, 2048, 768, 8, 1, 4096)          # K / 8 = 96
+    if grad:
+        _backward(shape, ccl.CCL_ACT_GELU, gated, rows=300)
+    else:
+        _forward(shape, ccl.CCL_ACT_GELU, gated, bias="bf16", residual=True, rows=300)
+
+
 @pytest.mark.parametrize("keep", [False, True])
 @pytest.mark.parametrize("residual", [False, True])
 @pytest.mark.parametrize("bias", [None, "f32", "bf16"])
