@@ -6,7 +6,9 @@
 //
 // s(x) = 1 / (1 + 2^(-x log2 e)) is one v_exp_f32 and one v_rcp_f32 (1 ulp
 // each), so an activation is within a few ulp of fp32 wherever it is not
-// tiny; a large negative x gives 1 / inf = 0. NaN stays NaN.
+// tiny; a large negative x gives 1 / inf = 0. NaN stays NaN. s is formed at z
+// clamped to +-100, where it is 0 or 1 to the last bit: beyond 2^64, z^2 is
+// infinite and SiLU's zero coefficient of it would make a NaN.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -37,8 +39,10 @@ __device__ __forceinline__ ActCoef act_coef(int act) {
 template <int CLASS>
 __device__ __forceinline__ float act_value(ActCoef k, float z) {
   if constexpr (CLASS == ACT_CLASS_RELU) return z < 0.f ? 0.f : z;
-  if constexpr (CLASS == ACT_CLASS_SMOOTH)
-    return z * logistic2(z * __builtin_fmaf(-kLog2e * k.k1, z * z, -kLog2e * k.k0));
+  if constexpr (CLASS == ACT_CLASS_SMOOTH) {
+    const float c = __builtin_amdgcn_fmed3f(z, -100.f, 100.f);
+    return z * logistic2(c * __builtin_fmaf(-kLog2e * k.k1, c * c, -kLog2e * k.k0));
+  }
   return z;
 }
 

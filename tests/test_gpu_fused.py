@@ -203,6 +203,13 @@ def test_parts_of_the_epilogue(bias, residual, keep):
     _forward(EXPERT, ccl.CCL_ACT_GELU, False, bias=bias, residual=residual, keep=keep, alpha=-0.5, beta=0.25)
 
 
+@pytest.mark.parametrize("alpha", [1e20, 1e30])
+@pytest.mark.parametrize("kind", ALL_ACTS)
+def test_pre_activations_whose_squares_overflow(kind, alpha):
+    """Finite in, finite out: z or 0."""
+    _forward(SMALL, kind, alpha=alpha)
+
+
 def test_residual_in_place():
     _forward(EXPERT, ccl.CCL_ACT_NONE, residual=True, keep=False, in_place=True)
     _forward(EXPERT, ccl.CCL_ACT_SILU, gated=True, residual=True, keep=False, in_place=True)
@@ -350,3 +357,39 @@ def test_another_stream():
     with torch.cuda.stream(s):
         _forward(EXPERT, ccl.CCL_ACT_GELU, True, residual=True)
         _backward(EXPERT, ccl.CCL_ACT_GELU, True)
+
+
+def test_graph_replays():
+    """A captured forward and backward call, replayed with eager work between:
+    the eager bits each time."""
+    M, N, K = 256, 512, 256
+    plan = ccl.ccl_plan(M, N, K, 4, 2, 4096)
+    rm = ccl.CCL_LAYOUT_ROWMAJOR
+    A = to_dev(W.draw_array(21, M, K, "normal", 1.0))
+    B = to_dev(W.draw_array(22, K, N, "normal", 0.06))
+    C, Z, dZ, db = dev_full(M * N // 2), dev_full(M * N), dev_full(M * 2 * N), torch.empty(2 * N, device="cuda")
+    Zin = to_dev(W.draw_array(23, M, 2 * N, "normal", 2.0))
+    need = max(ccl.ccl_gemm_fused_workspace(plan, layout=rm)[1],
+               ccl.ccl_gemm_fused_grad_workspace(plan, gated=True, dbias=True, layout=rm), 16)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+
+    def step():
+        ccl.ccl_gemm_fused(plan, A, B, C, activation=ccl.CCL_ACT_SILU, gated=True, preact=Z, rows=200, layout=rm,
+                           workspace=ws, workspace_bytes=need)
+        ccl.ccl_gemm_fused_grad(plan, A, B, Zin, dZ, activation=ccl.CCL_ACT_SILU, gated=True, dbias=db, rows=200,
+                                layout=rm, workspace=ws, workspace_bytes=need)
+
+    outs = (C, Z, dZ, db)
+    step()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outs]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        for t in outs:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+        (A.float() + 1).sum().item()
