@@ -793,12 +793,18 @@ MoeForm moe_form(const MoeShape& s, int64_t tokens) {
 //   (21 tiles of 12 and 32 steps 9.8 and 15.5; 136 tiles 0.4 a step).
 //   128x128 with two stages: two to a CU, 7 + 1.0 a step, or 0.6 alone (1248
 //   tiles of 24 steps 84, with four stages 90; 512 of 32 38).
+//   64x64 (symmetric), two to a CU: 5 + 0.16 a step, from one round of the CUs on
+//   0.41 (78 tiles of 12 steps 6.0, with 128x128 10.0; 288 of 16 11.3, with
+//   128x128 12.8).
+//   64x128 (the other), one to a CU: 5.6 + 0.22 a step (128 tiles of 16 steps 8.7,
+//   with 128x128 11.2).
 // The tiles past whole rounds may be cut into K ranges, of 4 steps at least,
-// which a further launch adds up (5, and reading the partials).
+// which a further launch adds up (5, and reading the partials); not of 64x128.
 static double ortho_split(int64_t m, int64_t n, int64_t steps, int64_t batch, bool sym, int tile, OrthoSplit* out) {
   constexpr int64_t kCus = 256;
   const auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-  const int64_t tm = up(m, tile), tn = up(n, tile);
+  const int64_t tile_n = tile == 64 && !sym ? 128 : tile;
+  const int64_t tm = up(m, tile), tn = up(n, tile_n);
   const int64_t total = (sym ? tm * (tm + 1) / 2 : tm * tn) * batch;
   out->tile = tile;
   out->paired = tile == 128 && total > kCus;
@@ -806,18 +812,20 @@ static double ortho_split(int64_t m, int64_t n, int64_t steps, int64_t batch, bo
   out->splits = 1;
   out->ksplit = (int32_t)steps;
   out->part_elems = 0;
-  const int64_t slots = out->paired ? 2 * kCus : kCus;
-  const double fixed = tile == 256 ? 16.0 : out->paired ? 7.0 : 6.4;
-  const double step = tile == 256 ? 1.5 : out->paired ? 1.0 : total > 64 ? 0.4 : 0.3;
+  const int64_t slots = out->paired || (tile == 64 && sym) ? 2 * kCus : kCus;
+  const double fixed = tile == 256 ? 16.0 : out->paired ? 7.0 : tile == 128 ? 6.4 : sym ? 5.0 : 5.6;
+  const double step = tile == 256 ? 1.5 : out->paired ? 1.0 : tile == 128 ? (total > 64 ? 0.4 : 0.3)
+                      : !sym ? 0.22 : total > kCus ? 0.41 : 0.16;
   const int64_t whole = total / slots * slots, rest = total - whole;
   const double rounds = (double)(whole / slots) * (fixed + step * (double)steps);
   if (rest == 0) return rounds;
   const double last = out->paired && rest <= kCus ? 0.6 : step;
   double best = rounds + fixed + last * (double)steps;
-  const int64_t s = std::min<int64_t>(std::min<int64_t>(slots / rest, steps / 4), 16);
+  const int64_t s = tile_n == tile ? std::min<int64_t>(std::min<int64_t>(slots / rest, steps / 4), 16) : 1;
   if (s < 2) return best;
   const int64_t per = up(steps, s), ranges = up(steps, per), elems = rest * ranges * tile * tile;
-  const double split = rounds + fixed + step * (double)per + 5.0 + (double)elems * 4 / 4e6;
+  const double split_step = tile == 64 && rest * ranges > kCus ? 0.41 : step;
+  const double split = rounds + fixed + split_step * (double)per + 5.0 + (double)elems * 4 / 4e6;
   if (split < best) {
     best = split;
     out->whole = (int32_t)whole;
@@ -836,9 +844,16 @@ OrthoForm ortho_form(const OrthoShape& s) {
   f.chunks = (int32_t)std::min<int64_t>(1024, std::max<int64_t>(1, s.rows * s.cols / 16384));
   // Each product on the tiles that take least.
   const auto best = [&](int64_t m, int64_t n, int64_t k, bool sym, OrthoSplit* out) {
-    const double t = ortho_split(m, n, k / 64, s.batch, sym, 128, out);
-    OrthoSplit large;
-    if (f.pp >= 256 && ortho_split(m, n, k / 64, s.batch, sym, 256, &large) < t) *out = large;
+    double t = ortho_split(m, n, k / 64, s.batch, sym, 128, out);
+    for (const int tile : {256, 64}) {
+      OrthoSplit other;
+      if (tile == 256 && f.pp < 256) continue;
+      const double o = ortho_split(m, n, k / 64, s.batch, sym, tile, &other);
+      if (o < t) {
+        t = o;
+        *out = other;
+      }
+    }
   };
   best(f.pp, f.pp, f.qp, true, &f.gram);
   best(f.pp, f.pp, f.pp, true, &f.square);

@@ -230,7 +230,7 @@ struct OrthoShape {
 // One product's tiles over the batch: the first `whole` by a workgroup each, the
 // rest cut into `splits` K ranges of ksplit steps of 64.
 struct OrthoSplit {
-  int tile = 0;                     // 128 or 256 squared
+  int tile = 0;                     // 64 (not symmetric: 64 x 128), 128 or 256 squared
   bool paired = false;              // 128: two workgroups of two LDS stages share a CU
   int32_t whole = 0, splits = 1, ksplit = 0;
   int64_t part_elems = 0;           // fp32 values of the ranges' partial tiles

@@ -58,6 +58,7 @@ struct NsTile {
   static constexpr int U_BYTES = BM * 128, V_BYTES = BN * 128;   // a stage of 64 K
   static constexpr int NU = U_BYTES / (1024 * NW), NV = V_BYTES / (1024 * NW), NL = NU + NV;
   static constexpr int CPR_V = BN / 8, RPI_V = 64 / CPR_V;       // 16-byte chunks and rows of a load (not NT)
+  static_assert(BM * BN / 8 % THREADS == 0, "whole copies");
   static constexpr int NS = NS_;
   // With two stage buffers a step's loads go out behind its barrier, into the
   // buffer it has just read; otherwise NS - 1 stages ahead of it.
@@ -179,27 +180,39 @@ __device__ __forceinline__ void ns_copy_out_trans(const StagedTile<BM, BN>& t, u
   }
 }
 
-// D's ROWS x COLS from row r0, column c0 into the staged tile. (Accumulators
-// that started from D instead, loaded in their own order with the first stages,
-// took 1 to 5 % longer: 32-byte pieces.)
+// D's ROWS x COLS from row r0, column c0, through registers into the staged
+// tile. (Accumulators that started from D instead, loaded in their own order with
+// the first stages, took 1 to 5 % longer: 32-byte pieces.)
 template <int ROWS, int COLS, int THREADS>
-__device__ __forceinline__ void ns_copy_in(const NsParams& p, const StagedTile<ROWS, COLS>& t, int mat, int r0, int c0,
-                                           int tid) {
-  constexpr int CPR = COLS / 8, N = ROWS * CPR / THREADS, B = N < 8 ? N : 8;
-  const uint16_t* d = p.D + mat * p.out_stride;
-  for (int i = 0; i < N; i += B) {
-    uint4 v[B];
+struct NsAddend {
+  static constexpr int CPR = COLS / 8, N = ROWS * CPR / THREADS, B = N < 8 ? N : 8;
+  uint4 v[B];
+  __device__ __forceinline__ void load(const NsParams& p, int mat, int r0, int c0, int i, int tid) {
+    const uint16_t* d = p.D + mat * p.out_stride;
 #pragma unroll
     for (int j = 0; j < B; ++j) {
       const int at = (i + j) * THREADS + tid, r = r0 + at / CPR, c = c0 + at % CPR * 8;
       v[j] = make_uint4(0, 0, 0, 0);
       if (r < p.M && c < p.N) v[j] = *reinterpret_cast<const uint4*>(d + (int64_t)r * p.ld_out + c);
     }
+  }
+  __device__ __forceinline__ void put(const StagedTile<ROWS, COLS>& t, int i, int tid) const {
 #pragma unroll
     for (int j = 0; j < B; ++j) {
       const int at = (i + j) * THREADS + tid;
       *reinterpret_cast<uint4*>(t.chunk(at / CPR, at % CPR)) = v[j];
     }
+  }
+};
+
+template <int ROWS, int COLS, int THREADS>
+__device__ __forceinline__ void ns_copy_in(const NsParams& p, const StagedTile<ROWS, COLS>& t, int mat, int r0, int c0,
+                                           int tid) {
+  using A = NsAddend<ROWS, COLS, THREADS>;
+  for (int i = 0; i < A::N; i += A::B) {
+    A a;
+    a.load(p, mat, r0, c0, i, tid);
+    a.put(t, i, tid);
   }
 }
 
@@ -327,6 +340,13 @@ __global__ void __launch_bounds__(512, NS * (BM + BN) * 128 <= 80 * 1024 ? 4 : 2
     }
   };
 
+  // Of the smaller tiles D is loaded ahead of the stages, so that the epilogue
+  // does not wait for it.
+  using Addend = NsAddend<BM, BN, T::THREADS>;
+  constexpr bool kEarly = Addend::N == Addend::B && Addend::N <= 4;
+  Addend early;
+  if (kEarly && p.D && part < 0) early.load(p, mat, ti * BM, tj * BN, 0, tid);
+
   f32x4 acc[T::TM][T::TN];
 #pragma unroll
   for (int i = 0; i < T::TM; ++i)
@@ -417,7 +437,8 @@ __global__ void __launch_bounds__(512, NS * (BM + BN) * 128 <= 80 * 1024 ? 4 : 2
   asm volatile("" ::: "memory");
   const StagedTile<BM, BN> t{smU[0], smV[0]};
   if (p.D) {
-    ns_copy_in<BM, BN, T::THREADS>(p, t, mat, ti * BM, tj * BN, tid);
+    if constexpr (kEarly) early.put(t, 0, tid);
+    else ns_copy_in<BM, BN, T::THREADS>(p, t, mat, ti * BM, tj * BN, tid);
     staged_barrier();
   }
 #pragma unroll
@@ -431,35 +452,36 @@ __global__ void __launch_bounds__(512, NS * (BM + BN) * 128 <= 80 * 1024 ? 4 : 2
 }
 
 // The split tiles: ranges summed in order. A workgroup takes 32 rows of a tile
-// (two rows of 16x16 tiles of one row of waves).
+// (two rows of 16x16 tiles of one row of waves), or a whole one of 64.
 template <int B, bool SYM>
 __global__ void __launch_bounds__(512) ns_split_sum_kernel(NsParams p) {
   using T = NsTile<B, B, true, 2>;
-  constexpr int PARTS = B / 32, FRAGS = 2 * B / 16;          // 16x16 tiles of a part
-  __shared__ __attribute__((aligned(16))) char sm[32 * B * 2];
-  const int32_t tile = blockIdx.x / PARTS, row0 = blockIdx.x % PARTS * 32;
+  constexpr int ROWS = B == 64 ? 64 : 32, PARTS = B / ROWS;
+  constexpr int R16 = ROWS / 16, FRAGS = R16 * B / 16;       // 16x16 tiles of a column, of a part
+  __shared__ __attribute__((aligned(16))) char sm[ROWS * B * 2];
+  const int32_t tile = blockIdx.x / PARTS, row0 = blockIdx.x % PARTS * ROWS;
   const int32_t id = p.whole + tile, mat = id / p.tiles;
   int32_t ti, tj;
   ns_tile<SYM>(p, id - mat * p.tiles, &ti, &tj);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const StagedTile<32, B> t{sm, sm + 32 * B};
+  const StagedTile<ROWS, B> t{sm, sm + ROWS * B};
   if (p.D) {
-    ns_copy_in<32, B, 512>(p, t, mat, ti * B + row0, tj * B, tid);
+    ns_copy_in<ROWS, B, 512>(p, t, mat, ti * B + row0, tj * B, tid);
     __syncthreads();
   }
   const f32x4* from = reinterpret_cast<const f32x4*>(p.part + (int64_t)tile * p.splits * (B * B));
 #pragma unroll
   for (int i = 0; i < FRAGS / 8; ++i) {
-    const int f = wave * (FRAGS / 8) + i, sub = f % 2, col = f / 2;          // 16-row half, 16-column tile
-    const int w = row0 / T::WM * T::WGN + col / T::TN;                       // the wave that computed it
-    const int at = frag_index<T::TM, T::TN, 1>(w, row0 % T::WM / 16 + sub, col % T::TN, 0, lane);
+    const int f = wave * (FRAGS / 8) + i, row = f % R16 * 16, col = f / R16;
+    const int w = (row0 + row) / T::WM * T::WGN + col / T::TN;               // the wave that computed it
+    const int at = frag_index<T::TM, T::TN, 1>(w, (row0 + row) % T::WM / 16, col % T::TN, 0, lane);
     f32x4 v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
     for (int r = 0; r < p.splits; ++r) v += from[(int64_t)r * (B * B / 4) + at];
-    ns_combine(p, t.at(16 * sub + (lane & 15), 16 * col + 4 * (lane >> 4)), v);
+    ns_combine(p, t.at(row + (lane & 15), 16 * col + 4 * (lane >> 4)), v);
   }
   __syncthreads();
-  ns_store<32, B, SYM>(p, t, mat, ti * B + row0, tj * B, ti != tj, tid);
+  ns_store<ROWS, B, SYM>(p, t, mat, ti * B + row0, tj * B, ti != tj, tid);
 }
 
 // ---- the norm and the first X ----
@@ -587,9 +609,9 @@ __global__ void __launch_bounds__(256) ns_copy_kernel(const uint16_t* X, int64_t
 // One product of the batch.
 template <bool SYM>
 hipError_t ns_launch(NsParams p, int64_t batch, const OrthoSplit& f, hipStream_t stream) {
-  const int b = f.tile;
+  const int b = f.tile, bn = b == 64 && !SYM ? 128 : b;
   p.tiles_m = (p.M + b - 1) / b;
-  p.tiles_n = (p.N + b - 1) / b;
+  p.tiles_n = (p.N + bn - 1) / bn;
   p.tiles = SYM ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
   p.total = (int32_t)(p.tiles * batch);
   p.group = p.tiles_m < 8 ? p.tiles_m : 8;
@@ -600,12 +622,14 @@ hipError_t ns_launch(NsParams p, int64_t batch, const OrthoSplit& f, hipStream_t
   const int32_t rest = p.total - p.whole;
   p.split_xcd = (rest * f.splits + 7) / 8;
   const dim3 grid((unsigned)(8 * (p.whole_xcd + p.split_xcd))), block(512);
-  if (b == 128 && f.paired) hipLaunchKernelGGL((ns_product_kernel<128, 128, SYM, 2>), grid, block, 0, stream, p);
+  if (b == 64) hipLaunchKernelGGL((ns_product_kernel<64, SYM ? 64 : 128, SYM, 4>), grid, block, 0, stream, p);
+  else if (b == 128 && f.paired) hipLaunchKernelGGL((ns_product_kernel<128, 128, SYM, 2>), grid, block, 0, stream, p);
   else if (b == 128) hipLaunchKernelGGL((ns_product_kernel<128, 128, SYM, 4>), grid, block, 0, stream, p);
   else hipLaunchKernelGGL((ns_product_kernel<256, 256, SYM, 2>), grid, block, 0, stream, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || rest == 0) return e;
-  if (b == 128) hipLaunchKernelGGL((ns_split_sum_kernel<128, SYM>), dim3((unsigned)(rest * 4)), block, 0, stream, p);
+  if (b == 64) hipLaunchKernelGGL((ns_split_sum_kernel<64, true>), dim3((unsigned)rest), block, 0, stream, p);
+  else if (b == 128) hipLaunchKernelGGL((ns_split_sum_kernel<128, SYM>), dim3((unsigned)(rest * 4)), block, 0, stream, p);
   else hipLaunchKernelGGL((ns_split_sum_kernel<256, SYM>), dim3((unsigned)(rest * 8)), block, 0, stream, p);
   return hipGetLastError();
 }
