@@ -50,6 +50,8 @@ struct NsParams {
   float alpha, beta;
 };
 
+// 8 waves, 2 x 4. (64x64 in 2 x 2 waves reads a third less of LDS a step and took
+// 6 to 9 % longer.)
 template <int BM, int BN, bool NT, int NS_>
 struct NsTile {
   static constexpr int WGN = 4, NW = 8, THREADS = 512;
@@ -340,10 +342,11 @@ __global__ void __launch_bounds__(512, NS * (BM + BN) * 128 <= 80 * 1024 ? 4 : 2
     }
   };
 
-  // Of the smaller tiles D is loaded ahead of the stages, so that the epilogue
-  // does not wait for it.
+  // D of the 64-row tiles is loaded ahead of the stages, so that the epilogue
+  // does not wait for it (17 launches of 128x128: 68.0 -> 67.5 us; of the 128x128
+  // tiles, whose registers it takes, 3 of 1000x2000 242 -> 247).
   using Addend = NsAddend<BM, BN, T::THREADS>;
-  constexpr bool kEarly = Addend::N == Addend::B && Addend::N <= 4;
+  constexpr bool kEarly = Addend::N == Addend::B && Addend::N <= 2;
   Addend early;
   if (kEarly && p.D && part < 0) early.load(p, mat, ti * BM, tj * BN, 0, tid);
 
