@@ -735,15 +735,19 @@ FusedForm fused_form(const Plan& plan, bool rowmajor, int splits, bool grad, boo
           (k == GemmKernel::A2 || k == GemmKernel::K64 || k == GemmKernel::K32 || k == GemmKernel::FP8P ||
            k == GemmKernel::FP8S);
   f.direct = f.own && f.gemm.splits == 1;
-  // Where at most three quarters of the partition rows have valid rows, the
-  // XCDs of the others would idle: the tiles then go round the XCDs in raster
-  // order instead of to their owners' (the workspace is the same: none).
-  const int64_t live = (rows + p.part_rows() - 1) / p.part_rows();
-  if (f.direct && live > 0 && 4 * live <= 3 * p.Gr) {
-    const GemmForm g = gemm_form(p, f.a, f.b, false, 1);
-    if (g.kernel == f.gemm.kernel && !g.far) {
+  // Where the valid rows leave XCDs idle, their tiles go round the XCDs instead
+  // of to their owners': if that takes fewer rounds of the CUs (us: 4350 of 7168
+  // rows in 8 partition rows, 25088x2048 702 -> 516; 845 of them, 5632x1280 27 -> 23).
+  const int64_t live_m = (rows + f.gemm.tile_m - 1) / f.gemm.tile_m;
+  if (f.direct && live_m > 0) {
+    const TileMap& m = f.gemm.map;
+    const int64_t cols = (int64_t)m.tiles_n * p.Gc, round = 32;
+    const int64_t owned = std::min<int64_t>(live_m, m.tiles_m) * m.tiles_n;
+    const auto rounds = [&](int64_t tiles) { return (tiles + round - 1) / round; };
+    if (rounds((live_m * cols + 7) / 8) < rounds((owned + m.xcd_per_chip - 1) / m.xcd_per_chip)) {
       f.remap = false;
-      f.gemm = g;
+      f.live = make_live_map(m, (int32_t)p.Gr, (int32_t)live_m);
+      f.gemm.workgroups = 8 * (int64_t)(f.live.live_per_xcd + f.live.rest_per_xcd);
     }
   }
   f.sum_rows = f.direct ? f.gemm.tile_m : k == GemmKernel::FP8 ? 32 : 16;

@@ -187,6 +187,7 @@ struct FusedForm {
   bool direct = false;              // the GEMM's kernel has the epilogue itself (else: by way of partials)
   bool own = false;                 // the GEMM's kernel knows the valid rows
   bool remap = true;                // tiles on the XCDs of their owners
+  LiveMap live{};                   // else: the tiles with valid rows over all XCDs
   int sum_rows = 0;                 // rows of one block of column sums
   bool c_nt = false;
   int64_t partial_bytes = 0;        // fp32 partial tiles

@@ -102,4 +102,61 @@ CCL_HD bool map_tile(const TileMap& m, int64_t wg, int32_t* pr, int32_t* pc, int
   return map_tile(m, wg, pr, pc, ti, tj, &split);
 }
 
+// The map of a launch of which only the first live_m tile rows of C (over all
+// partitions) are to be computed: those tiles first, each XCD a contiguous range
+// of a grouped raster over the whole width, whoever owns them; then the rest.
+struct LiveMap {
+  int32_t live_m, rows_m, cols_n;   // tile rows with work, all tile rows, tile columns of C
+  int32_t live_per_xcd, rest_per_xcd;
+  int32_t group_m;
+  FastDiv by_group, by_height, by_last, by_cols, by_tiles_m, by_tiles_n;
+  int32_t tiles_m, tiles_n;         // of a partition
+};
+
+inline LiveMap make_live_map(const TileMap& m, int32_t grid_r, int32_t live_m) {
+  LiveMap l;
+  l.live_m = live_m;
+  l.rows_m = m.tiles_m * grid_r;
+  l.cols_n = m.tiles_n * m.grid_c;
+  l.live_per_xcd = (int32_t)(((int64_t)live_m * l.cols_n + 7) / 8);
+  l.rest_per_xcd = (int32_t)(((int64_t)(l.rows_m - live_m) * l.cols_n + 7) / 8);
+  l.group_m = m.group_m < live_m ? m.group_m : live_m;
+  const int32_t last = live_m % l.group_m ? live_m % l.group_m : l.group_m;
+  l.by_group = fast_div(l.group_m * l.cols_n);
+  l.by_height = fast_div(l.group_m);
+  l.by_last = fast_div(last);
+  l.by_cols = fast_div(l.cols_n);
+  l.by_tiles_m = fast_div(m.tiles_m);
+  l.by_tiles_n = fast_div(m.tiles_n);
+  l.tiles_m = m.tiles_m;
+  l.tiles_n = m.tiles_n;
+  return l;
+}
+
+CCL_HD bool live_tile(const LiveMap& m, int64_t wg, int32_t* pr, int32_t* pc, int32_t* ti, int32_t* tj) {
+  const int32_t xcd = (int32_t)(wg & 7), slot = (int32_t)(wg >> 3);
+  int32_t i, j;
+  if (slot < m.live_per_xcd) {
+    const int32_t t = xcd * m.live_per_xcd + slot;
+    if (t >= m.live_m * m.cols_n) return false;
+    const int32_t first = (t / m.by_group) * m.group_m;
+    const int32_t within = t - first * m.cols_n;
+    const bool whole = m.live_m - first >= m.group_m;
+    const int32_t gm = whole ? m.group_m : m.live_m - first;
+    j = within / (whole ? m.by_height : m.by_last);
+    i = first + within - j * gm;
+  } else {
+    const int32_t t = xcd * m.rest_per_xcd + slot - m.live_per_xcd;
+    if (slot - m.live_per_xcd >= m.rest_per_xcd || t >= (m.rows_m - m.live_m) * m.cols_n) return false;
+    i = t / m.by_cols;
+    j = t - i * m.cols_n;
+    i += m.live_m;
+  }
+  *pr = i / m.by_tiles_m;
+  *ti = i - *pr * m.tiles_m;
+  *pc = j / m.by_tiles_n;
+  *tj = j - *pc * m.tiles_n;
+  return true;
+}
+
 }  // namespace ccl

@@ -28,7 +28,17 @@ struct FusedEpi {
 
 struct FusedParams : GemmParams {
   FusedEpi e;
+  LiveMap live;             // read where remap is 0
 };
+
+// The tile of this workgroup: its owner's (remap), or by the map over the tiles
+// that have valid rows.
+__device__ __forceinline__ bool tile_of_block_raw(const FusedParams& p, int32_t* pr, int32_t* pc, int32_t* ti,
+                                                  int32_t* tj, int32_t* split) {
+  *split = 0;
+  if (p.remap) return map_tile(p.map, blockIdx.x, pr, pc, ti, tj, split);
+  return live_tile(p.live, blockIdx.x, pr, pc, ti, tj);
+}
 
 __device__ __forceinline__ f32x4 bf16x4_to_f32(uint2 b) {
   return f32x4{__uint_as_float(b.x << 16), __uint_as_float(b.x & 0xffff0000u), __uint_as_float(b.y << 16),

@@ -270,6 +270,7 @@ hipError_t launch_gemm_fused(const Plan& plan, const FusedCall& call, int splits
   p.gemm.wide_n = 0;
   FusedParams fp;
   gemm_params(p, f, call.A, call.B, call.C, ff.a, ff.b, ff.c, ff.remap, &fp);
+  fp.live = ff.live;
   fp.alpha = call.alpha;
   fp.c_nt = ff.c_nt ? 1 : 0;
   fp.e.bias = call.bias;

@@ -272,7 +272,8 @@ __device__ __forceinline__ bool tile_of_block_raw(const GemmParams& p, int32_t* 
   return true;
 }
 
-__device__ __forceinline__ bool tile_of_block(const GemmParams& p, int32_t* pr, int32_t* pc,
+template <typename P>
+__device__ __forceinline__ bool tile_of_block(const P& p, int32_t* pr, int32_t* pc,
                                               int32_t* ti, int32_t* tj, int32_t* split) {
   if (!tile_of_block_raw(p, pr, pc, ti, tj, split)) return false;
   *pr = __builtin_amdgcn_readfirstlane(*pr);

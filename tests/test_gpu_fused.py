@@ -164,6 +164,17 @@ def test_every_tile(monkeypatch, tile, waves, fp8, K):
                  alpha=0.05 if fp8 else 1.0, layout=ccl.CCL_LAYOUT_ROWMAJOR)
 
 
+# 40 tile columns in each of 8 and 4 partition rows: few valid rows leave XCDs idle
+@pytest.mark.parametrize("rows", [1, 128, 300, 700, 896])
+@pytest.mark.parametrize("shape", [(1024, 5120, 256, 8, 8, 4096), (1024, 10240, 256, 8, 4, 4096)])
+@pytest.mark.parametrize("grad", [False, True])
+def test_valid_rows_of_few_partitions(shape, rows, grad):
+    if grad:
+        _backward(shape, ccl.CCL_ACT_SILU, True, rows=rows, spoil=True)
+    else:
+        _forward(shape, ccl.CCL_ACT_SILU, True, residual=True, rows=rows, spoil=True)
+
+
 # plans whose launch takes 128-row tiles of 192 or 320 columns, whole and odd K
 # blocks (K / 8 of 64 i and of 32)
 WIDE_TILES = [((256, 1920, 512, 1, 1, 4096), 192), ((256, 1920, 512, 1, 1, 4096), 320),

@@ -1,6 +1,9 @@
 """What ccl_gemm_fused, its gradient and their queries refuse (no GPU needed:
 every refusal comes before the first device call), and the workspaces they ask
 for."""
+import pathlib
+import subprocess
+
 import pytest
 
 from paper_2606_11718_amd import ccl
@@ -94,3 +97,13 @@ def test_matrix_layout():
     assert (lay.block_rows, lay.block_cols, lay.total_bytes) == (256, 512, 512 * 2048 * 2)
     for cols in (0, -4, 6, 1 << 31):
         _refused("CCL_ERR_INVALID_ARG", ccl.ccl_plan_matrix_layout, plan, cols)
+
+
+def test_live_map_covers_every_tile_once(tmp_path):
+    """The map over the tiles with valid rows, compiled for the host."""
+    root = pathlib.Path(__file__).resolve().parent.parent
+    exe = tmp_path / "live_map"
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-I", str(root / "paper_2606_11718_amd/csrc/host"),
+                    str(root / "tests/c/live_map.cpp"), "-o", str(exe)], check=True)
+    run = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert run.returncode == 0, run.stdout
