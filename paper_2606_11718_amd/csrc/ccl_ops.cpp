@@ -35,7 +35,7 @@ ccl_status check_fused(ccl_plan_t plan, int layout, int activation, int gated, i
   if (ccl::splitk_workgroups(p, splits) > kMaxGrid || ccl::splitk_reduce_workgroups(p) > kMaxGrid)
     return fail(CCL_ERR_UNSUPPORTED, "grid exceeds the launch limit");
   if (grad && gated && 2 * p.N > kMaxGrid) return fail(CCL_ERR_UNSUPPORTED, "2 N exceeds 31 bits");
-  *form = ccl::fused_form(p, layout == CCL_LAYOUT_ROWMAJOR, splits, grad, gated == 1, dbias, rows);
+  *form = ccl::fused_form(p, layout == CCL_LAYOUT_ROWMAJOR, splits, grad, gated == 1, dbias, rows, 0);
   if (!offsets_fit(p, form->a, form->b)) return fail(CCL_ERR_UNSUPPORTED, "rows too long for 32-bit in-tile offsets");
   return CCL_OK;
 }

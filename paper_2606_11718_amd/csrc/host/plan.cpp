@@ -710,7 +710,28 @@ OperandAddr matrix_addressing(const Plan& p, int64_t cols, bool rowmajor) {
   return {p.Gc * s, s, (int32_t)(cols / p.Gc), 0};
 }
 
-FusedForm fused_form(const Plan& plan, bool rowmajor, int splits, bool grad, bool gated, bool dbias, int64_t rows) {
+// The 32-K kernel's 128x128 tiles, whose stages let two workgroups share a CU,
+// for an unsplit bf16 launch of f's on larger or deeper-staged ones: while one
+// waits for its epilogue's matrices, `moved` bytes an element of D, the other
+// multiplies. Larger tiles need fewer bytes of A and B an operation, so:
+//  * below 256x256, past one round of the CUs, up to K 1024 (128x128: 2048): in
+//    us, dZ of 5632x6400x512 106.9 -> 80.4, 3072x8704x1792 gated 135 -> 123,
+//    GELU of 7168x5632x1024 104.7 -> 94.9, 2048x4608x768 with a residual 29.0 ->
+//    27.8; K 2048: 128x128 174 -> 155 and 204 -> 170, others 0.87 to 1.09.
+//  * 256x256: from 4 bytes on, up to K 128 for each, 192 from 8 on: dZ of
+//    8192x2048x512 43.9 -> 41.4, gated (8 bytes) K 1024 70.2 -> 58.9, 1536 79.8 ->
+//    73.9; a GELU alone (2 bytes) 1.02 to 1.10 at K 512, 4 bytes 0.97 to 1.08 at
+//    K 1024, 6 bytes 1.04 to 1.12 at K 1536.
+static bool pairs_pay(const Plan& p, const GemmForm& f, int64_t rows, int moved) {
+  if (p.ab_type != DT_BF16 || p.gemm.waves != 8 || f.splits != 1 || f.far || f.stream_b) return false;
+  if (f.kernel == GemmKernel::K32 && f.tile_m == 128 && f.tile_n == 128) return false;
+  const int64_t live = ((rows + f.tile_m - 1) / f.tile_m * f.map.tiles_n * p.Gc + 7) / 8;   // tiles per XCD
+  if (f.tile_m == 256 && f.tile_n == 256) return live > 16 && moved >= 4 && p.K <= (moved >= 8 ? 192 : 128) * moved;
+  return live > 32 && p.K <= (f.tile_m == 128 && f.tile_n == 128 ? 2048 : 1024);
+}
+
+FusedForm fused_form(const Plan& plan, bool rowmajor, int splits, bool grad, bool gated, bool dbias, int64_t rows,
+                     int moved) {
   const Plan& p = plan;
   FusedForm f;
   OperandAddr c;
@@ -725,16 +746,32 @@ FusedForm fused_form(const Plan& plan, bool rowmajor, int splits, bool grad, boo
   f.c_cols = grad ? f.z_cols : gated ? p.N / 2 : p.N;
   f.z = matrix_addressing(p, f.z_cols, rowmajor);
   f.c = matrix_addressing(p, f.c_cols, rowmajor);
-  f.c_nt = f.gemm.c_nt;
   // The kernels whose accumulators are in 16x16 MFMA order under 8 waves take
   // the epilogue themselves; split-K sums its ranges first, and the rest (fp8
   // plans whose K blocks are odd multiples of 64, 4 waves, operands of 2 GiB and
   // more) pass through one range's partials.
+  f.config = p.gemm;
+  if (pairs_pay(p, f.gemm, rows, moved)) {
+    Plan q = p;
+    GemmConfig& g = q.gemm;
+    g.tile_m = g.tile_n = 128;
+    g.tiles_m = p.part_rows() / 128;
+    g.tiles_n = p.part_cols() / 128;
+    g.tiles_per_xcd = (g.tiles_m * g.tiles_n + g.xcd_per_chiplet - 1) / g.xcd_per_chiplet;
+    g.workgroups = g.tiles_per_xcd * kNumXcd;
+    g.group_m = (int)std::min<int64_t>(panels_touched(g, 8) < panels_touched(g, 4) ? 8 : 4, g.tiles_m);
+    g.stage_k = 32;
+    g.stage_64 = g.a_pairs = g.stream_b = false;
+    g.wide_n = 0;
+    f.config = g;
+    f.gemm = gemm_form(q, f.a, f.b, true, 1);
+  }
   const GemmKernel k = f.gemm.kernel;
   f.own = f.gemm.waves == 8 && !f.gemm.far &&
           (k == GemmKernel::A2 || k == GemmKernel::K64 || k == GemmKernel::K32 || k == GemmKernel::FP8P ||
            k == GemmKernel::FP8S);
   f.direct = f.own && f.gemm.splits == 1;
+  f.c_nt = f.gemm.c_nt;
   // Where the valid rows leave XCDs idle, their tiles go round the XCDs instead
   // of to their owners': if that takes fewer rounds of the CUs (us: 4350 of 7168
   // rows in 8 partition rows, 25088x2048 702 -> 516; 845 of them, 5632x1280 27 -> 23).
@@ -752,7 +789,8 @@ FusedForm fused_form(const Plan& plan, bool rowmajor, int splits, bool grad, boo
   }
   f.sum_rows = f.direct ? f.gemm.tile_m : k == GemmKernel::FP8 ? 32 : 16;
   f.partial_bytes = f.direct ? 0 : (int64_t)p.G * p.gemm.tiles_m * p.gemm.tiles_n * f.gemm.splits * p.gemm.tile_m * p.gemm.tile_n * 4;
-  f.workspace_bytes = f.partial_bytes + (dbias ? p.M / f.sum_rows * f.z_cols * 4 : 0);
+  // of 128-row blocks for whichever tile (pairs_pay goes by the call's rows and matrices)
+  f.workspace_bytes = f.partial_bytes + (dbias ? p.M / std::min(f.sum_rows, 128) * f.z_cols * 4 : 0);
   return f;
 }
 

@@ -182,6 +182,7 @@ OperandAddr matrix_addressing(const Plan& p, int64_t cols, bool rowmajor);
 // z_cols columns (N; 2 N for a gated gradient).
 struct FusedForm {
   GemmForm gemm;
+  GemmConfig config;                // the plan's, or that of other tiles
   OperandAddr a, b, c, z;
   int64_t z_cols = 0, c_cols = 0;
   bool direct = false;              // the GEMM's kernel has the epilogue itself (else: by way of partials)
@@ -193,7 +194,10 @@ struct FusedForm {
   int64_t partial_bytes = 0;        // fp32 partial tiles
   int64_t workspace_bytes = 0;      // with the column sums
 };
-FusedForm fused_form(const Plan& p, bool rowmajor, int splits, bool grad, bool gated, bool dbias, int64_t rows);
+// moved: bytes of C, Z and R that the epilogue reads and writes an element of A B
+// (the workspace does not depend on it).
+FusedForm fused_form(const Plan& p, bool rowmajor, int splits, bool grad, bool gated, bool dbias, int64_t rows,
+                     int moved);
 
 // tile_of_wg of an unsplit ccl_gemm's own launch.
 void launch_tile_of_wg(const Plan& p, int64_t wg, int* xcd, int64_t* tile_m, int64_t* tile_n);

@@ -263,10 +263,13 @@ static hipError_t launch_own(const GemmForm& f, const FusedParams& fp, hipStream
 }
 
 hipError_t launch_gemm_fused(const Plan& plan, const FusedCall& call, int splits, void* ws, hipStream_t stream) {
+  const int wide = call.gated ? 2 : 1;        // matrices of half or twice D's columns
+  const int moved = call.grad ? (call.Zin ? 4 : 2) * wide : (call.R ? 4 : 2) / wide + (call.Zout ? 2 : 0);
   const FusedForm ff = fused_form(plan, call.rowmajor, splits, call.grad, call.gated, call.dbias != nullptr,
-                                  call.rows);
+                                  call.rows, moved);
   const GemmForm& f = ff.gemm;
   Plan p = plan;
+  p.gemm = ff.config;
   p.gemm.wide_n = 0;
   FusedParams fp;
   gemm_params(p, f, call.A, call.B, call.C, ff.a, ff.b, ff.c, ff.remap, &fp);

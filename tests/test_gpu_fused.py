@@ -175,6 +175,19 @@ def test_valid_rows_of_few_partitions(shape, rows, grad):
         _forward(shape, ccl.CCL_ACT_SILU, True, residual=True, rows=rows, spoil=True)
 
 
+# past one round of the CUs on 128x192, 128x128 and 256x256 tiles, short K: 128x128
+# tiles, two workgroups to a CU
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("shape,rows", [((2048, 4608, 256, 8, 2, 4096), 1900), ((1408, 6400, 96, 1, 1, 4096), None),
+                                        ((4096, 4096, 128, 8, 2, 4096), 4001)])
+def test_paired_workgroups(shape, rows, grad, gated):
+    if grad:
+        _backward(shape, ccl.CCL_ACT_GELU, gated, rows=rows, spoil=True)
+    else:
+        _forward(shape, ccl.CCL_ACT_GELU, gated, bias="f32", residual=True, keep=not gated, rows=rows, spoil=True)
+
+
 # plans whose launch takes 128-row tiles of 192 or 320 columns, whole and odd K
 # blocks (K / 8 of 64 i and of 32)
 WIDE_TILES = [((256, 1920, 512, 1, 1, 4096), 192), ((256, 1920, 512, 1, 1, 4096), 320),
