@@ -35,7 +35,8 @@ TRAFFIC_FILE = os.path.join(ROOT, "profiles", "gemm_llama_fwd_traffic.json")
 CSRC = os.path.join(ROOT, "paper_2606_11718_amd", "csrc")
 # the sources that fix the GEMM's memory traffic: the kernels, the
 # workgroup -> tile map and the plan that picks tile shape and raster
-GEMM_SRCS = tuple(os.path.join(CSRC, f) for f in ("kernels/gemm.hip", "host/tile_map.hpp", "host/plan.cpp"))
+GEMM_SRCS = tuple(os.path.join(CSRC, f) for f in ("kernels/gemm.hip", "kernels/gemm_tiles.hpp", "host/tile_map.hpp",
+                                                    "host/plan.cpp"))
 
 
 def kernel_hash(srcs=GEMM_SRCS) -> str:

@@ -811,13 +811,16 @@ MoeForm moe_form(const MoeShape& s, int64_t tokens) {
   f.up_workgroups = used * groups + (f.list ? 0 : (tokens + 7) / 8);
   // The down product, in steps of a 128-byte line of 16 rows. kMoeDownTiles
   // tiles of y share the loads of h, in ranges until every CU has a workgroup (a
-  // step at least for every wave). Where that takes ranges, whose sum is a launch
+  // step at least for every wave); one tile a workgroup where 16 ranges of four
+  // would reach half of the CUs (hidden 256 and 512: 45.1 -> 38.7, 36.7 -> 33.7 us;
+  // 768: 55.2 -> 57.7). Where that takes ranges, whose sum is a launch
   // of its own, of few steps: one tile a workgroup and no ranges (3 tokens, 9
   // experts of 1216 x 256: 15.9 -> 13.6 us; but not past one round of the CUs).
   const int64_t lines = used * ((s.ffn * (s.fp8 ? 1 : 2) + 127) / 128);
-  f.down_nt = lines >= 16 && lines <= kMoeFewLines && f.down_tiles <= 256 ? 1 : kMoeDownTiles;
+  const bool few = lines >= 16 && lines <= kMoeFewLines && f.down_tiles <= 256;
+  f.down_nt = few || (lines > kMoeFewLines && f.down_tiles <= 8 * kMoeDownTiles) ? 1 : kMoeDownTiles;
   f.down_groups = (f.down_tiles + f.down_nt - 1) / f.down_nt;
-  f.splits = f.down_nt == 1 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(16, std::min<int64_t>(256 / f.down_groups, lines / 8)));
+  f.splits = few ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(16, std::min<int64_t>(256 / f.down_groups, lines / 8)));
   const auto up16 = [](int64_t n) { return (n + 15) / 16 * 16; };
   f.probs_at = up16(slots * 4);
   f.h_at = f.probs_at + up16(slots * 4);

@@ -114,6 +114,13 @@ def test_sizes(hidden, ffn, fp8):
     _run(5, hidden, ffn, 6, 2, fp8)
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("tokens", [9, 50])
+def test_narrow_layer_in_ranges(tokens, fp8):
+    """Few columns of y, many steps: one column tile a workgroup, cut into ranges."""
+    _run(tokens, 256, 1200, 40, 4, fp8)
+
+
 @pytest.mark.parametrize("experts,top_k", [(1, 1), (2, 2), (3, 1), (16, 16), (63, 8), (64, 8), (65, 3), (128, 8), (257, 10), (512, 16)])
 @pytest.mark.parametrize("tokens", [1, 3, 40])
 def test_experts(experts, top_k, tokens):
