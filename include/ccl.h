@@ -405,14 +405,15 @@ typedef struct ccl_moe {
  * fp32 (rows logits_ld apart), y as x; ids (int32) and probs (fp32), both
  * tokens x top_k, take the choice, or are NULL. The scales are fp32, one per
  * expert, or NULL (1). x, gate_up, down and the workspace are 16-byte aligned,
- * x_ld a multiple of 8, and every leading dimension at most 2^22. y may overlap x only if it is a call of no tokens; the
- * workspace's contents on entry do not matter, and calls that share one must
- * be ordered on one stream. No tokens: nothing is launched.
+ * x_ld a multiple of 8, and every leading dimension at most 2^22. y must not
+ * overlap an input; the workspace's contents on entry do not matter, and calls
+ * that share one must be ordered on one stream. No tokens: nothing is launched.
  * Errors: CCL_ERR_INVALID_ARG (NULL argument, sizes outside the ranges above,
  * an unknown activation or weight type, a leading dimension or stride smaller
  * than what it spans, workspace missing or too small); CCL_ERR_UNSUPPORTED
- * (hidden or ffn not a multiple of 16, or above 2^22; tokens * top_k * ffn of 2^29
- * and more; a launch too large; device not gfx950); CCL_ERR_MISALIGNED_POINTER; CCL_ERR_HIP.
+ * (hidden or ffn not a multiple of 16, or above 2^22; tokens * top_k * ffn of
+ * 2^29 and more; a launch too large; device not gfx950);
+ * CCL_ERR_MISALIGNED_POINTER; CCL_ERR_HIP.
  */
 ccl_status ccl_moe_workspace(const ccl_moe* moe, int64_t tokens, int64_t* workspace_bytes);
 ccl_status ccl_moe_decode(const ccl_moe* moe, int64_t tokens, const void* x, int64_t x_ld,

@@ -1,5 +1,5 @@
 // Epilogues of ccl_gemm_fused and ccl_gemm_fused_grad on a tile of the
-// product D = A B. Included by gemm.hip inside its namespace.
+// product D = A B. Included by gemm_tiles.hpp inside its namespace.
 //
 // Forward:  Z = alpha D + bias, C = act(Z) + beta R; gated: the columns of D
 //           alternate in groups of 16, gate and up, and C = act(Zg) Zu + beta R
@@ -10,6 +10,12 @@
 //           sums of the fp32 dZ (the bias gradient) are formed tile by tile
 //           and added up in ascending row order by bias_reduce_kernel.
 // Rows at and past `rows` come out as zeros; nothing of D, R or Z reaches them.
+//
+// What it adds to the product, us (product alone -> with it): SwiGLU with Z kept, 4096x1536x2048, 24.7 -> 27.3; dZ of a gated
+// 4096x768x2048 15.7 -> 22.1 (25 MB of Z and dZ behind a K loop of 10 us); GELU with
+// Z kept, 8192x28672x8192, 2596 -> 2690. Reading R and Z and storing wait on memory
+// while the workgroup's matrix cores idle: short K takes tiles of which two share
+// a CU (fused_form's rule).
 
 struct FusedEpi {
   const void* bias;         // per column of D (null: none)

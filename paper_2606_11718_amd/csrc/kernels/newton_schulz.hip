@@ -16,6 +16,11 @@
 // leave the result 1.3e-3 from the 64-bit one; bf16 iterates, with 8 bits, 1e-2.
 //
 // Sides are padded with zeros to multiples of 128, which the steps keep zero.
+//
+// Measured, us a call of five steps (PFLOP/s of the operations above): 768x2048
+// 133 (0.15: 17 dependent launches of 4 to 9), 16 of 2048x1536 1749 (0.83: 128x128
+// tiles in the symmetric products, three rounds of 256x256 in the third), 8192x28672
+// 24400 (1.30: the matrix cores at the power limit).
 #include "gemm_tiles.hpp"
 
 namespace ccl {
