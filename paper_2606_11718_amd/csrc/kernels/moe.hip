@@ -278,10 +278,14 @@ __global__ void __launch_bounds__(kThreads, STREAM ? 2 : 4) moe_up_kernel(MoePar
       if (lane < p.top_k) s_ids[t * p.top_k + lane] = id;
       if (blockIdx.x == 0) put_route(p, t, lane, id, prob);
     }
+    if (p.tokens == 1 && threadIdx.x == 0) {      // one token's experts are distinct
+      s_entry[0] = slot;
+      s_n = 1;
+    }
     __syncthreads();
     expert = s_ids[slot];
     if (expert < 0) return;
-    if (wave == 0) {
+    if (wave == 0 && p.tokens > 1) {
       // The first slot of an expert does its work for all of them.
       int n = 0;
       bool first = true;
@@ -294,7 +298,7 @@ __global__ void __launch_bounds__(kThreads, STREAM ? 2 : 4) moe_up_kernel(MoePar
       }
       if (lane == 0) s_n = first ? n : 0;
     }
-    __syncthreads();
+    if (p.tokens > 1) __syncthreads();
   } else {
     const int routers = (p.tokens + kWaves - 1) / kWaves;
     if ((int)blockIdx.x < routers) {
@@ -485,46 +489,64 @@ __global__ void __launch_bounds__(kThreads, 2) moe_down_kernel(MoeParams p) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int slots = p.tokens * p.top_k;
   const int group = blockIdx.x % p.groups, split = blockIdx.x / p.groups;
-  int32_t my_id[2], my_rank[2];                   // kSlots / kThreads slots per thread
-  for (int e = threadIdx.x; e < p.experts; e += kThreads) s_count[e] = 0;
   for (int i = threadIdx.x; i < kWaves * p.tokens * COLS / 4; i += kThreads)
     reinterpret_cast<f32x4*>(s_y)[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int i = threadIdx.x + j * kThreads;
-    my_id[j] = i < slots ? p.ws_ids[i] : -1;
-    if (my_id[j] >= 0) s_probs[i] = p.ws_probs[i] * (p.down_scale ? p.down_scale[my_id[j]] : 1.f);
-  }
-  __syncthreads();
-  // The order of an expert's slots in its list is free: it places rows of a
-  // product, whose sums do not mix rows.
-#pragma unroll
-  for (int j = 0; j < 2; ++j)
-    if (my_id[j] >= 0) my_rank[j] = atomicAdd(&s_count[my_id[j]], 1);
-  __syncthreads();
-  if (wave == 0) {
-    int used = 0, start = 0;
-    for (int e0 = 0; e0 < p.experts; e0 += 64) {
-      const int c = e0 + lane < p.experts ? s_count[e0 + lane] : 0;
-      const uint64_t mask = __ballot(c > 0);
-      if (c > 0) s_used[used + __builtin_popcountll(mask & ((1ull << lane) - 1))] = e0 + lane;
-      used += __builtin_popcountll(mask);
-      int sum = c;
-#pragma unroll
-      for (int x = 1; x < 64; x <<= 1) {
-        const int o = __shfl_up(sum, x);
-        if (lane >= x) sum += o;
+  if (p.tokens == 1) {
+    // Its experts are distinct: in the order of their slots, without counting.
+    if (wave == 0) {
+      const int id = lane < slots ? p.ws_ids[lane] : -1;
+      const uint64_t mask = __ballot(id >= 0);
+      if (id >= 0) {
+        const int at = __builtin_popcountll(mask & ((1ull << lane) - 1));
+        s_probs[lane] = p.ws_probs[lane] * (p.down_scale ? p.down_scale[id] : 1.f);
+        s_used[at] = id;
+        s_count[id] = 1;
+        s_start[id] = at;
+        s_list[at] = lane;
       }
-      if (e0 + lane < p.experts) s_start[e0 + lane] = start + sum - c;
-      start += __shfl(sum, 63);
+      if (lane == 0) s_total = __builtin_popcountll(mask);
     }
-    if (lane == 0) s_total = used;
-  }
-  __syncthreads();
+    __syncthreads();
+  } else {
+    int32_t my_id[2], my_rank[2];                   // kSlots / kThreads slots per thread
+    for (int e = threadIdx.x; e < p.experts; e += kThreads) s_count[e] = 0;
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
-    if (my_id[j] >= 0) s_list[s_start[my_id[j]] + my_rank[j]] = threadIdx.x + j * kThreads;
-  __syncthreads();
+    for (int j = 0; j < 2; ++j) {
+      const int i = threadIdx.x + j * kThreads;
+      my_id[j] = i < slots ? p.ws_ids[i] : -1;
+      if (my_id[j] >= 0) s_probs[i] = p.ws_probs[i] * (p.down_scale ? p.down_scale[my_id[j]] : 1.f);
+    }
+    __syncthreads();
+    // The order of an expert's slots in its list is free: it places rows of a
+    // product, whose sums do not mix rows.
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (my_id[j] >= 0) my_rank[j] = atomicAdd(&s_count[my_id[j]], 1);
+    __syncthreads();
+    if (wave == 0) {
+      int used = 0, start = 0;
+      for (int e0 = 0; e0 < p.experts; e0 += 64) {
+        const int c = e0 + lane < p.experts ? s_count[e0 + lane] : 0;
+        const uint64_t mask = __ballot(c > 0);
+        if (c > 0) s_used[used + __builtin_popcountll(mask & ((1ull << lane) - 1))] = e0 + lane;
+        used += __builtin_popcountll(mask);
+        int sum = c;
+#pragma unroll
+        for (int x = 1; x < 64; x <<= 1) {
+          const int o = __shfl_up(sum, x);
+          if (lane >= x) sum += o;
+        }
+        if (e0 + lane < p.experts) s_start[e0 + lane] = start + sum - c;
+        start += __shfl(sum, 63);
+      }
+      if (lane == 0) s_total = used;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (my_id[j] >= 0) s_list[s_start[my_id[j]] + my_rank[j]] = threadIdx.x + j * kThreads;
+    __syncthreads();
+  }
 
   const int K = p.ffn, D = p.hidden;
   const int r = lane & 15, g = lane >> 4;
