@@ -430,10 +430,10 @@ ccl_status ccl_moe_decode(const ccl_moe* moe, int64_t tokens, const void* x, int
  *   O = X, transposed back.
  * The defaults (steps 5, (a, b, c) = 3.4445, -4.7750, 2.0315, eps 1e-7) bring
  * every singular value that is not tiny to around 1. The norm is summed in 64
- * bits; X, S and S S are held in fp16 times 2^13 with 32-bit sums, which is
- * about 1.3e-3 of the result, and O is rounded to bf16 once. Other
- * coefficients must keep the elements of X, S and b S + c S S below 8: past
- * that fp16 overflows to infinity. A zero G gives zeros; an infinity or a NaN
+ * bits; X, S and b S + c S S - (b + c) I are held in fp16 times 2^13 with 32-bit
+ * sums, which is up to about 1.4e-3 of the result, and O is rounded to bf16
+ * once. Other coefficients must keep their elements below 8 (the shift is left
+ * out where |b + c| is 4 or more): past that fp16 overflows to infinity. A zero G gives zeros; an infinity or a NaN
  * in G gives NaNs in its own matrix only. steps 0: the scaled G.
  */
 

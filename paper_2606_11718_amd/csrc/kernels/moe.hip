@@ -22,8 +22,8 @@
 // end. Sums over K, over experts and the softmax are fp32, in a fixed order.
 //
 // Measured, us a call: one token, 8 of 128 experts of 2048 x 768 in bf16 (75 MB)
-// 25.3: up 17, of which launch, routing and the sums about 6 and the weights 4.6
-// TB/s; down 10. 48 tokens over the same experts in fp8 (577 MB) 128, 4.5 TB/s:
+// 25.6: up 17, of which launch, routing and the sums about 6 and the weights 4.6
+// TB/s; down 9. 48 tokens over the same experts in fp8 (577 MB) 128, 4.5 TB/s:
 // up 84, down 43, its ranges' sum 5.
 #include <hip/hip_runtime.h>
 

@@ -1,7 +1,8 @@
 // Orthogonalised updates (ccl_orthogonalize): Newton-Schulz steps of an odd
 // quintic on a batch of matrices,
 //   X = G / (|G|_F + eps), transposed if tall (p = min side, q = max side)
-//   S = X X^T;  B = b S + c S S;  X <- a X + B X       (each step)
+//   S = X X^T;  B = b S + c S S + s I;  X <- (a - s) X + B X       (each step;
+//   s = -(b + c), which leaves B near 0 where S is near I)
 // The three products of a step are matrix products with an addend, out = alpha
 // U V' + beta D, on the matrix cores. S and B are symmetric: only the tiles on
 // and below the diagonal are computed, each stored twice, which halves two of
@@ -13,14 +14,15 @@
 // stay below 1.3, so every element of X, S and B is below 3 and 2^13 of it
 // below fp16's 65504, while 2^13 keeps elements down to 2^-27 at full
 // precision (those of a first X of 8192 x 28672 are around 2^-14). The 11 bits
-// leave the result 1.3e-3 from the 64-bit one; bf16 iterates, with 8 bits, 1e-2.
+// leave the result 0.9e-3 (wide) to 1.4e-3 (square) from the 64-bit one; bf16
+// iterates, with 8 bits, 1e-2.
 //
 // Sides are padded with zeros to multiples of 128, which the steps keep zero.
 //
 // Measured, us a call of five steps (PFLOP/s of the operations above): 768x2048
-// 133 (0.15: 17 dependent launches of 4 to 9), 16 of 2048x1536 1749 (0.83: 128x128
+// 132 (0.15: 17 dependent launches of 4 to 9), 16 of 2048x1536 1749 (0.83: 128x128
 // tiles in the symmetric products, three rounds of 256x256 in the third), 8192x28672
-// 24400 (1.30: the matrix cores at the power limit).
+// 24100 (1.31: the matrix cores at the power limit).
 #include "gemm_tiles.hpp"
 
 namespace ccl {
@@ -53,6 +55,7 @@ struct NsParams {
   int32_t splits, ksplit;   // the other tiles' K ranges, of ksplit steps
   int32_t whole_xcd, split_xcd;   // workgroups of each kind per XCD
   float alpha, beta;
+  float diag;               // added on the diagonal of a symmetric out
 };
 
 // 8 waves, 2 x 4. (64x64 in 2 x 2 waves reads a third less of LDS a step and took
@@ -223,9 +226,16 @@ __device__ __forceinline__ void ns_copy_in(const NsParams& p, const StagedTile<R
   }
 }
 
-// alpha acc + beta D on four staged values, in place.
-__device__ __forceinline__ void ns_combine(const NsParams& p, uint2* at, f32x4 acc) {
+// alpha acc + beta D + diag I on four staged values of row r, columns c .. c + 3,
+// in place.
+template <bool SYM>
+__device__ __forceinline__ void ns_combine(const NsParams& p, uint2* at, f32x4 acc, int r, int c) {
   f32x4 o = acc * p.alpha;
+  if constexpr (SYM) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (r == c + j) o[j] += p.diag;
+  }
   if (p.D) {
     const f16x4 d = __builtin_bit_cast(f16x4, *at);
 #pragma unroll
@@ -453,7 +463,10 @@ __global__ void __launch_bounds__(512, NS * (BM + BN) * 128 <= 80 * 1024 ? 4 : 2
   for (int mt = 0; mt < T::TM; ++mt)
 #pragma unroll
     for (int nt = 0; nt < T::TN; ++nt)
-      ns_combine(p, t.at(wm * T::WM + 16 * mt + (lane & 15), wn * T::WN + 16 * nt + 4 * (lane >> 4)), acc[mt][nt]);
+      {
+        const int r = wm * T::WM + 16 * mt + (lane & 15), c = wn * T::WN + 16 * nt + 4 * (lane >> 4);
+        ns_combine<SYM>(p, t.at(r, c), acc[mt][nt], ti * BM + r, tj * BN + c);
+      }
   staged_barrier();
   ns_store<BM, BN, SYM>(p, t, mat, ti * BM, tj * BN, ti != tj, tid);
 #endif
@@ -486,7 +499,8 @@ __global__ void __launch_bounds__(512) ns_split_sum_kernel(NsParams p) {
     f32x4 v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
     for (int r = 0; r < p.splits; ++r) v += from[(int64_t)r * (B * B / 4) + at];
-    ns_combine(p, t.at(row + (lane & 15), 16 * col + 4 * (lane >> 4)), v);
+    const int r = row + (lane & 15), c = 16 * col + 4 * (lane >> 4);
+    ns_combine<SYM>(p, t.at(r, c), v, ti * B + row0 + r, tj * B + c);
   }
   __syncthreads();
   ns_store<ROWS, B, SYM>(p, t, mat, ti * B + row0, tj * B, ti != tj, tid);
@@ -680,6 +694,11 @@ hipError_t launch_orthogonalize(const OrthoShape& s, const OrthoCall& c, void* w
                        static_cast<uint16_t*>(c.O), c.o_stride, c.o_ld, s.rows, s.cols, in.tall);
     return hipGetLastError();
   }
+  // S comes near I: B is held less its value there, whose rounding on the
+  // diagonal was the largest of the errors (100x100: 1.7e-3 of the result, now
+  // 1.4e-3). Larger values gain nothing and might overflow.
+  const float at_one = -(c.coeffs[1] + c.coeffs[2]);
+  const float shift = at_one > -4.f && at_one < 4.f ? at_one : 0.f;
   for (int step = 0; step < c.steps; ++step) {
     const uint16_t* X = x[step & 1];
     const bool last = step + 1 == c.steps;
@@ -700,7 +719,7 @@ hipError_t launch_orthogonalize(const OrthoShape& s, const OrthoCall& c, void* w
     p.K = f.qp;
     p.alpha = 1.f / kScale;
     if ((e = ns_launch<true>(p, s.batch, f.gram, stream)) != hipSuccess) return e;
-    // B = b S + c S S (S is its own transpose)
+    // B = b S + c S S + s I (S is its own transpose)
     p.U = p.V = p.D = S;
     p.u_stride = p.v_stride = f.s_elems;
     p.ldu = p.ldv = f.ld_p;
@@ -708,8 +727,10 @@ hipError_t launch_orthogonalize(const OrthoShape& s, const OrthoCall& c, void* w
     p.K = f.pp;
     p.alpha = c.coeffs[2] / kScale;
     p.beta = c.coeffs[1];
+    p.diag = kScale * shift;
     if ((e = ns_launch<true>(p, s.batch, f.square, stream)) != hipSuccess) return e;
-    // X <- a X + B X
+    // X <- (a - s) X + B X
+    p.diag = 0.f;
     p.U = B;
     p.V = p.D = X;
     p.v_stride = f.x_elems;
@@ -721,7 +742,7 @@ hipError_t launch_orthogonalize(const OrthoShape& s, const OrthoCall& c, void* w
     p.o_trans = in.tall;
     p.O = last ? static_cast<uint16_t*>(c.O) : nullptr;
     p.alpha = last ? 1.f / (kScale * kScale) : 1.f / kScale;
-    p.beta = last ? c.coeffs[0] / kScale : c.coeffs[0];
+    p.beta = (c.coeffs[0] - shift) / (last ? kScale : 1.f);
     e = ns_launch<false>(p, s.batch, f.update, stream);
     if (e != hipSuccess) return e;
   }
