@@ -715,7 +715,7 @@ OperandAddr matrix_addressing(const Plan& p, int64_t cols, bool rowmajor) {
 // waits for its epilogue's matrices, `moved` bytes an element of D, the other
 // multiplies. Larger tiles need fewer bytes of A and B an operation, so:
 //  * below 256x256, past one round of the CUs, up to K 1024 (128x128: 2048): in
-//    us, dZ of 5632x6400x512 106.9 -> 80.4, 3072x8704x1792 gated 135 -> 123,
+//    us, dZ of 5632x6400x512 106.9 -> 80.4, 7168x5632x512 gated 132 -> 111,
 //    GELU of 7168x5632x1024 104.7 -> 94.9, 2048x4608x768 with a residual 29.0 ->
 //    27.8; K 2048: 128x128 174 -> 155 and 204 -> 170, others 0.87 to 1.09.
 //  * 256x256: from 4 bytes on, up to K 128 for each, 192 from 8 on: dZ of
