@@ -90,8 +90,17 @@ class GatedFFN:
         ccl.ccl_unpack(plan, ccl.CCL_C, buf[2], out, b.shape[1])
         return out
 
+    def _valid(self, t, rows):
+        """t with zeros past its first `rows` rows, whatever it holds there (0 * NaN would reach a sum over rows)."""
+        if rows is None or rows >= self.M:
+            return t
+        t = t.clone()
+        t[rows:] = 0
+        return t
+
     def backward(self, x, h, z, dy, rows: int | None = None):
-        """Gradients of W_up and W_down; rows of dy past `rows` must be zero."""
+        """Gradients of W_up and W_down from the first `rows` tokens and from forward's h and z for them."""
+        x, dy = self._valid(x, rows), self._valid(dy, rows)
         dz = self._empty(self.M, 2 * self.F)
         ccl.ccl_gemm_fused_grad(self.dh, dy, self.w_down16_t, z, dz, activation=ccl.CCL_ACT_SILU, gated=True, rows=rows,
                                 layout=ROWMAJOR, workspace=self.ws, workspace_bytes=self.ws.numel())
