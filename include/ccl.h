@@ -433,8 +433,9 @@ ccl_status ccl_moe_decode(const ccl_moe* moe, int64_t tokens, const void* x, int
  * bits; X, S and b S + c S S - (b + c) I are held in fp16 times 2^13 with 32-bit
  * sums, which is up to about 1.4e-3 of the result, and O is rounded to bf16
  * once. Other coefficients must keep their elements below 8 (the shift is left
- * out where |b + c| is 4 or more): past that fp16 overflows to infinity. A zero G gives zeros; an infinity or a NaN
- * in G gives NaNs in its own matrix only. steps 0: the scaled G.
+ * out where |b + c| is 4 or more): past that fp16 overflows to infinity. A zero G
+ * gives zeros, also with eps = 0; an infinity or a NaN in G gives NaNs in its own
+ * matrix only. steps 0: the scaled G.
  */
 
 /* Device workspace of ccl_orthogonalize in bytes, and the call. G is bf16 or

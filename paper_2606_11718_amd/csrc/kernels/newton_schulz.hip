@@ -585,7 +585,11 @@ __global__ void __launch_bounds__(256) ns_first_kernel(NsInput p) {
   const int32_t t = blockIdx.x - mat * tiles, tr = t / tiles_c, tc = t - tr * tiles_c;
   double sum = 0.0;
   for (int i = threadIdx.x; i < p.chunks; i += 256) sum += p.part[mat * p.chunks + i];
-  const float scale = (float)(kScale / (sqrt(block_sum(sum, sm)) + (double)p.eps));
+  sum = block_sum(sum, sm);
+  // The factor as m 2^e, m in [1/2, 1]: the inverse of a norm may be past fp32's
+  // largest, or subnormal, where G times it is not. A zero G: zeros, with no eps too.
+  int e;
+  const float m = (float)frexp(sum == 0.0 ? 0.0 : kScale / (sqrt(sum) + (double)p.eps), &e);
   // the tile in G: rows g_r .., columns g_c ..
   const int64_t g_r = 64 * (int64_t)(p.tall ? tc : tr), g_c = 64 * (int64_t)(p.tall ? tr : tc);
   uint16_t* X = p.X + mat * p.x_stride + 64 * (int64_t)tr * p.ld_x + 64 * tc;
@@ -596,7 +600,7 @@ __global__ void __launch_bounds__(256) ns_first_kernel(NsInput p) {
     if (g_r + r < p.rows && g_c + c < p.cols) ns_load8(p, mat, g_r + r, g_c + c, v);
     f16x8 o;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = (_Float16)(v[j] * scale);
+    for (int j = 0; j < 8; ++j) o[j] = (_Float16)(ldexpf(v[j], e) * m);
     if (!p.tall) {
       *reinterpret_cast<f16x8*>(X + (int64_t)r * p.ld_x + c) = o;
     } else {
