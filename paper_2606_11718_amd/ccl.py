@@ -2,7 +2,8 @@
 
 Argument marshalling only: every step runs in the HIP library. Device
 buffers may be given as torch tensors (their data_ptr() is passed) or as
-integer device addresses; `stream` may be a torch.cuda.Stream, an integer
+integer device addresses (what a call takes from a tensor beyond its address, a
+type or a stride, is checked against what the call reads); `stream` may be a torch.cuda.Stream, an integer
 hipStream_t, or None (torch's current stream when torch has initialised the
 GPU, else the null stream). Errors raise CCLError with the library's status
 and message. If libccl.so is not built, loading raises; there is no fallback.
@@ -362,22 +363,92 @@ def ccl_moe_workspace(moe: _Moe, tokens: int) -> int:
     return nbytes.value
 
 
-def _row_stride(t, ld, width: int) -> int:
-    """Elements between rows: as given, else a 2-d tensor's own (its row length for an address)."""
+def _refuse(name: str, why: str) -> None:
+    raise CCLError(1, f"{name}: {why}")
+
+
+def _rows(name: str, t, ld, rows: int, width: int, dtype, bits=None) -> tuple[int, int]:
+    """Address of a rows x width operand and the elements between its rows: as given, else a tensor's own (its row
+    length for an address or a flat tensor). A tensor has to be of dtype (or bits, an integer type that holds it)
+    and to have its rows whole and as many as the call takes."""
+    if t is None or isinstance(t, int):
+        return t or 0, width if ld is None else ld
+    if t.dtype is not dtype and (bits is None or t.dtype is not bits):
+        _refuse(name, f"a tensor of {t.dtype}, not {dtype}")
     if ld is not None:
-        return ld
-    return width if t is None or isinstance(t, int) or t.dim() < 2 else t.stride(0)
+        return t.data_ptr(), ld
+    shape, stride = t.shape, t.stride()
+    if len(shape) > 2:
+        try:
+            flat = t.view(-1, shape[-1])
+        except RuntimeError:
+            _refuse(name, "rows that are not one stride apart")
+        shape, stride = flat.shape, flat.stride()
+    if len(shape) < 2:
+        if not t.is_contiguous() or t.numel() < rows * width:
+            _refuse(name, f"a flat tensor has to hold {rows} x {width} elements without gaps")
+        return t.data_ptr(), width
+    n, w = shape
+    ld, step = stride
+    if n < rows or w < width or (step != 1 and w > 1):
+        _refuse(name, f"a tensor of {n} x {w} with columns {step} apart, not {rows} x {width} with columns side by side")
+    return t.data_ptr(), ld
+
+
+def _whole(name: str, t, n: int, dtype) -> int:
+    """Address of n elements side by side."""
+    if t is None or isinstance(t, int):
+        return t or 0
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
+        _refuse(name, f"not {n} elements of {dtype} without gaps")
+    return t.data_ptr()
+
+
+def _expert_weights(name: str, t, experts: int, rows: int, cols: int, ld: int, stride: int, dtype) -> int:
+    """Address of a layer's weights, (experts, rows, cols) or raw memory of as many bytes."""
+    if t is None or isinstance(t, int):
+        return t or 0
+    ld = ld or cols
+    stride = stride or rows * ld
+    if t.dtype is dtype:
+        shape = t.shape
+        if len(shape) == 3:
+            steps = t.stride()
+            apart = steps == (stride, ld, 1) or (experts == 1 and steps[1:] == (ld, 1))
+            if shape[0] < experts or shape[1] < rows or shape[2] < cols or not apart:
+                _refuse(name, f"{tuple(shape)} with strides {steps}, not {(experts, rows, cols)} with {(stride, ld, 1)}")
+            return t.data_ptr()
+    elif t.dtype.is_floating_point:
+        _refuse(name, f"a tensor of {t.dtype}, not {dtype}")
+    if not t.is_contiguous() or t.nbytes < ((experts - 1) * stride + (rows - 1) * ld + cols) * dtype.itemsize:
+        _refuse(name, "smaller than the layer's weights, or with gaps")
+    return t.data_ptr()
 
 
 def ccl_moe_decode(moe: _Moe, tokens: int, x, logits, gate_up, down, y, *, ids=None, probs=None, gate_up_scale=None,
                    down_scale=None, workspace=None, workspace_bytes: int = 0, x_ld: int | None = None,
                    logits_ld: int | None = None, y_ld: int | None = None, stream=None) -> None:
     """y = the layer on `tokens` rows of x, routed by logits; ids and probs take the choice."""
-    _check(library().ccl_moe_decode(
-        ctypes.byref(moe), tokens, _ptr(x), _row_stride(x, x_ld, moe.hidden), _ptr(logits),
-        _row_stride(logits, logits_ld, moe.experts), _ptr(gate_up), _ptr(gate_up_scale), _ptr(down), _ptr(down_scale),
-        _ptr(y), _row_stride(y, y_ld, moe.hidden), _ptr(ids), _ptr(probs), _ptr(workspace), workspace_bytes,
-        _stream(stream)))
+    call = library().ccl_moe_decode
+    import torch
+    bf16, f32, bits = torch.bfloat16, torch.float32, torch.int16
+    D, F, E = moe.hidden, moe.ffn, moe.experts
+    w = torch.float8_e4m3fn if moe.weight_type == CCL_DT_FP8_E4M3 else bf16
+    x, x_ld = _rows("x", x, x_ld, tokens, D, bf16, bits)
+    logits, logits_ld = _rows("logits", logits, logits_ld, tokens, E, f32)
+    y, y_ld = _rows("y", y, y_ld, tokens, D, bf16, bits)
+    if ids is not None:
+        ids = _whole("ids", ids, tokens * moe.top_k, torch.int32)
+    if probs is not None:
+        probs = _whole("probs", probs, tokens * moe.top_k, f32)
+    if gate_up_scale is not None:
+        gate_up_scale = _whole("gate_up_scale", gate_up_scale, E, f32)
+    if down_scale is not None:
+        down_scale = _whole("down_scale", down_scale, E, f32)
+    gate_up = _expert_weights("gate_up", gate_up, E, 2 * F, D, moe.gate_up_ld, moe.gate_up_stride, w)
+    down = _expert_weights("down", down, E, D, F, moe.down_ld, moe.down_stride, w)
+    _check(call(ctypes.byref(moe), tokens, x, x_ld, logits, logits_ld, gate_up, gate_up_scale, down, down_scale, y, y_ld,
+                ids, probs, _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 def ccl_orthogonalize_workspace(batch: int, rows: int, cols: int) -> int:
