@@ -392,7 +392,7 @@ def _rows(name: str, t, ld, rows: int, width: int, dtype, bits=None) -> tuple[in
     ld, step = stride
     if n < rows or w < width or (step != 1 and w > 1):
         _refuse(name, f"a tensor of {n} x {w} with columns {step} apart, not {rows} x {width} with columns side by side")
-    return t.data_ptr(), ld
+    return t.data_ptr(), ld if rows > 1 else width      # one row: a stride that means nothing
 
 
 def _whole(name: str, t, n: int, dtype) -> int:
