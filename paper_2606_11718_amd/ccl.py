@@ -171,6 +171,19 @@ def _ptr(x) -> int:
     return int(x.data_ptr())
 
 
+def _refuse(name: str, why: str) -> None:
+    raise CCLError(1, f"{name}: {why}")
+
+
+def _whole(name: str, t, n: int, dtype) -> int:
+    """Address of n elements side by side."""
+    if t is None or isinstance(t, int):
+        return t or 0
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
+        _refuse(name, f"not {n} elements of {dtype} without gaps")
+    return t.data_ptr()
+
+
 def _stream(s) -> int:
     if s is None:
         torch = sys.modules.get("torch")
@@ -308,12 +321,20 @@ def ccl_gemm_fused_workspace(plan: Plan, splits: int = 1, *, layout: int = CCL_L
     return s.value, nbytes.value
 
 
-def _bias_type(bias, bias_type):
-    """The element type of a bias: as given, else a tensor's own (CCL_DT_FP32 for an address)."""
-    if bias_type is not None or bias is None or isinstance(bias, int):
-        return CCL_DT_FP32 if bias_type is None else bias_type
-    # -1, which the library refuses, for a tensor that is neither
-    return {"torch.float32": CCL_DT_FP32, "torch.bfloat16": CCL_DT_BF16}.get(str(bias.dtype), -1)
+def _bias(bias, bias_type, n: int) -> tuple[int, int]:
+    """Address and element type of a bias of n columns: the type as given, else a tensor's own (CCL_DT_FP32 for an
+    address). A tensor has to hold n of them side by side."""
+    if bias is None or isinstance(bias, int):
+        return bias or 0, CCL_DT_FP32 if bias_type is None else bias_type
+    own = {"torch.float32": CCL_DT_FP32, "torch.bfloat16": CCL_DT_BF16}.get(str(bias.dtype))
+    if bias_type is None:
+        bias_type = own
+    size = {CCL_DT_FP32: 4, CCL_DT_BF16: 2}.get(bias_type)
+    if size is None or (bias.dtype.is_floating_point and own != bias_type):
+        _refuse("bias", f"a tensor of {bias.dtype}; the bias must be fp32 or bf16")
+    if not bias.is_contiguous() or bias.nbytes < n * size:
+        _refuse("bias", f"not {n} elements without gaps")
+    return bias.data_ptr(), bias_type
 
 
 def ccl_gemm_fused(plan: Plan, A, B, C, *, activation: int = CCL_ACT_NONE, gated: bool = False, bias=None,
@@ -321,8 +342,9 @@ def ccl_gemm_fused(plan: Plan, A, B, C, *, activation: int = CCL_ACT_NONE, gated
                    rows: int | None = None, layout: int = CCL_LAYOUT_CCL, splits: int = 1, workspace=None,
                    workspace_bytes: int = 0, stream=None) -> None:
     """C = act(alpha A B + bias) + beta residual, gated or not; preact takes alpha A B + bias."""
-    e = _Epilogue(activation, int(gated), layout, _bias_type(bias, bias_type), alpha, beta,
-                  plan.args[0] if rows is None else rows, _ptr(bias), _ptr(residual), _ptr(preact))
+    bias, bias_type = _bias(bias, bias_type, plan.args[1])
+    e = _Epilogue(activation, int(gated), layout, bias_type, alpha, beta, plan.args[0] if rows is None else rows, bias,
+                  _ptr(residual), _ptr(preact))
     _check(library().ccl_gemm_fused(plan, ctypes.byref(e), _ptr(A), _ptr(B), _ptr(C), splits, _ptr(workspace),
                                     workspace_bytes, _stream(stream)))
 
@@ -339,8 +361,10 @@ def ccl_gemm_fused_grad(plan: Plan, A, B, preact, dZ, *, activation: int = CCL_A
                         dbias=None, alpha: float = 1.0, rows: int | None = None, layout: int = CCL_LAYOUT_CCL,
                         workspace=None, workspace_bytes: int = 0, stream=None) -> None:
     """dZ = (alpha A B) * act'(preact), gated or not; dbias takes its column sums."""
-    e = _EpilogueGrad(activation, int(gated), layout, alpha, plan.args[0] if rows is None else rows, _ptr(preact),
-                      _ptr(dbias))
+    if dbias is not None:
+        import torch
+        dbias = _whole("dbias", dbias, plan.args[1] * (2 if gated else 1), torch.float32)
+    e = _EpilogueGrad(activation, int(gated), layout, alpha, plan.args[0] if rows is None else rows, _ptr(preact), dbias)
     _check(library().ccl_gemm_fused_grad(plan, ctypes.byref(e), _ptr(A), _ptr(B), _ptr(dZ), _ptr(workspace),
                                          workspace_bytes, _stream(stream)))
 
@@ -361,10 +385,6 @@ def ccl_moe_workspace(moe: _Moe, tokens: int) -> int:
     nbytes = ctypes.c_int64(0)
     _check(library().ccl_moe_workspace(ctypes.byref(moe), tokens, ctypes.byref(nbytes)))
     return nbytes.value
-
-
-def _refuse(name: str, why: str) -> None:
-    raise CCLError(1, f"{name}: {why}")
 
 
 def _rows(name: str, t, ld, rows: int, width: int, dtype, bits=None) -> tuple[int, int]:
@@ -393,15 +413,6 @@ def _rows(name: str, t, ld, rows: int, width: int, dtype, bits=None) -> tuple[in
     if n < rows or w < width or (step != 1 and w > 1):
         _refuse(name, f"a tensor of {n} x {w} with columns {step} apart, not {rows} x {width} with columns side by side")
     return t.data_ptr(), ld if rows > 1 else width      # one row: a stride that means nothing
-
-
-def _whole(name: str, t, n: int, dtype) -> int:
-    """Address of n elements side by side."""
-    if t is None or isinstance(t, int):
-        return t or 0
-    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
-        _refuse(name, f"not {n} elements of {dtype} without gaps")
-    return t.data_ptr()
 
 
 def _expert_weights(name: str, t, experts: int, rows: int, cols: int, ld: int, stride: int, dtype) -> int:
