@@ -1,0 +1,66 @@
+"""What the FFN operators launch, asked of the library's own rules compiled for
+the host (tests/c/forms.cpp), and the cases that the parity tests run to reach
+every form. A case whose rule moves elsewhere fails the host test beside it."""
+import functools
+import os
+import pathlib
+import subprocess
+import tempfile
+
+ROOT = pathlib.Path(__file__).resolve().parent.parent
+CSRC = ROOT / "paper_2606_11718_amd" / "csrc"
+
+
+@functools.lru_cache(maxsize=None)
+def _program() -> str:
+    exe = os.path.join(tempfile.mkdtemp(prefix="ccl_forms_"), "forms")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-I", str(CSRC), "-I", str(CSRC / "host"),
+                    str(ROOT / "tests" / "c" / "forms.cpp"), str(CSRC / "host" / "plan.cpp"), "-o", exe], check=True)
+    return exe
+
+
+def ask(*question, env=None) -> dict:
+    """The form of one call: ("ortho", batch, rows, cols) and so on, as forms.cpp reads them."""
+    line = " ".join(str(int(q)) if not isinstance(q, str) else q for q in question)
+    out = subprocess.run([_program()], input=line + "\n", capture_output=True, text=True, check=True,
+                         env={**os.environ, **(env or {})}).stdout.split()
+    return {k: v if k == "kernel" else int(v) for k, v in (pair.split("=") for pair in out)}
+
+
+# ---- ccl_orthogonalize ----
+
+# (batch, rows, cols): sides off the grid of 128 and 256, wide and tall
+ORTHO = [(1, 127, 2300), (2, 2300, 128), (8, 512, 2431), (8, 2400, 500), (12, 639, 640), (8, 1020, 1024), (12, 1150, 1270),
+         (3, 4090, 1660), (8, 1024, 3840), (12, 1279, 1400), (4, 2940, 3960), (12, 1400, 1408), (8, 1408, 1400),
+         (4, 3071, 3072), (8, 1536, 1530), (4, 128, 4224), (4, 4200, 100), (2, 1150, 3710), (2, 3700, 1151), (8, 4222, 128),
+         (2, 1790, 4860), (6, 3710, 1536), (6, 512, 4300), (6, 4220, 510), (6, 2304, 2944)]
+
+
+def ortho_forms(batch, rows, cols) -> set:
+    """(product, tile, two workgroups to a CU, K ranges, ragged at the 256-row tile, tall) of its three products."""
+    f = ask("ortho", batch, rows, cols)
+    out = set()
+    for name in ("gram", "square", "update"):
+        tile, ranges, whole = f[name + "_tile"], f[name + "_ranges"], f[name + "_whole"]
+        cut = "none" if ranges == 1 else "some" if whole else "all"
+        ragged = tile == 256 and (f["pp"] % 256 != 0 or (name == "update" and f["qp"] % 256 != 0))
+        out.add((name, tile, f[name + "_paired"], cut, ragged))
+    return out
+
+
+# Every form that the rules give, and is to be run; the update's also from the
+# transpose (tall).
+ORTHO_FORMS = {
+    ("gram", 64, 0, "none", False), ("gram", 64, 0, "all", False), ("gram", 128, 0, "none", False),
+    ("gram", 128, 0, "all", False), ("gram", 128, 1, "none", False), ("gram", 128, 1, "some", False),
+    ("gram", 256, 0, "none", False), ("gram", 256, 0, "none", True), ("gram", 256, 0, "all", False),
+    ("gram", 256, 0, "all", True), ("gram", 256, 0, "some", False), ("gram", 256, 0, "some", True),
+    ("square", 64, 0, "none", False), ("square", 128, 0, "none", False), ("square", 128, 1, "none", False),
+    ("square", 128, 1, "some", False), ("square", 256, 0, "none", False), ("square", 256, 0, "none", True),
+    ("square", 256, 0, "some", False),
+    ("update", 64, 0, "none", False), ("update", 128, 0, "none", False), ("update", 128, 1, "none", False),
+    ("update", 128, 1, "some", False), ("update", 256, 0, "none", False), ("update", 256, 0, "none", True),
+    ("update", 256, 0, "some", False), ("update", 256, 0, "some", True),
+}
+ORTHO_TALL = {("update", 64, 0, "none"), ("update", 128, 0, "none"), ("update", 128, 1, "none"), ("update", 128, 1, "some"),
+              ("update", 256, 0, "none"), ("update", 256, 0, "some")}
