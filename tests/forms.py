@@ -64,3 +64,24 @@ ORTHO_FORMS = {
 }
 ORTHO_TALL = {("update", 64, 0, "none"), ("update", 128, 0, "none"), ("update", 128, 1, "none"), ("update", 128, 1, "some"),
               ("update", 256, 0, "none"), ("update", 256, 0, "some")}
+
+# ---- ccl_moe_decode ----
+
+# (tokens, hidden, ffn, experts, top_k): streaming up workgroups whose waves take
+# several chunks of K, the down product on four column tiles with many lines a
+# wave, in ranges and not, and column tiles past the last
+MOE = [(64, 6144, 1024, 30, 8), (3, 6144, 1024, 30, 8), (48, 2048, 768, 40, 8), (64, 1040, 2064, 12, 4), (17, 4112, 1200, 20, 4),
+       (2, 4112, 2064, 24, 8), (9, 528, 2064, 40, 4), (33, 16400, 512, 8, 4), (1, 8208, 1040, 9, 8), (64, 5008, 144, 512, 16)]
+
+
+def moe_form(case, fp8) -> dict:
+    """The form, with the chunks of K that a wave of the up product takes and the lines of a wave of the down product."""
+    tokens, hidden, ffn, experts, top_k = case
+    f = ask("moe", tokens, hidden, ffn, experts, top_k, fp8)
+    size = 1 if fp8 else 2
+    per = -(-(-(-hidden * size // 128)) // 8)
+    f["chunks"] = -(-per // (2 if fp8 else 4))
+    used = min(experts, tokens * top_k)
+    f["lines"] = used * -(-ffn * size // 128) / (f["ranges"] * 8)
+    f["clamped"] = f["down_tiles"] % f["down_nt"] != 0
+    return f
