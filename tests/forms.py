@@ -85,3 +85,64 @@ def moe_form(case, fp8) -> dict:
     f["lines"] = used * -(-ffn * size // 128) / (f["ranges"] * 8)
     f["clamped"] = f["down_tiles"] % f["down_nt"] != 0
     return f
+
+# ---- ccl_gemm_fused, ccl_gemm_fused_grad ----
+
+
+def _fused(M, N, K, grid_rows, rows, *, grad=False, gated=False, fp8=False, splits=1, chiplets=8, env=None, **expect):
+    return dict(M=M, N=N, K=K, grid_rows=grid_rows, rows=rows, grad=grad, gated=gated, fp8=fp8, splits=splits,
+                chiplets=chiplets, env=env or {}, expect=expect)
+
+
+def _both(*args, **more):
+    """The forward and the gradient call, plain and gated."""
+    return [_fused(*args, grad=grad, gated=gated, **more) for grad in (False, True) for gated in (False, True)]
+
+
+FUSED = (
+    # the tiles with valid rows go round all XCDs
+    _both(1024, 4224, 256, 8, 100, remap=0, kernel="gemm_kernel", tile_m=128, tile_n=128)
+    + _both(2048, 6272, 256, 8, 100, remap=0, kernel="gemm_kernel", tile_m=256, tile_n=128)
+    + _both(512, 8960, 256, 4, 100, remap=0, kernel="gemm_k64_kernel", tile_m=128, tile_n=128)
+    + _both(1024, 12544, 256, 4, 300, remap=0, kernel="gemm_k64_kernel", tile_m=256, tile_n=128)
+    + _both(512, 16896, 256, 4, 100, remap=0, kernel="gemm_k64_kernel", tile_m=128, tile_n=192, ragged=0)
+    + _both(1024, 8448, 768, 8, 129, remap=0, kernel="gemm_k64_kernel", tile_m=128, tile_n=192, ragged=1)
+    + _both(2048, 8960, 256, 4, 1025, remap=0, kernel="gemm_k64_kernel", tile_m=128, tile_n=320, ragged=0)
+    + _both(2048, 8320, 768, 8, 1025, remap=0, kernel="gemm_k64_kernel", tile_m=128, tile_n=320, ragged=1)
+    + _both(1024, 4224, 1024, 8, 100, fp8=True, remap=0, kernel="gemm_fp8s_kernel", tile_m=128, tile_n=128)
+    + _both(2048, 6272, 1024, 8, 300, fp8=True, remap=0, kernel="gemm_fp8s_kernel", tile_m=256, tile_n=128)
+    + [_fused(4096, 6400, 1024, 8, 2049, remap=0, kernel="gemm_a2_kernel"),
+       _fused(4096, 6400, 1024, 8, 2049, grad=True, remap=0, kernel="gemm_a2_kernel")]
+    + _both(4096, 6400, 1024, 8, 2049, fp8=True, remap=0, kernel="gemm_fp8p_kernel")
+    # short K: 128x128 tiles, two workgroups to a CU, in place of larger ones
+    + _both(2048, 4608, 256, 2, 1900, kernel="gemm_kernel", tile_m=128, tile_n=128, direct=1)
+    + [_fused(4096, 4096, 128, 2, 4001, kernel="gemm_kernel", tile_m=128, tile_n=128),
+       _fused(4096, 4096, 128, 2, 4001, grad=True, gated=True, kernel="gemm_kernel", tile_m=128, tile_n=128)]
+    # K ranges, whole tiles without a valid row: their partials are not written
+    + [c for rows in (0, 5, 100, 256) for c in
+       _both(256, 512, 4096, 2, rows, chiplets=4, splits=16, direct=0, own=1, ranges=16, kernel="gemm_k64_kernel")]
+    + [c for rows in (0, 5, 200) for c in
+       _both(256, 512, 4096, 2, rows, chiplets=4, splits=16, fp8=True, direct=0, own=1, ranges=8, kernel="gemm_fp8s_kernel")]
+    # the form for operands of 2 GiB and more, by way of one range's partials
+    + [c for tile in ("128x128", "256x128", "128x256") for c in
+       _both(512, 2048, 512, 1, 300, env={"CCL_GEMM_FAR": "1", "CCL_GEMM_TILE": tile}, direct=0, far=1, ranges=1)]
+    # and with K ranges
+    + _both(256, 512, 4096, 2, 100, chiplets=4, splits=16, env={"CCL_GEMM_FAR": "1"}, direct=0, far=1, ranges=16)
+)
+
+
+def fused_moved(case) -> int:
+    """Bytes of C, Z and R an element of A B, for a forward call that reads a residual and keeps Z."""
+    wide = 2 if case["gated"] else 1
+    return 4 * wide if case["grad"] else 4 // wide + 2
+
+
+def fused_form(case) -> dict:
+    c = case
+    return ask("fused", c["M"], c["N"], c["K"], c["chiplets"], c["grid_rows"], 4096, c["fp8"], 0, 16 if c["grad"] else c["splits"],
+               c["grad"], c["gated"], c["grad"], c["rows"], fused_moved(c), env=c["env"])
+
+
+def fused_name(c) -> str:
+    return "-".join([f"{c['M']}x{c['N']}x{c['K']}", "grad" if c["grad"] else "fwd"] + ["gated"] * c["gated"] + ["fp8"] * c["fp8"] +
+                    [f"rows{c['rows']}"] + [f"splits{c['splits']}"] * (c["splits"] > 1) + sorted(c["env"].values()))

@@ -1,4 +1,6 @@
 """The cases of tests/forms.py reach the forms that they are there for."""
+import pytest
+
 from tests import forms
 
 
@@ -24,3 +26,9 @@ def test_moe():
         assert any(f["ranges"] == 1 for f in wide) and any(f["ranges"] > 1 for f in wide)
         assert any(f["clamped"] for f in wide)
         assert has(up_group=1, list=1) or has(up_group=1, list=0)
+
+
+@pytest.mark.parametrize("case", forms.FUSED, ids=forms.fused_name)
+def test_fused(case):
+    form = forms.fused_form(case)
+    assert {k: form[k] for k in case["expect"]} == case["expect"]
