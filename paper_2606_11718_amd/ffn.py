@@ -71,8 +71,15 @@ class GatedFFN:
     def _empty(self, *shape, dtype=torch.bfloat16):
         return torch.empty(shape, dtype=dtype, device=self.device)
 
+    def _whole(self, name, t, cols):
+        """The products read M x cols elements side by side from t's address."""
+        if t.dtype != torch.bfloat16 or t.shape != (self.M, cols) or not t.is_contiguous():
+            raise ValueError(f"{name} has to be a contiguous bf16 tensor of {self.M} x {cols}, not {t.dtype} of "
+                             f"{tuple(t.shape)} with strides {t.stride()}")
+
     def forward(self, x, rows: int | None = None):
         """(y, h, z) of x (tokens x hidden, bf16), of which the first `rows` count."""
+        self._whole("x", x, self.D)
         z, h, y = self._empty(self.M, 2 * self.F), self._empty(self.M, self.F), self._empty(self.M, self.D)
         common = dict(layout=ROWMAJOR, rows=rows, workspace=self.ws, workspace_bytes=self.ws.numel())
         ccl.ccl_gemm_fused(self.up, x, self.w_up16, h, activation=ccl.CCL_ACT_SILU, gated=True, preact=z, **common)
@@ -100,6 +107,8 @@ class GatedFFN:
 
     def backward(self, x, h, z, dy, rows: int | None = None):
         """Gradients of W_up and W_down from the first `rows` tokens and from forward's h and z for them."""
+        for name, t, cols in (("x", x, self.D), ("h", h, self.F), ("z", z, 2 * self.F), ("dy", dy, self.D)):
+            self._whole(name, t, cols)
         x, dy = self._valid(x, rows), self._valid(dy, rows)
         dz = self._empty(self.M, 2 * self.F)
         ccl.ccl_gemm_fused_grad(self.dh, dy, self.w_down16_t, z, dz, activation=ccl.CCL_ACT_SILU, gated=True, rows=rows,
