@@ -300,7 +300,10 @@ ccl_status ccl_plan_matrix_layout(ccl_plan_t plan, int64_t cols, ccl_layout* out
  * Gated: the columns of B (and of bias and Z) alternate in groups of 16, the
  * gate columns j .. j + 15 at 2 j .. 2 j + 15 and their up columns behind
  * them, so that one tile holds both; a weight is stored so once. Everything up
- * to C is formed in fp32 and rounded to bf16 once (nearest even).
+ * to C is formed in fp32 and rounded to bf16 once (nearest even). With fp8
+ * operands, as in ccl_gemm, the matrix instruction adds eight products at a time
+ * and drops what lies more than 13 bits below the largest of them: 1.3e-5 of the
+ * sums' root mean square, whatever K (bf16: 2e-7 to 6e-7 at K 1024 to 8192).
  * Rows `rows` .. M - 1 (a ragged number of tokens in whole tiles) come out as
  * zeros in C and in preact, whatever A and R hold there.
  */
@@ -431,8 +434,8 @@ ccl_status ccl_moe_decode(const ccl_moe* moe, int64_t tokens, const void* x, int
  * The defaults (steps 5, (a, b, c) = 3.4445, -4.7750, 2.0315, eps 1e-7) bring
  * every singular value that is not tiny to around 1. The norm is summed in 64
  * bits; X, S and b S + c S S - (b + c) I are held in fp16 times 2^13 with 32-bit
- * sums, which is up to about 1.4e-3 of the result, and O is rounded to bf16
- * once. Other coefficients must keep their elements below 8 (the shift is left
+ * sums, which is 0.9e-3 to 1.7e-3 of the result (up to 2.3e-3 with fewer than 64
+ * rows or columns, 4.6e-3 with fewer than 32), and O is rounded to bf16 once. Other coefficients must keep their elements below 8 (the shift is left
  * out where |b + c| is 4 or more): past that fp16 overflows to infinity. A zero G
  * gives zeros, also with eps = 0; an infinity or a NaN in G gives NaNs in its own
  * matrix only. steps 0: the scaled G.

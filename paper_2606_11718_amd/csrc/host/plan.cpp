@@ -804,7 +804,8 @@ MoeForm moe_form(const MoeShape& s, int64_t tokens) {
   // workgroups in front that route.
   f.list = slots < s.experts;
   // Up to two tiles per CU: a workgroup each. More: workgroups that stream their
-  // tiles, about three rounds of one per CU (some find no tokens).
+  // tiles, about three per CU, of which one (bf16) or two (fp8) run at a time
+  // (some find no tokens).
   const int64_t used = f.list ? slots : s.experts;
   f.up_group = (int)std::max<int64_t>(1, used * f.up_tiles / 768);
   const int64_t groups = (f.up_tiles + f.up_group - 1) / f.up_group;

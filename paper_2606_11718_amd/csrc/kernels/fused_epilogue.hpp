@@ -16,6 +16,12 @@
 // Z kept, 8192x28672x8192, 2596 -> 2690. Reading R and Z and storing wait on memory
 // while the workgroup's matrix cores idle: short K takes tiles of which two share
 // a CU (fused_form's rule).
+//
+// On 256x256 tiles the accumulators take half of the 256 registers, and the
+// epilogue's values spill: 198 to 211 registers in the gradient kernels, nearly all
+// behind the K loop, and 11 in the pipelined fp8 forward kernel, 16 of whose 20
+// accesses lie in the K loop, where their waits drain its loads (4096x57344x8192
+// gated 1543 us, 2.49 PFLOP/s; ccl_gemm on the same kind of tiles 2.95).
 
 struct FusedEpi {
   const void* bias;         // per column of D (null: none)

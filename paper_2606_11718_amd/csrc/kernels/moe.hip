@@ -22,9 +22,10 @@
 // end. Sums over K, over experts and the softmax are fp32, in a fixed order.
 //
 // Measured, us a call: one token, 8 of 128 experts of 2048 x 768 in bf16 (75 MB)
-// 25.6: up 17, of which launch, routing and the sums about 6 and the weights 4.6
-// TB/s; down 9. 48 tokens over the same experts in fp8 (577 MB) 128, 4.5 TB/s:
-// up 84, down 43, its ranges' sum 5.
+// 25 to 26: up 17, of which launch, routing and the sums about 6 and the weights 4.6
+// TB/s; down 9, of 128 workgroups on 256 CUs; in fp8 19. 48 tokens over the same
+// experts in fp8 (577 MB) 129, 4.5 TB/s: up 84, down 44, its ranges' sum 5; in bf16
+// (1153 MB) 212, 5.4 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -252,9 +253,11 @@ __device__ __forceinline__ void staged_sync() {
 // The up launch: one workgroup per expert and group of 16-row tiles (of gate
 // and of up). The group is a stream of (tile, K chunk) steps: a step's weights
 // are loaded behind the products of the step before, ahead of its sums. A wave
-// keeps its x rows in registers where its share of K is one chunk. STREAM: one
-// workgroup to a CU (256 registers a lane: the next step's weights are in flight
-// during this one's sums). Otherwise a workgroup has one tile, and two share a CU.
+// keeps its x rows in registers where its share of K is one chunk. STREAM: a
+// workgroup takes several tiles and may use 256 registers a lane, for the next
+// step's weights in flight during this one's sums: 148 in bf16, where one workgroup
+// has a CU to itself, 113 in fp8, where two share it. Otherwise a workgroup has one
+// tile and at most 128 registers, and two share a CU.
 template <bool FP8, bool STREAM>
 __global__ void __launch_bounds__(kThreads, STREAM ? 2 : 4) moe_up_kernel(MoeParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)

@@ -14,15 +14,18 @@
 // stay below 1.3, so every element of X, S and B is below 3 and 2^13 of it
 // below fp16's 65504, while 2^13 keeps elements down to 2^-27 at full
 // precision (those of a first X of 8192 x 28672 are around 2^-14). The 11 bits
-// leave the result 0.9e-3 (wide) to 1.4e-3 (square) from the 64-bit one; bf16
-// iterates, with 8 bits, 1e-2.
+// leave the result 0.9e-3 (wide) to 1.4e-3 (square) from the 64-bit one; with few
+// singular values the roundings average out less (worst of 128 matrices: 1.7e-3 of
+// 100 x 4200 and 64 x 64, 2.3e-3 of 32 x 32, 4.6e-3 of 16 x 16). bf16 iterates, with 8
+// bits: 1e-2.
 //
-// Sides are padded with zeros to multiples of 128, which the steps keep zero.
+// Sides are padded to multiples of 128 with zeros, which the steps keep in X and S;
+// on B's padded diagonal lies s, which meets X's zeros only.
 //
 // Measured, us a call of five steps (PFLOP/s of the operations above): 768x2048
-// 132 (0.15: 17 dependent launches of 4 to 9), 16 of 2048x1536 1749 (0.83: 128x128
+// 134 (0.15: 17 dependent launches of 4 to 9), 16 of 2048x1536 1772 (0.82: 128x128
 // tiles in the symmetric products, three rounds of 256x256 in the third), 8192x28672
-// 24100 (1.31: the matrix cores at the power limit).
+// 24100 to 24900 (1.27 to 1.31: the matrix cores at the power limit).
 #include "gemm_tiles.hpp"
 
 namespace ccl {

@@ -10,8 +10,8 @@ gradient through the activation in the backward product's, weight gradients by
 ccl_gemm on packed operands, and both weights moved along their orthogonalised
 gradients. MoELayer serves experts of the same shape to a few tokens at a time.
 
-torch supplies memory, the transposed weight copies and elementwise updates;
-every product runs in the library. Operands of the epilogue calls are row-major,
+torch supplies memory, the transposed weight copies, elementwise updates and the
+router's logits; every other product runs in the library. Operands of the epilogue calls are row-major,
 weight gradients pack theirs (one from the stored transpose).
 """
 from __future__ import annotations
