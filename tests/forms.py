@@ -32,7 +32,7 @@ def ask(*question, env=None) -> dict:
 # (batch, rows, cols): sides off the grid of 128 and 256, wide and tall
 ORTHO = [(1, 127, 2300), (2, 2300, 128), (8, 512, 2431), (8, 2400, 500), (12, 639, 640), (8, 1020, 1024), (12, 1150, 1270),
          (3, 4090, 1660), (8, 1024, 3840), (12, 1279, 1400), (4, 2940, 3960), (12, 1400, 1408), (8, 1408, 1400),
-         (4, 3071, 3072), (8, 1536, 1530), (4, 128, 4224), (4, 4200, 100), (2, 1150, 3710), (2, 3700, 1151), (8, 4222, 128),
+         (4, 3300, 3328), (8, 1536, 1530), (4, 128, 4224), (4, 4200, 100), (2, 1150, 3710), (2, 3700, 1151), (8, 4222, 128),
          (2, 1790, 4860), (6, 3710, 1536), (6, 512, 4300), (6, 4220, 510), (6, 2304, 2944)]
 
 
