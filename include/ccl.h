@@ -462,6 +462,78 @@ ccl_status ccl_orthogonalize(int64_t batch, int64_t rows, int64_t cols, const vo
                              const float* coeffs, float eps, void* O, int64_t o_ld, int64_t o_stride,
                              void* workspace, int64_t workspace_bytes, void* stream);
 
+/*
+ * Experts' products for any number of tokens: rows sorted by expert, expert e's
+ * being ends[e-1] .. ends[e] - 1 (from 0 for the first), each multiplied with
+ * its expert's weight W_e, out_features x in_features (output-major, the form
+ * of ccl_moe's weights):
+ *   ccl_grouped_gemm        Z = X W_e^T;  Y = act(Z), or gated act(Zg) * Zu of
+ *                           Z's gate columns, its first half, and up columns
+ *   ccl_grouped_gemm_grad   D = dY W_e, the gradient of the product's input;
+ *                           where that was act(Z) or act(Zg) * Zu, through it:
+ *                           dZ = D * act'(Z), or dZg = D * Zu * act'(Zg) and
+ *                           dZu = D * act(Zg), gate columns first
+ *   ccl_grouped_gemm_wgrad  dW_e = dY_e^T X_e (+ dW_e); zeros for an expert
+ *                           without rows
+ * `activation` and `gated` describe the forward call's Z, or the grad call's;
+ * wgrad takes no notice of them. Sums are fp32 in a fixed order, each result is
+ * rounded once. act'(0) = 0 for CCL_ACT_RELU.
+ */
+typedef struct ccl_grouped {
+  int64_t in_features, out_features;  /* multiples of 16; gated forward:
+                                         out_features (gate and up) of 32 */
+  int32_t experts;                    /* 1..512 */
+  ccl_activation activation;
+  int32_t gated;                      /* 0 or 1 */
+  /* W and dW: elements between rows and between experts, multiples of 8; 0: no
+   * gaps. */
+  int64_t w_ld, w_stride;
+} ccl_grouped;
+
+typedef enum ccl_grouped_direction {
+  CCL_GROUPED_FORWARD = 0,
+  CCL_GROUPED_GRAD = 1,
+  CCL_GROUPED_WGRAD = 2
+} ccl_grouped_direction;
+
+/*
+ * Device workspace of such a call, and the calls. rows: rows of X, dY, Y, ...;
+ * ends: `experts` ascending row numbers on the device, of which the last may be
+ * smaller than rows: rows behind it are neither read nor written. (Numbers that
+ * do not ascend or lie outside 0 .. rows give unspecified values, never an
+ * access outside the matrices.) X, dY, Y, dX and preact are bf16 with rows *_ld
+ * apart. preact takes Z (bf16) in the forward call, or is NULL; the grad call
+ * reads it, and it is not needed (NULL) with CCL_ACT_NONE and gated = 0. Z has
+ * out_features columns forward; in the grad call it and dX have in_features,
+ * or gated twice as many. dX may be preact itself; nothing else may overlap.
+ * dW is bf16 or fp32, (experts, out_features, in_features); accumulate = 1 adds
+ * to it. Matrices and the workspace are 16-byte aligned, leading dimensions
+ * multiples of 8, at most 2^21; the workspace (NULL where none is needed) is
+ * not read on entry, and calls that share one must be ordered on one stream.
+ * No rows: nothing is launched, except that wgrad zeros dW.
+ * Errors: CCL_ERR_INVALID_ARG (NULL argument, sizes outside the ranges above or
+ * rows outside 0..2^30, an unknown activation, direction or type, gated or
+ * accumulate not 0 or 1, a leading dimension or stride smaller than what it
+ * spans, workspace missing or too small); CCL_ERR_UNSUPPORTED (a side not a
+ * multiple of 16 or above 2^20, a gated expert's weight of 2^30 elements and
+ * more, a launch too large; device not gfx950); CCL_ERR_MISALIGNED_POINTER;
+ * CCL_ERR_HIP.
+ */
+ccl_status ccl_grouped_gemm_workspace(const ccl_grouped* grouped, int64_t rows,
+                                      ccl_grouped_direction direction, int64_t* workspace_bytes);
+ccl_status ccl_grouped_gemm(const ccl_grouped* grouped, int64_t rows, const int32_t* ends,
+                            const void* X, int64_t x_ld, const void* W, void* Y, int64_t y_ld,
+                            void* preact, int64_t z_ld, void* workspace, int64_t workspace_bytes,
+                            void* stream);
+ccl_status ccl_grouped_gemm_grad(const ccl_grouped* grouped, int64_t rows, const int32_t* ends,
+                                 const void* dY, int64_t dy_ld, const void* W, void* dX,
+                                 int64_t dx_ld, const void* preact, int64_t z_ld, void* workspace,
+                                 int64_t workspace_bytes, void* stream);
+ccl_status ccl_grouped_gemm_wgrad(const ccl_grouped* grouped, int64_t rows, const int32_t* ends,
+                                  const void* dY, int64_t dy_ld, const void* X, int64_t x_ld,
+                                  void* dW, ccl_dtype dw_type, int accumulate, void* workspace,
+                                  int64_t workspace_bytes, void* stream);
+
 /* Flags of ccl_remote_bytes and ccl_remote_bytes_l2. */
 #define CCL_TRAFFIC_A_TRANS 1   /* A is stored transposed (e.g. H held for A = H^T) */
 #define CCL_TRAFFIC_B_TRANS 2   /* B is stored transposed */

@@ -29,13 +29,16 @@ HOST_FLAGS = ["-O3", "-std=c++17", "-fPIC", "-pthread", "-Wall", "-Wextra", "-I"
 SOURCES = [
     ("host/plan.cpp", "host"),       # plain C++, no HIP
     ("host/l2sim.cpp", "host"),
+    ("host/train.cpp", "host"),
     ("ccl_api.cpp", "hip"),
     ("ccl_ops.cpp", "hip"),
+    ("ccl_train.cpp", "hip"),
     ("kernels/pack.hip", "hip"),
     ("kernels/gemm.hip", "hip"),
     ("kernels/gemm_fused.hip", "hip"),
     ("kernels/moe.hip", "hip"),
     ("kernels/newton_schulz.hip", "hip"),
+    ("kernels/grouped.hip", "hip"),
 ]
 
 

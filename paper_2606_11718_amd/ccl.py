@@ -31,7 +31,9 @@ EXPORTED = ("ccl_plan", "ccl_plan_typed", "ccl_plan_destroy", "ccl_plan_grid", "
             "ccl_gemm_splitk", "ccl_gemm_splitk_noalloc", "ccl_gemm_rowmajor",
             "ccl_plan_matrix_layout", "ccl_gemm_fused_workspace", "ccl_gemm_fused", "ccl_gemm_fused_grad_workspace",
             "ccl_gemm_fused_grad", "ccl_moe_workspace", "ccl_moe_decode",
-            "ccl_orthogonalize_workspace", "ccl_orthogonalize", "ccl_remote_bytes", "ccl_remote_bytes_l2", "ccl_status_string", "ccl_last_error",
+            "ccl_orthogonalize_workspace", "ccl_orthogonalize",
+            "ccl_grouped_gemm_workspace", "ccl_grouped_gemm", "ccl_grouped_gemm_grad", "ccl_grouped_gemm_wgrad",
+            "ccl_remote_bytes", "ccl_remote_bytes_l2", "ccl_status_string", "ccl_last_error",
             "ccl_debug_tile_of_wg", "ccl_debug_gemm_config", "ccl_debug_dispatch",
             "ccl_debug_gemm_timeline", "ccl_debug_launch", "ccl_debug_launch_tile_of_wg",
             "ccl_debug_launch_dispatch", "ccl_debug_launch_timeline")
@@ -93,6 +95,12 @@ class _Moe(ctypes.Structure):
                [(n, ctypes.c_int64) for n in ("gate_up_ld", "gate_up_stride", "down_ld", "down_stride")]
 
 
+class _Grouped(ctypes.Structure):
+    _fields_ = [("in_features", ctypes.c_int64), ("out_features", ctypes.c_int64), ("experts", ctypes.c_int32),
+                ("activation", ctypes.c_int), ("gated", ctypes.c_int32), ("w_ld", ctypes.c_int64),
+                ("w_stride", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -135,6 +143,10 @@ def library() -> ctypes.CDLL:
         "ccl_orthogonalize_workspace": [i64, i64, i64, ctypes.POINTER(i64)],
         "ccl_orthogonalize": [i64, i64, i64, vp, i32, i64, i64, i32, ctypes.POINTER(ctypes.c_float), ctypes.c_float,
                               vp, i64, i64, vp, i64, vp],
+        "ccl_grouped_gemm_workspace": [ctypes.POINTER(_Grouped), i64, i32, ctypes.POINTER(i64)],
+        "ccl_grouped_gemm": [ctypes.POINTER(_Grouped), i64, vp, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp],
+        "ccl_grouped_gemm_grad": [ctypes.POINTER(_Grouped), i64, vp, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp],
+        "ccl_grouped_gemm_wgrad": [ctypes.POINTER(_Grouped), i64, vp, vp, i64, vp, i64, vp, i32, i32, vp, i64, vp],
         "ccl_remote_bytes": [vp, i32, i32, ctypes.POINTER(_Traffic)],
         "ccl_remote_bytes_l2": [vp, i32, i32, ctypes.POINTER(_L2Config), ctypes.POINTER(_L2Traffic)],
         "ccl_debug_tile_of_wg": [vp, i64, ctypes.POINTER(i32), ctypes.POINTER(i64), ctypes.POINTER(i64)],
@@ -478,6 +490,73 @@ def ccl_orthogonalize(batch: int, rows: int, cols: int, G, g_type: int, ld: int,
     _check(library().ccl_orthogonalize(batch, rows, cols, _ptr(G), g_type, ld, stride, steps, c, eps, _ptr(O), o_ld,
                                        rows * o_ld if o_stride is None else o_stride, _ptr(workspace), workspace_bytes,
                                        _stream(stream)))
+
+
+CCL_GROUPED_FORWARD, CCL_GROUPED_GRAD, CCL_GROUPED_WGRAD = 0, 1, 2
+
+
+def ccl_grouped(*, in_features: int, out_features: int, experts: int, activation: int = CCL_ACT_NONE, gated: bool = False,
+                w_ld: int = 0, w_stride: int = 0) -> _Grouped:
+    """Description of experts' products on sorted rows for the ccl_grouped_gemm calls."""
+    return _Grouped(in_features, out_features, experts, activation, int(gated), w_ld, w_stride)
+
+
+def ccl_grouped_gemm_workspace(grouped: _Grouped, rows: int, direction: int) -> int:
+    """Workspace bytes of ccl_grouped_gemm, _grad or _wgrad for `rows` rows."""
+    nbytes = ctypes.c_int64(0)
+    _check(library().ccl_grouped_gemm_workspace(ctypes.byref(grouped), rows, direction, ctypes.byref(nbytes)))
+    return nbytes.value
+
+
+def ccl_grouped_gemm(grouped: _Grouped, rows: int, ends, X, W, Y, *, preact=None, x_ld: int | None = None,
+                     y_ld: int | None = None, z_ld: int | None = None, workspace=None, workspace_bytes: int = 0,
+                     stream=None) -> None:
+    """Y = act(X W_e^T), gated or not, on rows sorted by expert; preact takes X W_e^T."""
+    call = library().ccl_grouped_gemm
+    import torch
+    bf16, bits = torch.bfloat16, torch.int16
+    K, N, E = grouped.in_features, grouped.out_features, grouped.experts
+    X, x_ld = _rows("X", X, x_ld, rows, K, bf16, bits)
+    Y, y_ld = _rows("Y", Y, y_ld, rows, N // 2 if grouped.gated else N, bf16, bits)
+    preact, z_ld = _rows("preact", preact, z_ld, rows, N, bf16, bits)
+    W = _expert_weights("W", W, E, N, K, grouped.w_ld, grouped.w_stride, bf16)
+    _check(call(ctypes.byref(grouped), rows, _whole("ends", ends, E, torch.int32), X, x_ld, W, Y, y_ld, preact, z_ld,
+                _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def ccl_grouped_gemm_grad(grouped: _Grouped, rows: int, ends, dY, W, dX, *, preact=None, dy_ld: int | None = None,
+                          dx_ld: int | None = None, z_ld: int | None = None, workspace=None, workspace_bytes: int = 0,
+                          stream=None) -> None:
+    """dX = dY W_e on rows sorted by expert, or with an activation dZ = (dY W_e) * act'(preact), gated or not."""
+    call = library().ccl_grouped_gemm_grad
+    import torch
+    bf16, bits = torch.bfloat16, torch.int16
+    K, N, E = grouped.in_features, grouped.out_features, grouped.experts
+    wide = 2 * K if grouped.gated else K
+    dY, dy_ld = _rows("dY", dY, dy_ld, rows, N, bf16, bits)
+    dX, dx_ld = _rows("dX", dX, dx_ld, rows, wide, bf16, bits)
+    preact, z_ld = _rows("preact", preact, z_ld, rows, wide, bf16, bits)
+    W = _expert_weights("W", W, E, N, K, grouped.w_ld, grouped.w_stride, bf16)
+    _check(call(ctypes.byref(grouped), rows, _whole("ends", ends, E, torch.int32), dY, dy_ld, W, dX, dx_ld, preact, z_ld,
+                _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def ccl_grouped_gemm_wgrad(grouped: _Grouped, rows: int, ends, dY, X, dW, *, dw_type: int | None = None,
+                           accumulate: bool = False, dy_ld: int | None = None, x_ld: int | None = None, workspace=None,
+                           workspace_bytes: int = 0, stream=None) -> None:
+    """dW_e = dY_e^T X_e (+ dW_e) over each expert's rows; dW's type is a tensor's own (bf16 for an address)."""
+    call = library().ccl_grouped_gemm_wgrad
+    import torch
+    bf16, bits = torch.bfloat16, torch.int16
+    K, N, E = grouped.in_features, grouped.out_features, grouped.experts
+    dY, dy_ld = _rows("dY", dY, dy_ld, rows, N, bf16, bits)
+    X, x_ld = _rows("X", X, x_ld, rows, K, bf16, bits)
+    if dw_type is None:
+        dw_type = CCL_DT_FP32 if getattr(dW, "dtype", None) is torch.float32 else CCL_DT_BF16
+    dW = _expert_weights("dW", dW, E, N, K, grouped.w_ld, grouped.w_stride,
+                         torch.float32 if dw_type == CCL_DT_FP32 else bf16)
+    _check(call(ctypes.byref(grouped), rows, _whole("ends", ends, E, torch.int32), dY, dy_ld, X, x_ld, dW, dw_type,
+                int(accumulate), _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 CCL_TRAFFIC_A_TRANS, CCL_TRAFFIC_B_TRANS, CCL_TRAFFIC_C_READ = 1, 2, 4
