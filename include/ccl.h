@@ -534,6 +534,119 @@ ccl_status ccl_grouped_gemm_wgrad(const ccl_grouped* grouped, int64_t rows, cons
                                   void* dW, ccl_dtype dw_type, int accumulate, void* workspace,
                                   int64_t workspace_bytes, void* stream);
 
+/*
+ * Softmax cross entropy over a vocabulary, from hidden states X (tokens x
+ * hidden) and the output matrix W (vocab x hidden, output-major):
+ *   z = scale X W^T;  lse = log sum_v exp(z_v);  loss = lse - z_target
+ * and its gradients for a weight g = dloss[token] * dloss_scale of each token:
+ *   dX = sum_v P_v w_v,  dW_v = sum_tokens P_v x  (+ dW_v),
+ *   P_v = g * scale * (exp(z_v - lse) - [v = target])
+ * A target outside 0 .. vocab - 1 (-100, say) marks a token that does not
+ * count: its loss is 0, its dX is 0 and it adds nothing to dW, whatever its x
+ * holds; lse is its own. A weight g of 0 is taken so too (the loss is not).
+ * The logits are never in memory: a block of `block` tokens at a time, tiles of
+ * them are reduced to fp32 maxima and sums, and where a gradient is asked for
+ * exp(z - tile maximum) is kept in bf16 for the block, 2 bytes a logit.
+ * loss and lse are fp32 of fp32 logits; P is rounded to bf16 twice on its way
+ * into the gradients' products (2^-8 relative each at most; the target's P
+ * once), whose sums are fp32 in a fixed order.
+ */
+typedef struct ccl_vocab {
+  int64_t hidden, vocab;        /* hidden: a multiple of 16 up to 2^20; vocab up to 2^20 */
+  int64_t w_ld;                 /* elements between W's rows, a multiple of 8; 0: no gaps */
+  int64_t block;                /* tokens at once, up to 32768; 0: chosen, for 4 GiB kept
+                                   at most */
+  float scale;
+} ccl_vocab;
+
+/*
+ * Device workspace of ccl_cross_entropy (grad = 0) or ccl_cross_entropy_grad
+ * (grad = 1) for `tokens` tokens, and the calls. X and dX are bf16 with rows
+ * x_ld, dx_ld apart, W bf16; targets, int64, dloss (fp32, or NULL: 1), loss and
+ * lse (fp32) have one element a token; loss or lse may be NULL (in
+ * ccl_cross_entropy not both). dX or dW may be NULL (not both) where it is not
+ * wanted. dW is bf16 or fp32 with rows dw_ld apart; accumulate = 1 adds to it.
+ * Outputs must not overlap inputs or each other. Matrices and the workspace are
+ * 16-byte aligned, leading dimensions whole 16 bytes, at most 2^21 elements; the
+ * workspace is not read on entry, and calls that share one must be ordered on
+ * one stream. No tokens: nothing is launched, except that dW is zeroed.
+ * Errors: CCL_ERR_INVALID_ARG (NULL argument, sizes outside the ranges above or
+ * tokens outside 0..2^30, a scale that is not finite, an unknown type, grad or
+ * accumulate not 0 or 1, a leading dimension smaller than its row, workspace
+ * missing or too small); CCL_ERR_UNSUPPORTED (hidden not a multiple of 16,
+ * hidden or vocab above 2^20, a launch too large; device not gfx950);
+ * CCL_ERR_MISALIGNED_POINTER; CCL_ERR_HIP.
+ */
+ccl_status ccl_cross_entropy_workspace(const ccl_vocab* vocab, int64_t tokens, int grad,
+                                       int64_t* workspace_bytes);
+ccl_status ccl_cross_entropy(const ccl_vocab* vocab, int64_t tokens, const void* X, int64_t x_ld,
+                             const void* W, const int64_t* targets, float* loss, float* lse,
+                             void* workspace, int64_t workspace_bytes, void* stream);
+ccl_status ccl_cross_entropy_grad(const ccl_vocab* vocab, int64_t tokens, const void* X,
+                                  int64_t x_ld, const void* W, const int64_t* targets,
+                                  const float* dloss, float dloss_scale, float* loss, float* lse,
+                                  void* dX, int64_t dx_ld, void* dW, int64_t dw_ld,
+                                  ccl_dtype dw_type, int accumulate, void* workspace,
+                                  int64_t workspace_bytes, void* stream);
+
+/*
+ * One AdamW step of many tensors (what ccl_orthogonalize does not train:
+ * embeddings, output matrices, routers, norms), for each element
+ *   g = grad * grad_scale;  m = beta1 m + (1 - beta1) g;
+ *   v = beta2 v + (1 - beta2) g^2;
+ *   param = param (1 - lr weight_decay)
+ *           - lr / (1 - beta1^step) m / (sqrt(v / (1 - beta2^step)) + eps)
+ * in fp32; a bf16 param is rounded to nearest, and so is `copy`, a bf16 copy of
+ * an fp32 one.
+ * Moments of 8 bits: 128 consecutive elements of a tensor share a power of two
+ * (one byte, the biased exponent of the largest |m| or v among them). exp_avg
+ * holds a sign, 4 exponent and 3 mantissa bits (bias 7), exp_avg_sq 5 and 3
+ * (bias 16), of the value times 2^(7 or 14 + 127 - the shared exponent, at least
+ * 8 or 15). They are rounded up or down at random, by a hash of the element's
+ * place in its tensor and of the step: the same call gives the same bits. A
+ * moment that is infinite or NaN is held as NaN, its neighbours are not touched.
+ * Zero bytes are moments of 0.
+ */
+typedef struct ccl_adamw {
+  double lr, beta1, beta2, eps;
+  int64_t step;                 /* counts from 1 */
+  const int64_t* step_ptr;      /* device: read in place of step, for captured calls; or NULL */
+  const float* lr_ptr;          /* device: read in place of lr; or NULL */
+  const float* grad_scale;      /* device: 1 / loss scale, a clipping factor; NULL: 1. Where it is
+                                   not finite the step is left out: nothing is written */
+} ccl_adamw;
+
+typedef struct ccl_adamw_tensor {
+  void* param;
+  const void* grad;
+  void *exp_avg, *exp_avg_sq;   /* fp32, or bytes with moment_bits 8 */
+  uint8_t *exp_avg_scale, *exp_avg_sq_scale;  /* (n + 127) / 128 bytes with moment_bits 8, else not read */
+  void* copy;                   /* bf16, or NULL */
+  int64_t n;                    /* elements, 0 .. 2^40 */
+  ccl_dtype param_type, grad_type;  /* CCL_DT_FP32 or CCL_DT_BF16 */
+  int32_t moment_bits;          /* 32 or 8 */
+  float weight_decay;
+} ccl_adamw_tensor;
+
+/*
+ * The step, of `count` tensors (an array on the host, read before the call
+ * returns), and the values that 8-bit moments stand for (m, v: n elements of
+ * fp32 or bf16, which holds them exactly while they are normal; either may be
+ * NULL). Buffers may start at any element; whole 16 bytes (8 for 8-bit moments)
+ * are faster. One launch for every 48 tensors of a kind, no workspace.
+ * Errors: CCL_ERR_INVALID_ARG (NULL argument, negative sizes or sizes above 2^40,
+ * an unknown type, moment_bits other than 8 and 32, betas outside [0, 1), eps
+ * negative or not finite, lr or weight_decay not finite, step below 1 without
+ * step_ptr, params, moments or copies that overlap); CCL_ERR_MISALIGNED_POINTER;
+ * CCL_ERR_UNSUPPORTED (ccl_adamw_moments: a launch too large; device not
+ * gfx950); CCL_ERR_HIP.
+ */
+ccl_status ccl_adamw_step(const ccl_adamw* adamw, const ccl_adamw_tensor* tensors, int64_t count,
+                          void* stream);
+ccl_status ccl_adamw_moments(int64_t n, const uint8_t* exp_avg, const uint8_t* exp_avg_scale,
+                             const uint8_t* exp_avg_sq, const uint8_t* exp_avg_sq_scale, void* m,
+                             void* v, ccl_dtype type, void* stream);
+
 /* Flags of ccl_remote_bytes and ccl_remote_bytes_l2. */
 #define CCL_TRAFFIC_A_TRANS 1   /* A is stored transposed (e.g. H held for A = H^T) */
 #define CCL_TRAFFIC_B_TRANS 2   /* B is stored transposed */

@@ -39,6 +39,8 @@ SOURCES = [
     ("kernels/moe.hip", "hip"),
     ("kernels/newton_schulz.hip", "hip"),
     ("kernels/grouped.hip", "hip"),
+    ("kernels/cross_entropy.hip", "hip"),
+    ("kernels/adamw.hip", "hip"),
 ]
 
 

@@ -33,6 +33,8 @@ EXPORTED = ("ccl_plan", "ccl_plan_typed", "ccl_plan_destroy", "ccl_plan_grid", "
             "ccl_gemm_fused_grad", "ccl_moe_workspace", "ccl_moe_decode",
             "ccl_orthogonalize_workspace", "ccl_orthogonalize",
             "ccl_grouped_gemm_workspace", "ccl_grouped_gemm", "ccl_grouped_gemm_grad", "ccl_grouped_gemm_wgrad",
+            "ccl_cross_entropy_workspace", "ccl_cross_entropy", "ccl_cross_entropy_grad",
+            "ccl_adamw_step", "ccl_adamw_moments",
             "ccl_remote_bytes", "ccl_remote_bytes_l2", "ccl_status_string", "ccl_last_error",
             "ccl_debug_tile_of_wg", "ccl_debug_gemm_config", "ccl_debug_dispatch",
             "ccl_debug_gemm_timeline", "ccl_debug_launch", "ccl_debug_launch_tile_of_wg",
@@ -101,6 +103,22 @@ class _Grouped(ctypes.Structure):
                 ("w_stride", ctypes.c_int64)]
 
 
+class _Vocab(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("hidden", "vocab", "w_ld", "block")] + [("scale", ctypes.c_float)]
+
+
+class _Adamw(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps")] + [("step", ctypes.c_int64)] + \
+               [(n, ctypes.c_void_p) for n in ("step_ptr", "lr_ptr", "grad_scale")]
+
+
+class _AdamwTensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "exp_avg", "exp_avg_sq", "exp_avg_scale",
+                                               "exp_avg_sq_scale", "copy")] + \
+               [("n", ctypes.c_int64), ("param_type", ctypes.c_int), ("grad_type", ctypes.c_int),
+                ("moment_bits", ctypes.c_int32), ("weight_decay", ctypes.c_float)]
+
+
 _lib = None
 
 
@@ -147,6 +165,12 @@ def library() -> ctypes.CDLL:
         "ccl_grouped_gemm": [ctypes.POINTER(_Grouped), i64, vp, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp],
         "ccl_grouped_gemm_grad": [ctypes.POINTER(_Grouped), i64, vp, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp],
         "ccl_grouped_gemm_wgrad": [ctypes.POINTER(_Grouped), i64, vp, vp, i64, vp, i64, vp, i32, i32, vp, i64, vp],
+        "ccl_cross_entropy_workspace": [ctypes.POINTER(_Vocab), i64, i32, ctypes.POINTER(i64)],
+        "ccl_cross_entropy": [ctypes.POINTER(_Vocab), i64, vp, i64, vp, vp, vp, vp, vp, i64, vp],
+        "ccl_cross_entropy_grad": [ctypes.POINTER(_Vocab), i64, vp, i64, vp, vp, vp, ctypes.c_float, vp, vp, vp, i64, vp, i64,
+                                   i32, i32, vp, i64, vp],
+        "ccl_adamw_step": [ctypes.POINTER(_Adamw), ctypes.POINTER(_AdamwTensor), i64, vp],
+        "ccl_adamw_moments": [i64, vp, vp, vp, vp, vp, vp, i32, vp],
         "ccl_remote_bytes": [vp, i32, i32, ctypes.POINTER(_Traffic)],
         "ccl_remote_bytes_l2": [vp, i32, i32, ctypes.POINTER(_L2Config), ctypes.POINTER(_L2Traffic)],
         "ccl_debug_tile_of_wg": [vp, i64, ctypes.POINTER(i32), ctypes.POINTER(i64), ctypes.POINTER(i64)],
@@ -557,6 +581,127 @@ def ccl_grouped_gemm_wgrad(grouped: _Grouped, rows: int, ends, dY, X, dW, *, dw_
                          torch.float32 if dw_type == CCL_DT_FP32 else bf16)
     _check(call(ctypes.byref(grouped), rows, _whole("ends", ends, E, torch.int32), dY, dy_ld, X, x_ld, dW, dw_type,
                 int(accumulate), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def ccl_vocab(*, hidden: int, vocab: int, scale: float = 1.0, w_ld: int = 0, block: int = 0) -> _Vocab:
+    """Description of an output matrix and its loss for the ccl_cross_entropy calls."""
+    return _Vocab(hidden, vocab, w_ld, block, scale)
+
+
+def ccl_cross_entropy_workspace(vocab: _Vocab, tokens: int, *, grad: bool = False) -> int:
+    """Workspace bytes of ccl_cross_entropy, or with grad of ccl_cross_entropy_grad."""
+    nbytes = ctypes.c_int64(0)
+    _check(library().ccl_cross_entropy_workspace(ctypes.byref(vocab), tokens, int(grad), ctypes.byref(nbytes)))
+    return nbytes.value
+
+
+def _vocab_weight(vocab: _Vocab, W, bf16) -> int:
+    """Address of W, vocab x hidden with its rows as the description says."""
+    W, ld = _rows("W", W, vocab.w_ld if W is None or isinstance(W, int) else None, vocab.vocab, vocab.hidden, bf16)
+    if ld != (vocab.w_ld or vocab.hidden) and vocab.vocab > 1 and ld != 0:
+        _refuse("W", f"rows {ld} apart, not {vocab.w_ld or vocab.hidden}")
+    return W
+
+
+def ccl_cross_entropy(vocab: _Vocab, tokens: int, X, W, targets, loss, *, lse=None, x_ld: int | None = None,
+                      workspace=None, workspace_bytes: int = 0, stream=None) -> None:
+    """loss = log sum exp(scale X W^T) - the target's logit, one fp32 a token (0 without a target); lse takes the first term."""
+    call = library().ccl_cross_entropy
+    import torch
+    bf16, f32 = torch.bfloat16, torch.float32
+    X, x_ld = _rows("X", X, x_ld, tokens, vocab.hidden, bf16, torch.int16)
+    _check(call(ctypes.byref(vocab), tokens, X, x_ld, _vocab_weight(vocab, W, bf16),
+                _whole("targets", targets, tokens, torch.int64), _whole("loss", loss, tokens, f32),
+                _whole("lse", lse, tokens, f32), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def ccl_cross_entropy_grad(vocab: _Vocab, tokens: int, X, W, targets, loss, dX, dW, *, lse=None, dloss=None,
+                           dloss_scale: float = 1.0, dw_type: int | None = None, accumulate: bool = False,
+                           x_ld: int | None = None, dx_ld: int | None = None, dw_ld: int | None = None, workspace=None,
+                           workspace_bytes: int = 0, stream=None) -> None:
+    """The loss and its gradients for token weights dloss * dloss_scale, dX and dW (either may be None); dW's type is a
+    tensor's own (bf16 for an address)."""
+    call = library().ccl_cross_entropy_grad
+    import torch
+    bf16, f32 = torch.bfloat16, torch.float32
+    if dw_type is None:
+        dw_type = CCL_DT_FP32 if getattr(dW, "dtype", None) is f32 else CCL_DT_BF16
+    D = vocab.hidden
+    X, x_ld = _rows("X", X, x_ld, tokens, D, bf16, torch.int16)
+    dX, dx_ld = _rows("dX", dX, dx_ld, tokens, D, bf16, torch.int16)
+    dW, dw_ld = _rows("dW", dW, dw_ld, vocab.vocab, D, f32 if dw_type == CCL_DT_FP32 else bf16)
+    _check(call(ctypes.byref(vocab), tokens, X, x_ld, _vocab_weight(vocab, W, bf16),
+                _whole("targets", targets, tokens, torch.int64), _whole("dloss", dloss, tokens, f32), dloss_scale,
+                _whole("loss", loss, tokens, f32), _whole("lse", lse, tokens, f32), dX, dx_ld, dW, dw_ld, dw_type,
+                int(accumulate), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+CCL_ADAMW_BLOCK = 128               # elements of 8-bit moments that share a scale
+
+
+def ccl_adamw_tensor(param, grad, exp_avg, exp_avg_sq, *, exp_avg_scale=None, exp_avg_sq_scale=None, copy=None,
+                     weight_decay: float = 0.0) -> tuple[_AdamwTensor, tuple]:
+    """One tensor of a ccl_adamw set: contiguous tensors of as many elements; uint8 moments (with their scales, one byte
+    for every 128) are 8-bit ones. The set keeps the tensors alive."""
+    import torch
+    types = {torch.float32: CCL_DT_FP32, torch.bfloat16: CCL_DT_BF16}
+    n = param.numel()
+    for name, t in (("param", param), ("grad", grad)):
+        if t.dtype not in types:
+            _refuse(name, f"a tensor of {t.dtype}, not fp32 or bf16")
+    bits = 8 if exp_avg.dtype is torch.uint8 else 32
+    moment = torch.uint8 if bits == 8 else torch.float32
+    blocks = -(-n // CCL_ADAMW_BLOCK)
+
+    def exact(name, t, count, dtype):
+        if t is not None and t.numel() != count:
+            _refuse(name, f"{t.numel()} elements, not {count}")
+        return _whole(name, t, count, dtype)
+    scales = (exact("exp_avg_scale", exp_avg_scale, blocks, torch.uint8),
+              exact("exp_avg_sq_scale", exp_avg_sq_scale, blocks, torch.uint8)) if bits == 8 else (0, 0)
+    t = _AdamwTensor(exact("param", param, n, param.dtype), exact("grad", grad, n, grad.dtype),
+                     exact("exp_avg", exp_avg, n, moment), exact("exp_avg_sq", exp_avg_sq, n, moment), *scales,
+                     exact("copy", copy, n, torch.bfloat16), n, types[param.dtype], types[grad.dtype], bits, weight_decay)
+    return t, (param, grad, exp_avg, exp_avg_sq, exp_avg_scale, exp_avg_sq_scale, copy)
+
+
+class AdamwSet:
+    """Tensors for ccl_adamw_step, held while it lives."""
+
+    def __init__(self, tensors):
+        tensors = list(tensors)
+        self.tensors = (_AdamwTensor * len(tensors))(*(t for t, _ in tensors))
+        self.kept = [held for _, held in tensors]
+
+
+def ccl_adamw(tensors) -> AdamwSet:
+    """A set of ccl_adamw_tensor to step together."""
+    return AdamwSet(tensors)
+
+
+def ccl_adamw_step(tensors: AdamwSet, *, lr: float, step: int = 0, beta1: float = 0.9, beta2: float = 0.999,
+                   eps: float = 1e-8, step_ptr=None, lr_ptr=None, grad_scale=None, stream=None) -> None:
+    """One AdamW step of the set; step counts from 1. step_ptr (int64), lr_ptr and grad_scale (fp32): one element on the
+    device, read when the step runs."""
+    call = library().ccl_adamw_step
+    import torch
+    a = _Adamw(lr, beta1, beta2, eps, step, _whole("step_ptr", step_ptr, 1, torch.int64),
+               _whole("lr_ptr", lr_ptr, 1, torch.float32), _whole("grad_scale", grad_scale, 1, torch.float32))
+    _check(call(ctypes.byref(a), tensors.tensors, len(tensors.tensors), _stream(stream)))
+
+
+def ccl_adamw_moments(n: int, exp_avg, exp_avg_scale, exp_avg_sq, exp_avg_sq_scale, m, v, *, stream=None) -> None:
+    """The values of n 8-bit moments, to m and v (fp32 or bf16 tensors of one type; either may be None)."""
+    call = library().ccl_adamw_moments
+    import torch
+    u8, blocks = torch.uint8, -(-n // CCL_ADAMW_BLOCK)
+    dtype = next((t.dtype for t in (m, v) if t is not None), torch.float32)
+    if dtype not in (torch.float32, torch.bfloat16):
+        _refuse("m and v", f"tensors of {dtype}, not fp32 or bf16")
+    _check(call(n, _whole("exp_avg", exp_avg, n, u8), _whole("exp_avg_scale", exp_avg_scale, blocks, u8),
+                _whole("exp_avg_sq", exp_avg_sq, n, u8), _whole("exp_avg_sq_scale", exp_avg_sq_scale, blocks, u8),
+                _whole("m", m, n, dtype), _whole("v", v, n, dtype), CCL_DT_BF16 if dtype is torch.bfloat16 else CCL_DT_FP32,
+                _stream(stream)))
 
 
 CCL_TRAFFIC_A_TRANS, CCL_TRAFFIC_B_TRANS, CCL_TRAFFIC_C_READ = 1, 2, 4

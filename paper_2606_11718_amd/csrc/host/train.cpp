@@ -31,4 +31,78 @@ GroupedForm grouped_form(const GroupedShape& s, int64_t rows, int direction) {
   return f;
 }
 
+namespace {
+
+constexpr int64_t kKeptBytes = (int64_t)4 << 30;   // of exp(z - tile max) at once
+constexpr int64_t kLossBlock = 16384;              // tokens at once at most
+
+ProductForm product_form(int64_t m, int64_t n, int tile_m, int tile_n, int64_t ksteps, int splits) {
+  ProductForm f;
+  f.tile_m = tile_m;
+  f.tile_n = tile_n;
+  f.tiles_m = (int32_t)up(m, tile_m);
+  f.tiles_n = (int32_t)up(n, tile_n);
+  f.group = 8;
+  f.chunk = 32;
+  f.ksplit = (int32_t)up(ksteps, splits);
+  f.splits = (int32_t)up(ksteps, f.ksplit);
+  f.workgroups = dealt((int64_t)f.tiles_m * f.tiles_n * f.splits, f.chunk);
+  return f;
+}
+
+}  // namespace
+
+ProductForm vocab_logits_form(const VocabShape& s, int64_t tokens) {
+  return product_form(tokens, s.vocab, tokens <= 64 ? 64 : 128, 128, up(s.hidden, 64), 1);
+}
+
+ProductForm vocab_dx_form(const VocabShape& s, int64_t tokens) {
+  const int tile_m = tokens <= 64 ? 64 : 128;
+  const int64_t tiles = up(tokens, tile_m) * up(s.hidden, 128);
+  const int64_t splits = tiles >= 512 ? 1 : std::min<int64_t>(std::min<int64_t>(up(512, tiles), 64), up(s.vocab, 1024));
+  return product_form(tokens, s.hidden, tile_m, 128, up(s.vocab, 64), (int)splits);
+}
+
+ProductForm vocab_dw_form(const VocabShape& s, int64_t tokens) {
+  return product_form(s.vocab, s.hidden, 128, 128, up(tokens, 64), 1);
+}
+
+VocabForm vocab_form(const VocabShape& s, int64_t tokens, bool grad) {
+  VocabForm f;
+  f.e_cols = (int32_t)(up(s.vocab, 64) * 64);
+  f.e_ld = f.e_cols + 64;      // rows a power of two apart would share memory channels
+  int64_t most = s.block ? s.block : kLossBlock;
+  if (!s.block && grad) most = std::min(most, std::max<int64_t>(256, kKeptBytes / (2 * f.e_ld) / 256 * 256));
+  f.blocks = std::max<int64_t>(1, up(tokens, most));
+  f.block = s.block ? std::min(s.block, tokens) : std::min(tokens, up(up(tokens, f.blocks), 256) * 256);
+  f.blocks = f.block ? up(tokens, f.block) : 0;
+  const ProductForm z = vocab_logits_form(s, f.block);
+  f.tile_n = z.tile_n;
+  f.tiles_n = z.tiles_n;
+  int64_t at = 0;
+  const auto take = [&](int64_t bytes) {
+    const int64_t here = at;
+    at += up(bytes, 256) * 256;
+    return here;
+  };
+  f.target_at = take(4 * f.block);
+  f.factor_at = take(8 * f.block);
+  f.stat_at = take(8 * f.block * f.tiles_n);
+  if (grad) {
+    f.e_at = take(2 * f.block * f.e_ld);
+    f.rows_at = take(2 * f.block * s.hidden);
+    // the last block may be cut into more ranges than the others
+    int64_t part = 0;
+    for (int64_t t : {f.block, tokens - (f.blocks - 1) * f.block})
+      if (t > 0) {
+        const ProductForm d = vocab_dx_form(s, t);
+        if (d.splits > 1) part = std::max(part, 4 * d.splits * t * s.hidden);
+      }
+    f.part_at = take(part);
+    f.sum_at = take(f.blocks > 1 ? 4 * s.vocab * s.hidden : 0);
+  }
+  f.workspace_bytes = at;
+  return f;
+}
+
 }  // namespace ccl

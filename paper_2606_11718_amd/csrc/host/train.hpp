@@ -23,4 +23,54 @@ struct GroupedForm {
 };
 GroupedForm grouped_form(const GroupedShape& s, int64_t rows, int direction);
 
+// ---- vocabulary loss ----
+constexpr int64_t kVocabMaxBlock = 32768;     // the scaling pass has a grid row a token
+struct VocabShape {
+  int64_t hidden = 0, vocab = 0, w_ld = 0;
+  int64_t block = 0;                          // tokens at once, 0: chosen
+  float scale = 1.f;
+};
+// A product's tiles of one kind, dealt to the XCDs in a raster of `group` tile
+// rows, and its K ranges.
+struct ProductForm {
+  int tile_m = 0, tile_n = 0;
+  int32_t tiles_m = 0, tiles_n = 0, group = 1, chunk = 1;
+  int32_t splits = 1, ksplit = 0;             // ksplit: stages of 64 K a range
+  int64_t workgroups = 0;
+};
+struct VocabForm {
+  int64_t block = 0, blocks = 0;              // tokens at once (the last block may have fewer)
+  int64_t e_ld = 0;                           // elements between rows of exp(z - tile max)
+  int32_t e_cols = 0;                         // of which whole 64s are used
+  int tile_n = 0;                             // columns that share a maximum
+  int32_t tiles_n = 0;
+  // bytes into the workspace
+  int64_t target_at = 0, factor_at = 0, stat_at = 0, e_at = 0, rows_at = 0, part_at = 0, sum_at = 0, workspace_bytes = 0;
+};
+// The blocks and the workspace; grad: with exp(z - tile max) kept for a block,
+// a copy of its x,
+// the ranges' partial dX and, where dW is rounded after several blocks, its fp32 sum.
+VocabForm vocab_form(const VocabShape& s, int64_t tokens, bool grad);
+// The products of a block of `tokens`: logits, dX, dW.
+ProductForm vocab_logits_form(const VocabShape& s, int64_t tokens);
+ProductForm vocab_dx_form(const VocabShape& s, int64_t tokens);
+ProductForm vocab_dw_form(const VocabShape& s, int64_t tokens);
+
+// ---- AdamW ----
+constexpr int kAdamwTensors = 48;             // of a launch: their table is a kernel argument of 4 KB at most
+constexpr int kAdamwBlock = 128;              // elements of 8-bit moments that share a scale
+constexpr int64_t kAdamwChunk = 8192;         // elements of a workgroup
+
+// 1 - beta^step and its like, the same bits on the host and the device: by
+// squaring, in double.
+#if defined(__HIPCC__)
+__host__ __device__
+#endif
+inline double power_of(double beta, int64_t step) {
+  double p = 1.0;
+  for (double b = beta; step > 0; step >>= 1, b *= b)
+    if (step & 1) p *= b;
+  return p;
+}
+
 }  // namespace ccl

@@ -26,14 +26,6 @@ struct GroupedParams {
   int32_t act, f32, accumulate;
 };
 
-// Tiles are dealt to the XCDs (workgroup mod 8) in runs of chunk, so that what
-// runs on one XCD together shares operands in its L2 and uneven experts spread.
-__device__ __forceinline__ int64_t dealt_tile(int32_t chunk) {
-  const uint32_t xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
-  const uint32_t run = slot / (uint32_t)chunk;
-  return ((int64_t)run * 8 + xcd) * chunk + (slot - run * chunk);
-}
-
 // Rows of expert e; whatever ends holds, within 0 .. rows.
 __device__ __forceinline__ void expert_rows(const GroupedParams& p, int e, int32_t* first, int32_t* n) {
   const int32_t lo = e ? min(max(p.ends[e - 1], 0), p.rows) : 0, hi = min(max(p.ends[e], 0), p.rows);
@@ -83,56 +75,6 @@ __device__ __forceinline__ bool row_tile(const GroupedParams& p, int64_t id, int
   t->rows = __builtin_amdgcn_readfirstlane(min(BM, sh[12] - ti * BM));
   t->tj = __builtin_amdgcn_readfirstlane(tj);
   return true;
-}
-
-// The staged tile's rows < rows and chunks with col(chunk) >= 0 to m.
-template <int ROWS, int COLS, int THREADS, typename Col>
-__device__ __forceinline__ void tile_out(const StagedTile<ROWS, COLS>& t, uint16_t* m, int64_t ld, int32_t rows, int tid,
-                                         Col&& col) {
-  constexpr int CPR = COLS / 8;
-#pragma unroll 4
-  for (int i = 0; i < ROWS * CPR / THREADS; ++i) {
-    const int at = i * THREADS + tid, r = at / CPR, c = at % CPR;
-    const uint4 v = *reinterpret_cast<const uint4*>(t.chunk(r, c));
-    const int32_t to = col(c);
-    if (r < rows && to >= 0) *reinterpret_cast<uint4*>(m + r * ld + to) = v;
-  }
-}
-
-template <int ROWS, int COLS, int THREADS, typename Col>
-__device__ __forceinline__ void tile_in(const StagedTile<ROWS, COLS>& t, const uint16_t* m, int64_t ld, int32_t rows, int tid,
-                                        Col&& col) {
-  constexpr int CPR = COLS / 8, N = ROWS * CPR / THREADS, B = N < 8 ? N : 8;
-  for (int i = 0; i < N; i += B) {
-    uint4 v[B];
-#pragma unroll
-    for (int j = 0; j < B; ++j) {
-      const int at = (i + j) * THREADS + tid, r = at / CPR;
-      const int32_t from = col(at % CPR);
-      v[j] = make_uint4(0, 0, 0, 0);
-      if (r < rows && from >= 0) v[j] = *reinterpret_cast<const uint4*>(m + r * ld + from);
-    }
-#pragma unroll
-    for (int j = 0; j < B; ++j) {
-      const int at = (i + j) * THREADS + tid;
-      *reinterpret_cast<uint4*>(t.chunk(at / CPR, at % CPR)) = v[j];
-    }
-  }
-}
-
-// A tile's values in a lane's order: f(mt, nt, row, column of its four).
-template <typename T, typename F>
-__device__ __forceinline__ void each4(int tid, F&& f) {
-  const int lane = tid & 63, wave = tid >> 6, wm = wave / T::WGN, wn = wave % T::WGN;
-#pragma unroll
-  for (int mt = 0; mt < T::TM; ++mt)
-#pragma unroll
-    for (int nt = 0; nt < T::TN; ++nt) f(mt, nt, wm * T::WM + 16 * mt + (lane & 15), wn * T::WN + 16 * nt + 4 * (lane >> 4));
-}
-
-template <int BM, int BN>
-__device__ __forceinline__ StagedTile<BM, BN> staged(char* sm) {
-  return StagedTile<BM, BN>{sm, sm + BM / 2 * BN * 2};
 }
 
 // Y (and Z) of a tile. A gated tile's columns alternate in groups of 16, gate
