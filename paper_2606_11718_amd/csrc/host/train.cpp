@@ -52,11 +52,18 @@ ProductForm product_form(int64_t m, int64_t n, int tile_m, int tile_n, int64_t k
 
 }  // namespace
 
+// 256x256 tiles where they are not mostly padding and fill the CUs.
+bool large_tiles(int64_t m, int64_t n, int splits = 1) {
+  return up(m, 256) * 256 <= up(m, 128) * 128 * 5 / 4 && up(m, 256) * up(n, 256) * splits >= 256;
+}
+
 ProductForm vocab_logits_form(const VocabShape& s, int64_t tokens) {
+  if (large_tiles(tokens, s.vocab)) return product_form(tokens, s.vocab, 256, 256, up(s.hidden, 64), 1);
   return product_form(tokens, s.vocab, tokens <= 64 ? 64 : 128, 128, up(s.hidden, 64), 1);
 }
 
 ProductForm vocab_dx_form(const VocabShape& s, int64_t tokens) {
+  if (large_tiles(tokens, s.hidden)) return product_form(tokens, s.hidden, 256, 256, up(s.vocab, 64), 1);
   const int tile_m = tokens <= 64 ? 64 : 128;
   const int64_t tiles = up(tokens, tile_m) * up(s.hidden, 128);
   const int64_t splits = tiles >= 512 ? 1 : std::min<int64_t>(std::min<int64_t>(up(512, tiles), 64), up(s.vocab, 1024));
@@ -64,6 +71,7 @@ ProductForm vocab_dx_form(const VocabShape& s, int64_t tokens) {
 }
 
 ProductForm vocab_dw_form(const VocabShape& s, int64_t tokens) {
+  if (large_tiles(s.vocab, s.hidden)) return product_form(s.vocab, s.hidden, 256, 256, up(tokens, 64), 1);
   return product_form(s.vocab, s.hidden, 128, 128, up(tokens, 64), 1);
 }
 
@@ -76,9 +84,6 @@ VocabForm vocab_form(const VocabShape& s, int64_t tokens, bool grad) {
   f.blocks = std::max<int64_t>(1, up(tokens, most));
   f.block = s.block ? std::min(s.block, tokens) : std::min(tokens, up(up(tokens, f.blocks), 256) * 256);
   f.blocks = f.block ? up(tokens, f.block) : 0;
-  const ProductForm z = vocab_logits_form(s, f.block);
-  f.tile_n = z.tile_n;
-  f.tiles_n = z.tiles_n;
   int64_t at = 0;
   const auto take = [&](int64_t bytes) {
     const int64_t here = at;
@@ -87,7 +92,7 @@ VocabForm vocab_form(const VocabShape& s, int64_t tokens, bool grad) {
   };
   f.target_at = take(4 * f.block);
   f.factor_at = take(8 * f.block);
-  f.stat_at = take(8 * f.block * f.tiles_n);
+  f.stat_at = take(8 * f.block * up(s.vocab, 128));      // the narrowest tiles'
   if (grad) {
     f.e_at = take(2 * f.block * f.e_ld);
     f.rows_at = take(2 * f.block * s.hidden);

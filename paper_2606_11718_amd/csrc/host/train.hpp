@@ -42,8 +42,6 @@ struct VocabForm {
   int64_t block = 0, blocks = 0;              // tokens at once (the last block may have fewer)
   int64_t e_ld = 0;                           // elements between rows of exp(z - tile max)
   int32_t e_cols = 0;                         // of which whole 64s are used
-  int tile_n = 0;                             // columns that share a maximum
-  int32_t tiles_n = 0;
   // bytes into the workspace
   int64_t target_at = 0, factor_at = 0, stat_at = 0, e_at = 0, rows_at = 0, part_at = 0, sum_at = 0, workspace_bytes = 0;
 };

@@ -310,6 +310,7 @@ hipError_t launch_plain(const ProductForm& f, PlainParams p, hipStream_t stream)
   p.ksplit = f.ksplit;
   const dim3 grid((unsigned)f.workgroups), block(512);
   if (f.tile_m == 64) hipLaunchKernelGGL((plain_kernel<64, 128, 2, 4, UK, VK>), grid, block, 0, stream, p);
+  else if (f.tile_m == 256) hipLaunchKernelGGL((plain_kernel<256, 256, 2, 4, UK, VK>), grid, block, 0, stream, p);
   else hipLaunchKernelGGL((plain_kernel<128, 128, 2, 4, UK, VK>), grid, block, 0, stream, p);
   return hipGetLastError();
 }
@@ -359,6 +360,7 @@ hipError_t launch_cross_entropy(const VocabShape& s, const VocabCall& c, void* w
     lp.scale = s.scale;
     const dim3 grid((unsigned)z.workgroups);
     if (z.tile_m == 64) hipLaunchKernelGGL((logits_kernel<64, 128, 2, 4>), grid, dim3(512), 0, stream, lp);
+    else if (z.tile_m == 256) hipLaunchKernelGGL((logits_kernel<256, 256, 2, 4>), grid, dim3(512), 0, stream, lp);
     else hipLaunchKernelGGL((logits_kernel<128, 128, 2, 4>), grid, dim3(512), 0, stream, lp);
     if (hipError_t e = hipGetLastError()) return e;
     CombineParams cp{};

@@ -12,8 +12,8 @@
 //
 // Bounds: rows past a KC side's extent and K rows past its end come from
 // outside the descriptor and read as zeros (its length is set stage by stage,
-// so the operands may be of any size), chunks of a KC row past K are sent past
-// it too. Columns past an RC side's extent hold other values of the matrix, but
+// so the operands may be of any size); chunks of a KC row past K, in a last
+// part of a stage, are sent past it too. Columns past an RC side's extent hold other values of the matrix, but
 // reach only rows or columns of D that are not stored.
 #pragma once
 
@@ -63,7 +63,7 @@ struct SideLoads {
   int64_t step;            // bytes from one stage to the next
   int64_t ld2;             // bytes between rows
   int32_t extent, left;    // left: K from the next stage on
-  int wave, lane;
+  int wave;
 
   __device__ __forceinline__ static int row(int wave, int lane, int i) {
     return KC ? 8 * (wave * N + i) + (lane >> 3) : RPI * (wave * N + i) + lane / CPR;
@@ -72,11 +72,11 @@ struct SideLoads {
     const int r = row(wave, lane, i);
     return KC ? (lane & 7) ^ swz_a64(r) : (lane % CPR) ^ swz_bn<B>(r);
   }
-  // map: the memory row of a KC tile row.
+  // map: the memory row of a KC tile row. chunks: of a KC stage row that exist,
+  // the others are sent past everything.
   template <typename Map>
-  __device__ __forceinline__ void init(const Side& s, int32_t k0, int w, int l, Map&& map) {
+  __device__ __forceinline__ void init(const Side& s, int32_t k0, int w, int l, Map&& map, int chunks = 8) {
     wave = w;
-    lane = l;
     ld2 = s.ld * 2;
     extent = s.extent;
     left = s.k - k0;
@@ -84,8 +84,9 @@ struct SideLoads {
     at = reinterpret_cast<uint64_t>(s.base) + (KC ? (int64_t)k0 * 2 : (int64_t)k0 * ld2) - kShift;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int r = row(w, l, i);
-      voff[i] = (uint32_t)((KC ? map(r) : r) * ld2) + chunk(w, l, i) * 16u + kShift - 1024u * i;
+      const int r = row(w, l, i), c = chunk(w, l, i);
+      voff[i] = (uint32_t)((KC ? map(r) : r) * ld2) + c * 16u + kShift - 1024u * i;
+      if (KC && c >= chunks) voff[i] = 0x80000000u;
     }
   }
   // The descriptor of the next stage (of no memory past the last).
@@ -93,14 +94,7 @@ struct SideLoads {
     int32_t bytes = 0;
     if (left > 0) {
       const int32_t k = min(left, 64);
-      bytes = KC ? (int32_t)((extent - 1) * ld2) + 2 * k : (int32_t)((k - 1) * ld2) + 2 * extent;
-      bytes += kShift;
-      if (KC && left < 64) {
-        // the last stage, of fewer K: the other chunks of a row lie past everything
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-          if (8 * chunk(wave, lane, i) >= left) voff[i] = 0x80000000u;
-      }
+      bytes = (KC ? (int32_t)((extent - 1) * ld2) + 2 * k : (int32_t)((k - 1) * ld2) + 2 * extent) + (int32_t)kShift;
     }
     i32x4 d;
     d[0] = (int)(uint32_t)at;
@@ -116,141 +110,195 @@ struct SideLoads {
   }
 };
 
-// The fragments of one side in a stage's half kk: 16 x 32 tiles, lane l with
-// row l % 16 and K 8 (l / 16) .. + 7.
-template <int B, bool KC, int T, int W>
-struct SideFrags {
-  static constexpr int READS = KC ? T : 2 * T;
-  bf16x8 k[KC ? T : 1];
-  i16x4 r[KC ? 1 : T][2];
-  // Byte offset of the wave's first tile; w0: the wave's first row or column.
-  __device__ __forceinline__ static int32_t first(int w0, int lane) {
+// A fragment of one side in a stage's half kk: 16 x 32 of a wave's T tiles, lane l
+// with row l % 16 and K 8 (l / 16) .. + 7.
+template <int B, bool KC, int T>
+struct SideFrag {
+  static constexpr int READS = KC ? 1 : 2;
+  bf16x8 k;
+  i16x4 r[2];
+  // Addresses that its reads start from, the rest being constants: KC: of the
+  // halves (half 1 of a row is the chunk with bit 2 flipped); RC: of the tiles (a
+  // tile's columns start 32 bytes after the last one's, below the wave's width, so
+  // its chunk is the first tile's XOR that; rows 4 on have the same swizzle). Kept
+  // from the compiler, which would form and spill one for every read.
+  static constexpr int NA = KC ? 2 : T;
+  static_assert(KC || (T & (T - 1)) == 0, "the wave's columns start at a multiple of their number");
+  // w0: the wave's first row or column.
+  __device__ __forceinline__ static void addresses(const char* lds, int w0, int lane, uint32_t (&at)[NA]) {
+    uint32_t first;
     if constexpr (KC) {
       const int row = w0 + (lane & 15);
-      return row * 128 + (((lane >> 4) ^ swz_a64(row)) * 16);
+      first = row * 128 + (((lane >> 4) ^ swz_a64(row)) * 16);
     } else {
       const int g = lane >> 4, s = lane & 15, krow = 8 * g + (s >> 2), col = w0 + 4 * (s & 3);
-      return krow * (B * 2) + (((col >> 3) ^ swz_bn<B>(krow)) * 16) + ((col >> 2) & 1) * 8;
+      first = krow * (B * 2) + (((col >> 3) ^ swz_bn<B>(krow)) * 16) + ((col >> 2) & 1) * 8;
+    }
+#pragma unroll
+    for (int i = 0; i < NA; ++i) {
+      at[i] = (uint32_t)(uintptr_t)(const lds_char*)lds + (first ^ (KC ? i * 64 : i * 32));
+      asm volatile("" : "+v"(at[i]));
     }
   }
-  // Read i of READS. KC: half kk of a row is the chunk with bit 2 flipped. RC:
-  // a tile's columns start 32 bytes after the last one's, below the wave's
-  // width, so its chunk is the first tile's XOR that; rows 4 on have the same
-  // swizzle.
-  __device__ __forceinline__ void read(const char* lds, int32_t first, int kk, int i) {
+  // Read h of tile t, in the stage buffer `stage` bytes on.
+  __device__ __forceinline__ void read(const uint32_t (&at)[NA], int stage, int kk, int t, int h) {
     if constexpr (KC) {
-      k[i] = *(const lds_bf16x8*)(lds + (first ^ (kk * 64)) + i * 16 * 128);
+      k = *(const lds_bf16x8*)(uintptr_t)(at[kk] + stage + t * 16 * 128);
     } else {
-      static_assert((W & (W - 1)) == 0, "the wave's columns start at a multiple of their number");
-      const int t = i >> 1, h = i & 1;
-      r[t][h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (lds_i16x4*)(lds + (first ^ (t * 32)) + h * 4 * B * 2 + kk * 32 * B * 2));
+      r[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (lds_i16x4*)(uintptr_t)(at[t] + stage + h * 4 * B * 2 + kk * 32 * B * 2));
     }
   }
-  __device__ __forceinline__ bf16x8 get(int t) const {
-    if constexpr (KC) return k[t];
-    else return __builtin_bit_cast(bf16x8, __builtin_shufflevector(r[t][0], r[t][1], 0, 1, 2, 3, 4, 5, 6, 7));
+  __device__ __forceinline__ bf16x8 get() const {
+    if constexpr (KC) return k;
+    else return __builtin_bit_cast(bf16x8, __builtin_shufflevector(r[0], r[1], 0, 1, 2, 3, 4, 5, 6, 7));
   }
 };
 
 #if defined(__HIP_DEVICE_COMPILE__)
-// acc = U V' over K [k0, ...) of ksteps stages of 64 (at least one). sm: T::LDS
-// bytes, 1024-byte aligned, free when this returns. vmap: the memory row of a
-// KC V tile row.
+// acc = U V' over K [k0, ...) of ksteps stages of 64 (at least one), the last of
+// which may be part of one. sm: T::LDS bytes, 1024-byte aligned, free when this
+// returns. vmap: the memory row of a KC V tile row.
+//
+// A half's MFMAs go tile row by tile row of U: as soon as a row's are issued, its
+// fragment's registers take the next half's. The last two rows and V have two
+// sets, read first, so that every read of a stage is a good part of a half old at
+// the barrier (whole second sets of U too would not fit beside a 256x256 tile's
+// accumulators).
 template <typename T, typename VMap>
-__device__ __forceinline__ void product(const Side& u, const Side& v, int32_t k0, int32_t ksteps,
-                                        f32x4 (&acc)[T::TM][T::TN], char* sm, int tid, VMap&& vmap) {
-  constexpr int NS = T::NS;
+__device__ __forceinline__ void product(Side u, Side v, int32_t k0, int32_t ksteps, f32x4 (&acc)[T::TM][T::TN], char* sm,
+                                        int tid, VMap&& vmap) {
+  constexpr int NS = T::NS, TM = T::TM, TN = T::TN;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / T::WGN, wn = wave % T::WGN;
-  char* const smU = sm;
-  char* const smV = sm + NS * T::U_BYTES;
-  SideLoads<T::BM, T::UK, T::NU> lu;
-  SideLoads<T::BN, T::VK, T::NV> lv;
-  lu.init(u, k0, wave, lane, [](int r) { return r; });
-  lv.init(v, k0, wave, lane, vmap);
-  using FU = SideFrags<T::BM, T::UK, T::TM, T::WM>;
-  using FV = SideFrags<T::BN, T::VK, T::TN, T::WN>;
-  FU fu0, fu1;
-  FV fv0, fv1;
-  const int32_t u_rd = FU::first(wm * T::WM, lane), v_rd = FV::first(wn * T::WN, lane);
+  char* const smV = sm;
+  char* const smU = sm + NS * T::V_BYTES;
+  using LU = SideLoads<T::BM, T::UK, T::NU>;
+  using LV = SideLoads<T::BN, T::VK, T::NV>;
+  using FU = SideFrag<T::BM, T::UK, TM>;
+  using FV = SideFrag<T::BN, T::VK, TN>;
+  constexpr int SP = TM < 2 ? TM : 2, KEPT = TM - SP;    // rows of U with two sets, and with one
+  FU fu[KEPT ? KEPT : 1], fs[2][SP];
+  FV fv[2][TN];
+  uint32_t ua[FU::NA], va[FV::NA];
+  FU::addresses(smU, wm * T::WM, lane, ua);
+  FV::addresses(smV, wn * T::WN, lane, va);
 #pragma unroll
-  for (int i = 0; i < T::TM; ++i)
+  for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int j = 0; j < T::TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  auto mfma_one = [&](const FU& fu, const FV& fv, int i) __attribute__((always_inline)) {
-    const int mt = i / T::TN, nt = i % T::TN;
-    acc[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fv.get(nt), fu.get(mt), acc[mt][nt], 0, 0, 0);
+  // Part of a stage where chunks of K-contiguous rows end: apart, behind the loop.
+  const int32_t end = T::UK ? u.k : v.k;
+  const int32_t rest = (T::UK || T::VK) && k0 + ksteps * 64 > end ? end & 63 : 0;
+  if (rest) --ksteps;
+  const Side u_all = u, v_all = v;
+  u.k = min(u.k, k0 + ksteps * 64);
+  v.k = min(v.k, k0 + ksteps * 64);
+
+  auto mfma_one = [&](int set, int i) __attribute__((always_inline)) {
+    const int mt = i / TN, nt = i % TN;
+    const bf16x8 a = mt < KEPT ? fu[mt < KEPT ? mt : 0].get() : fs[set][mt < KEPT ? 0 : mt - KEPT].get();
+    acc[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fv[set][nt].get(), a, acc[mt][nt], 0, 0, 0);
   };
-  auto load_one = [&](const i32x4& du, const i32x4& dv, int at, int i) __attribute__((always_inline)) {
-    if (i < T::NU) lu.load(du, smU + at * T::U_BYTES, i);
-    else lv.load(dv, smV + at * T::V_BYTES, i - T::NU);
+  // Reads into the second sets: V's tiles and U's last rows, in this order.
+  constexpr int kV = TN * FV::READS, kFirst = kV + SP * FU::READS;
+  auto read_first = [&](int set, int ph, int kk, int i) __attribute__((always_inline)) {
+    if (i < kV) fv[set][i / FV::READS].read(va, ph * T::V_BYTES, kk, i / FV::READS, i % FV::READS);
+    else fs[set][(i - kV) / FU::READS].read(ua, ph * T::U_BYTES, kk, KEPT + (i - kV) / FU::READS, (i - kV) % FU::READS);
   };
-  constexpr int kReads = FU::READS + FV::READS;
-  auto read_one = [&](FU& fu, FV& fv, int at, int kk, int i) __attribute__((always_inline)) {
-    if (i < FU::READS) fu.read(smU + at * T::U_BYTES, u_rd, kk, i);
-    else fv.read(smV + at * T::V_BYTES, v_rd, kk, i - FU::READS);
+  // One half on set `set`; behind its MFMAs the reads of the next one (half kk of
+  // stage buffer ph) and `loads` further operations.
+  auto half = [&](int set, int ph, int kk, int loads, auto&& load) __attribute__((always_inline)) {
+    constexpr int kMfma = TM * TN;
+    const int all = kFirst + loads > kMfma ? kFirst + loads : kMfma;
+#pragma unroll
+    for (int i = 0; i < all; ++i) {
+      if (i < kMfma) mfma_one(set, i);
+      if (i < kFirst) read_first(set ^ 1, ph, kk, i);
+      else if (i < kFirst + loads) load(i - kFirst);
+      if (i < kMfma && (i + 1) % TN == 0 && i / TN < KEPT) {
+#pragma unroll
+        for (int h = 0; h < FU::READS; ++h) fu[i / TN].read(ua, ph * T::U_BYTES, kk, i / TN, h);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
-  auto stage_barrier = [&]() __attribute__((always_inline)) {
-    __builtin_amdgcn_s_waitcnt(waitcnt_imm((NS - 2) * T::NL, 0));
+  auto read_all = [&](int kk) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kFirst; ++i) read_first(0, 0, kk, i);
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i)
+#pragma unroll
+      for (int h = 0; h < FU::READS; ++h) fu[i].read(ua, 0, kk, i, h);
+  };
+  auto barrier = [&](auto vm) __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(waitcnt_imm(decltype(vm)::value, 0));
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  // A step on stage buffer ph; on entry fu0 / fv0 hold its first half.
-  auto step = [&](int ph) __attribute__((always_inline)) {
-    constexpr int kMfma = T::TM * T::TN;
-    constexpr int kOps1 = kReads + (T::kLate ? 0 : T::NL), kAll1 = kMfma > kOps1 ? kMfma : kOps1;
-    const i32x4 du = lu.next(), dv = lv.next();
-    const int to = (ph + T::AHEAD) % NS, nx = (ph + 1) % NS;
-#pragma unroll
-    for (int i = 0; i < kAll1; ++i) {
-      if (i < kMfma) mfma_one(fu0, fv0, i);
-      if (i < kReads) read_one(fu1, fv1, ph, 1, i);
-      else if (i < kOps1) load_one(du, dv, to, i - kReads);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    stage_barrier();
-    constexpr int kOps2 = T::kLate && T::NL > kReads ? T::NL : kReads, kAll2 = kMfma > kOps2 ? kMfma : kOps2;
-#pragma unroll
-    for (int i = 0; i < kAll2; ++i) {
-      if (i < kMfma) mfma_one(fu1, fv1, i);
-      if (i < kReads) read_one(fu0, fv0, nx, 0, i);
-      if (T::kLate && i < T::NL) load_one(du, dv, to, i);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  };
 
+  if (ksteps > 0) {
+    LU lu;
+    LV lv;
+    lu.init(u, k0, wave, lane, [](int r) { return r; });
+    lv.init(v, k0, wave, lane, vmap);
+    auto load_one = [&](const i32x4& du, const i32x4& dv, int at, int i) __attribute__((always_inline)) {
+      if (i < T::NU) lu.load(du, smU + at * T::U_BYTES, i);
+      else lv.load(dv, smV + at * T::V_BYTES, i - T::NU);
+    };
+    // A step on stage buffer ph; on entry set 0 holds its first half.
+    auto step = [&](int ph) __attribute__((always_inline)) {
+      const i32x4 du = lu.next(), dv = lv.next();
+      const int to = (ph + T::AHEAD) % NS, nx = (ph + 1) % NS;
+      auto load = [&](int i) __attribute__((always_inline)) { load_one(du, dv, to, i); };
+      half(0, ph, 1, T::kLate ? 0 : T::NL, load);
+      barrier(std::integral_constant<int, (NS - 2) * T::NL>{});
+      half(1, nx, 0, T::kLate ? T::NL : 0, load);
+    };
 #pragma unroll
-  for (int j = 0; j < T::AHEAD; ++j) {
+    for (int j = 0; j < T::AHEAD; ++j) {
+      const i32x4 du = lu.next(), dv = lv.next();
+#pragma unroll
+      for (int i = 0; i < T::NL; ++i) load_one(du, dv, j, i);
+    }
+    barrier(std::integral_constant<int, T::kLate ? T::NL : (NS - 2) * T::NL>{});
+    read_all(0);
+    // One loop, left behind any step: with a second copy of the steps for what a
+    // multiple of NS leaves over, the 256x256 tiles' accumulators were spilled.
+    bool more = true;
+    for (int32_t s = 0; more;) {
+#pragma unroll
+      for (int j = 0; j < NS; ++j)
+        if (more) {
+          step(j);
+          more = ++s < ksteps;
+        }
+    }
+    // loads past the last stage write zeros to LDS: they land before it is reused
+    barrier(std::integral_constant<int, 0>{});
+  }
+  if (rest) {
+    const int32_t k = k0 + ksteps * 64;
+    LU lu;
+    LV lv;
+    lu.init(u_all, k, wave, lane, [](int r) { return r; }, rest / 8);
+    lv.init(v_all, k, wave, lane, vmap, rest / 8);
     const i32x4 du = lu.next(), dv = lv.next();
 #pragma unroll
-    for (int i = 0; i < T::NL; ++i) load_one(du, dv, j, i);
-  }
-  if constexpr (T::kLate) {
-    __builtin_amdgcn_s_waitcnt(waitcnt_imm(T::NL, 0));
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-  } else {
-    stage_barrier();
-  }
+    for (int i = 0; i < T::NU; ++i) lu.load(du, smU, i);
 #pragma unroll
-  for (int i = 0; i < kReads; ++i) read_one(fu0, fv0, 0, 0, i);
-  int32_t s = 0;
-  for (; s + NS <= ksteps; s += NS) {
+    for (int i = 0; i < T::NV; ++i) lv.load(dv, smV, i);
+    barrier(std::integral_constant<int, 0>{});
 #pragma unroll
-    for (int j = 0; j < NS; ++j) step(j);
+    for (int kk = 0; kk < 2; ++kk) {
+      read_all(kk);
+#pragma unroll
+      for (int i = 0; i < TM * TN; ++i) mfma_one(0, i);
+    }
+    barrier(std::integral_constant<int, 0>{});
   }
-#pragma unroll
-  for (int j = 0; j < NS - 1; ++j)
-    if (s + j < ksteps) step(j);
-  // loads past the last stage write zeros to LDS: they land before it is reused
-  __builtin_amdgcn_s_waitcnt(0);
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
 }
 #endif
 
