@@ -497,7 +497,8 @@ typedef enum ccl_grouped_direction {
 } ccl_grouped_direction;
 
 /*
- * Device workspace of such a call, and the calls. rows: rows of X, dY, Y, ...;
+ * Device workspace of such a call (of `rows` rows or fewer; 32 MB at most), and
+ * the calls. rows: rows of X, dY, Y, ...;
  * ends: `experts` ascending row numbers on the device, of which the last may be
  * smaller than rows: rows behind it are neither read nor written. (Numbers that
  * do not ascend or lie outside 0 .. rows give unspecified values, never an
@@ -561,7 +562,7 @@ typedef struct ccl_vocab {
 
 /*
  * Device workspace of ccl_cross_entropy (grad = 0) or ccl_cross_entropy_grad
- * (grad = 1) for `tokens` tokens, and the calls. X and dX are bf16 with rows
+ * (grad = 1) for up to `tokens` tokens, and the calls. X and dX are bf16 with rows
  * x_ld, dx_ld apart, W bf16; targets, int64, dloss (fp32, or NULL: 1), loss and
  * lse (fp32) have one element a token; loss or lse may be NULL (in
  * ccl_cross_entropy not both). dX or dW may be NULL (not both) where it is not

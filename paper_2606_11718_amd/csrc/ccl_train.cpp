@@ -70,7 +70,8 @@ ccl_status check_grouped(const ccl_grouped* g, int64_t rows, int direction, ccl:
     return fail(CCL_ERR_MISALIGNED_POINTER, "weight rows and experts must lie whole 16 bytes apart");
   if (gated && direction == CCL_GROUPED_FORWARD && s.out * s.w_ld >= (int64_t)1 << 30)
     return fail(CCL_ERR_UNSUPPORTED, "gated: an expert's weight must span less than 2^30 elements");
-  if (ccl::grouped_form(s, rows, direction).workgroups > kMaxGrid) return fail(CCL_ERR_UNSUPPORTED, "launch too large");
+  // the tiles' numbers are 32-bit, beyond the last by a round of workgroups
+  if (ccl::grouped_form(s, rows, direction).tiles > kMaxGrid / 2) return fail(CCL_ERR_UNSUPPORTED, "launch too large");
   *out = s;
   return CCL_OK;
 }
@@ -93,8 +94,8 @@ ccl_status check_vocab(const ccl_vocab* v, int64_t tokens, bool grad, ccl::Vocab
   if (s.w_ld % 8) return fail(CCL_ERR_MISALIGNED_POINTER, "rows of W must lie whole 16 bytes apart");
   if (tokens) {
     const ccl::VocabForm f = ccl::vocab_form(s, tokens, grad);
-    if (ccl::vocab_logits_form(s, f.block).workgroups > kMaxGrid || ccl::vocab_dw_form(s, f.block).workgroups > kMaxGrid ||
-        ccl::vocab_dx_form(s, f.block).workgroups > kMaxGrid || (f.block * s.hidden + 1023) / 1024 > kMaxGrid)
+    if (ccl::vocab_logits_form(s, f.block).tiles > kMaxGrid / 2 || ccl::vocab_dw_form(s, f.block).tiles > kMaxGrid / 2 ||
+        ccl::vocab_dx_form(s, f.block).tiles > kMaxGrid / 2 || (f.block * s.hidden + 1023) / 1024 > kMaxGrid)
       return fail(CCL_ERR_UNSUPPORTED, "launch too large");
   }
   *out = s;
@@ -138,7 +139,7 @@ ccl_status ccl_grouped_gemm_workspace(const ccl_grouped* grouped, int64_t rows, 
   if (!workspace_bytes) return fail(CCL_ERR_INVALID_ARG, "NULL argument");
   ccl::GroupedShape s;
   if (ccl_status st = check_grouped(grouped, rows, direction, &s)) return st;
-  *workspace_bytes = rows ? ccl::grouped_form(s, rows, direction).workspace_bytes : 0;
+  *workspace_bytes = ccl::grouped_workspace(s, rows, direction);
   return ok();
 }
 

@@ -8,27 +8,70 @@ namespace {
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Workgroups of `tiles` dealt to the 8 XCDs in runs of `chunk`.
-int64_t dealt(int64_t tiles, int64_t chunk) { return 8 * chunk * up(tiles, 8 * chunk); }
+// fp32 tiles of all K ranges of a product, at most: ranges are made while tiles times
+// ranges fit 512 workgroups of 128 x 128.
+constexpr int64_t kPartBytes = (int64_t)512 * 128 * 128 * 4;
+constexpr int kMaxRanges = 64;
+int64_t part_bound(int64_t elems) { return std::min<int64_t>(kPartBytes, 4 * kMaxRanges * elems); }
 
 }  // namespace
 
+// Workgroups that stay and take `tiles` in turn, per_cu of them on a CU; one for
+// every tile where there are fewer (a multiple of 8: XCDs).
+int64_t resident(int64_t tiles, int per_cu) { return std::min<int64_t>(up(std::max<int64_t>(tiles, 1), 8) * 8, 256 * per_cu); }
+
+// Tiles, measured (us, 256x256 against 128x128 tiles, of which two workgroups share a
+// CU): a large tile moves half as much through LDS for each product, but hides
+// neither its rows' padding nor its wait for memory behind another workgroup.
+//   forward  32768 rows over 128 experts of 2048 -> 1536 322 / 331, 16384 272 / 246,
+//            8192 over 8 104 / 74 (fewer tiles than CUs), over one of 4096 -> 4096
+//            218 / 278
+//   grad     32768 over 128 of 768 -> 2048 through SwiGLU 258 / 213 (three tiles a CU,
+//            uneven), 65536 372 / 369, 8192 over one of 4096 -> 4096 235 / 288
+//   wgrad    32768 over 128 of 2048 -> 1536 387 / 451, 8192 over one 223 / 288, 65536
+//            over 4 of 256 -> 256 334 / 181 (4 tiles an expert)
+// 64x128 ones where few rows come to an expert: 8 rows 24.6 us against 26.6, 64 rows
+// 68.2 / 71.2 (forward as above), at 32 rows an expert 212 / 195.
 GroupedForm grouped_form(const GroupedShape& s, int64_t rows, int direction) {
   GroupedForm f;
-  f.tile_m = f.tile_n = 128;
-  f.chunk = 32;
-  int64_t tiles;
-  if (direction == GROUPED_WGRAD) {
-    f.tiles_m = (int32_t)up(s.out, f.tile_m);
-    f.tiles_n = (int32_t)up(s.in, f.tile_n);
-    tiles = (int64_t)s.experts * f.tiles_m * f.tiles_n;
-  } else {
-    f.tiles_n = (int32_t)up(direction == GROUPED_FORWARD ? s.out : s.in, f.tile_n);
-    // at most: every expert with rows has one tile that is not whole
-    tiles = (rows / f.tile_m + std::min<int64_t>(s.experts, rows)) * f.tiles_n;
+  const bool wgrad = direction == GROUPED_WGRAD;
+  const int64_t n = direction == GROUPED_FORWARD ? s.out : s.in;
+  const int64_t used = std::max<int64_t>(1, std::min<int64_t>(s.experts, rows)), mean = rows / used;
+  const auto tiles = [&](int64_t tm, int64_t tn) {
+    // at most: every expert with rows has one row tile that is not whole
+    return wgrad ? s.experts * up(s.out, tm) * up(s.in, tn) : (rows / tm + std::min<int64_t>(s.experts, rows)) * up(n, tn);
+  };
+  const int64_t large = tiles(256, 256);
+  if (wgrad ? large >= 256 : (mean >= 512 && large >= (direction == GROUPED_FORWARD ? 256 : 512)) ||
+                                 (direction == GROUPED_FORWARD && mean >= 192 && large >= 512))
+    f.tile_m = f.tile_n = 256;
+  else {
+    f.tile_m = wgrad || mean >= 24 ? 128 : 64;
+    f.tile_n = 128;
   }
-  f.workgroups = dealt(tiles, f.chunk);
+  const int per_cu = f.tile_m == 256 ? 1 : 2;
+  if (wgrad) f.tiles_m = (int32_t)up(s.out, f.tile_m);
+  f.tiles_n = (int32_t)up(wgrad ? s.in : n, f.tile_n);
+  f.tiles = tiles(f.tile_m, f.tile_n);
+  // K ranges where tiles leave half of the workgroups without one, of four steps of
+  // 64 K at least; their fp32 sums are added up by a second launch.
+  const int64_t steps = wgrad ? mean / 64 : up(direction == GROUPED_FORWARD ? s.in : s.out, 64);
+  const int64_t fit = 256 * per_cu / std::max<int64_t>(f.tiles, 1);
+  if (fit >= 2 && steps >= 8) {
+    f.splits = (int32_t)std::min<int64_t>(std::min(fit, steps / 4), kMaxRanges);
+    f.tiles *= f.splits;
+    f.workspace_bytes = 4 * f.splits * (wgrad ? s.experts * s.out * s.in : rows * n);
+  }
+  f.workgroups = resident(f.tiles, per_cu);
+  // 16 against 32 and 64 a workgroup of a CU: 321 / 326 / 326 us (forward above)
+  f.chunk = (int32_t)std::min<int64_t>(16, f.workgroups / 8);
   return f;
+}
+
+int64_t grouped_workspace(const GroupedShape& s, int64_t rows, int direction) {
+  const int64_t k = direction == GROUPED_WGRAD ? rows : direction == GROUPED_FORWARD ? s.in : s.out;
+  if (up(k, 64) < 8 || rows == 0) return 0;
+  return part_bound(direction == GROUPED_WGRAD ? s.experts * s.out * s.in : rows * (direction == GROUPED_FORWARD ? s.out : s.in));
 }
 
 namespace {
@@ -43,10 +86,12 @@ ProductForm product_form(int64_t m, int64_t n, int tile_m, int tile_n, int64_t k
   f.tiles_m = (int32_t)up(m, tile_m);
   f.tiles_n = (int32_t)up(n, tile_n);
   f.group = 8;
-  f.chunk = 32;
   f.ksplit = (int32_t)up(ksteps, splits);
   f.splits = (int32_t)up(ksteps, f.ksplit);
-  f.workgroups = dealt((int64_t)f.tiles_m * f.tiles_n * f.splits, f.chunk);
+  const int per_cu = tile_m == 256 ? 1 : 2;
+  f.tiles = (int64_t)f.tiles_m * f.tiles_n * f.splits;
+  f.workgroups = resident(f.tiles, per_cu);
+  f.chunk = (int32_t)std::min<int64_t>(32 * per_cu, f.workgroups / 8);
   return f;
 }
 
@@ -66,7 +111,7 @@ ProductForm vocab_dx_form(const VocabShape& s, int64_t tokens) {
   if (large_tiles(tokens, s.hidden)) return product_form(tokens, s.hidden, 256, 256, up(s.vocab, 64), 1);
   const int tile_m = tokens <= 64 ? 64 : 128;
   const int64_t tiles = up(tokens, tile_m) * up(s.hidden, 128);
-  const int64_t splits = tiles >= 512 ? 1 : std::min<int64_t>(std::min<int64_t>(up(512, tiles), 64), up(s.vocab, 1024));
+  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / tiles, kMaxRanges), up(s.vocab, 1024)));
   return product_form(tokens, s.hidden, tile_m, 128, up(s.vocab, 64), (int)splits);
 }
 
@@ -81,8 +126,7 @@ VocabForm vocab_form(const VocabShape& s, int64_t tokens, bool grad) {
   f.e_ld = f.e_cols + 64;      // rows a power of two apart would share memory channels
   int64_t most = s.block ? s.block : kLossBlock;
   if (!s.block && grad) most = std::min(most, std::max<int64_t>(256, kKeptBytes / (2 * f.e_ld) / 256 * 256));
-  f.blocks = std::max<int64_t>(1, up(tokens, most));
-  f.block = s.block ? std::min(s.block, tokens) : std::min(tokens, up(up(tokens, f.blocks), 256) * 256);
+  f.block = std::min(tokens, most);
   f.blocks = f.block ? up(tokens, f.block) : 0;
   int64_t at = 0;
   const auto take = [&](int64_t bytes) {
@@ -96,14 +140,7 @@ VocabForm vocab_form(const VocabShape& s, int64_t tokens, bool grad) {
   if (grad) {
     f.e_at = take(2 * f.block * f.e_ld);
     f.rows_at = take(2 * f.block * s.hidden);
-    // the last block may be cut into more ranges than the others
-    int64_t part = 0;
-    for (int64_t t : {f.block, tokens - (f.blocks - 1) * f.block})
-      if (t > 0) {
-        const ProductForm d = vocab_dx_form(s, t);
-        if (d.splits > 1) part = std::max(part, 4 * d.splits * t * s.hidden);
-      }
-    f.part_at = take(part);
+    f.part_at = take(part_bound(f.block * s.hidden));
     f.sum_at = take(f.blocks > 1 ? 4 * s.vocab * s.hidden : 0);
   }
   f.workspace_bytes = at;

@@ -19,9 +19,13 @@ struct GroupedForm {
   int tile_m = 0, tile_n = 0;
   int32_t tiles_m = 0, tiles_n = 0;           // tiles_m: of a weight gradient
   int32_t chunk = 1;                          // consecutive tiles of one XCD
+  int32_t splits = 1;                         // K ranges of a tile
+  int64_t tiles = 0;                          // at most, of all ranges
   int64_t workgroups = 0, workspace_bytes = 0;
 };
 GroupedForm grouped_form(const GroupedShape& s, int64_t rows, int direction);
+// Workspace for that many rows or fewer (fewer may be cut into more ranges).
+int64_t grouped_workspace(const GroupedShape& s, int64_t rows, int direction);
 
 // ---- vocabulary loss ----
 constexpr int64_t kVocabMaxBlock = 32768;     // the scaling pass has a grid row a token
@@ -35,8 +39,8 @@ struct VocabShape {
 struct ProductForm {
   int tile_m = 0, tile_n = 0;
   int32_t tiles_m = 0, tiles_n = 0, group = 1, chunk = 1;
-  int32_t splits = 1, ksplit = 0;             // ksplit: stages of 64 K a range
-  int64_t workgroups = 0;
+  int32_t splits = 1, ksplit = 0;             // ksplit: steps of 64 K a range
+  int64_t tiles = 0, workgroups = 0;          // tiles: of all ranges
 };
 struct VocabForm {
   int64_t block = 0, blocks = 0;              // tokens at once (the last block may have fewer)
@@ -45,7 +49,7 @@ struct VocabForm {
   // bytes into the workspace
   int64_t target_at = 0, factor_at = 0, stat_at = 0, e_at = 0, rows_at = 0, part_at = 0, sum_at = 0, workspace_bytes = 0;
 };
-// The blocks and the workspace; grad: with exp(z - tile max) kept for a block,
+// The blocks and the workspace, which fewer tokens do not exceed; grad: with exp(z - tile max) kept for a block,
 // a copy of its x,
 // the ranges' partial dX and, where dW is rounded after several blocks, its fp32 sum.
 VocabForm vocab_form(const VocabShape& s, int64_t tokens, bool grad);

@@ -34,97 +34,111 @@ struct LogitsParams {
   float scale;
 };
 
-// Tile `id` in a raster of `group` tile rows, column by column.
-__device__ __forceinline__ void raster(int64_t id, int32_t tiles_m, int32_t tiles_n, int32_t group, int32_t* ti, int32_t* tj) {
-  const int32_t per = group * tiles_n, r = (int32_t)(id / per), first = r * group, h = min(group, tiles_m - first);
-  const int32_t w = (int32_t)(id - (int64_t)r * per);
-  *tj = __builtin_amdgcn_readfirstlane(w / h);
-  *ti = __builtin_amdgcn_readfirstlane(first + w - w / h * h);
-}
-
-template <int BM, int BN, int NS, int WGN>
-__global__ void __launch_bounds__(512, NS * (BM + BN) * 128 <= 80 * 1024 ? 4 : 2) logits_kernel(LogitsParams p) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  using T = ProductTile<BM, BN, true, true, NS, WGN>;
-  __shared__ __attribute__((aligned(1024))) char sm[T::LDS];
-  const int64_t id = dealt_tile(p.chunk);
-  if (id >= (int64_t)p.tiles_m * p.tiles_n) return;
+struct LogitsWork {
+  Side u, v;
+  int32_t steps;
   int32_t ti, tj;
-  raster(id, p.tiles_m, p.tiles_n, p.group, &ti, &tj);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wn = wave % WGN;
-  const int32_t rows = min(BM, p.tokens - ti * BM), cols = min(BN, p.vocab - tj * BN);
-  f32x4 acc[T::TM][T::TN];
-  product<T>(Side{p.X + (int64_t)ti * BM * p.x_ld, p.x_ld, rows, p.hidden},
-             Side{p.W + (int64_t)tj * BN * p.w_ld, p.w_ld, cols, p.hidden}, 0, (p.hidden + 63) / 64, acc, sm, tid,
-             [](int r) { return r; });
-  float* const part = reinterpret_cast<float*>(sm);     // [WGN][BM]
-  float* const whole = part + WGN * BM;                 // [BM]: the tile's maxima
-  // rows' maxima over a wave's columns, then over the waves
-  float top[T::TM];
+};
+
+template <typename T>
+__global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) logits_kernel(LogitsParams p) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int BM = T::BM, BN = T::BN, TM = T::TM, TN = T::TN, WGN = T::WGN;
+  __shared__ __attribute__((aligned(1024))) char sm[T::LDS];
+  __shared__ float part[WGN][BM], whole[BM];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / WGN, wn = wave % WGN;
+  product_tiles<T, LogitsWork>(
+      p.x_ld, p.w_ld, sm, tid,
+      [&](int i, LogitsWork* w) __attribute__((always_inline)) {
+        const int32_t id = dealt_tile(i, p.chunk);
+        if (id >= p.tiles_m * p.tiles_n) return false;
+        raster(id, p.tiles_m, p.tiles_n, p.group, &w->ti, &w->tj);
+        w->steps = product_steps<T>(p.hidden);
+        w->u = Side{p.X + (int64_t)w->ti * BM * p.x_ld, min(BM, p.tokens - w->ti * BM), p.hidden};
+        w->v = Side{p.W + (int64_t)w->tj * BN * p.w_ld, min(BN, p.vocab - w->tj * BN), p.hidden};
+        return true;
+      },
+      [](int r) { return r; },
+      [&](const LogitsWork& w, f32x4 (&acc)[TM][TN]) __attribute__((always_inline)) {
+        const int32_t rows = w.u.extent, col0 = w.tj * BN + wn * T::WN + 4 * (lane >> 4);
+        const int32_t left = p.vocab - col0;         // columns from the lane's first on
+        // rows' maxima over a wave's columns, then over the waves
+        float top[TM], sum[TM];
 #pragma unroll
-  for (int mt = 0; mt < T::TM; ++mt) top[mt] = -INFINITY;
-  each4<T>(tid, [&](int mt, int nt, int r, int c) __attribute__((always_inline)) {
+        for (int mt = 0; mt < TM; ++mt) {
+          top[mt] = -INFINITY;
+          if (T::row(wm, mt) < rows) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      acc[mt][nt][j] = c + j < cols ? acc[mt][nt][j] * p.scale : -INFINITY;
-      top[mt] = fmaxf(top[mt], acc[mt][nt][j]);
-    }
-  });
-  const int r0 = (wave / WGN) * T::WM + (lane & 15);
+            for (int nt = 0; nt < TN; ++nt)
 #pragma unroll
-  for (int mt = 0; mt < T::TM; ++mt) {
-    top[mt] = fmaxf(top[mt], __shfl_xor(top[mt], 16));
-    top[mt] = fmaxf(top[mt], __shfl_xor(top[mt], 32));
-    if (lane < 16) part[wn * BM + r0 + 16 * mt] = top[mt];
-  }
-  __syncthreads();
-  float sum[T::TM];
+              for (int j = 0; j < 4; ++j) {
+                acc[mt][nt][j] = 16 * nt + j < left ? acc[mt][nt][j] * p.scale : -INFINITY;
+                top[mt] = fmaxf(top[mt], acc[mt][nt][j]);
+              }
+          }
+          top[mt] = fmaxf(top[mt], __shfl_xor(top[mt], 16));
+          top[mt] = fmaxf(top[mt], __shfl_xor(top[mt], 32));
+          if (lane < 16) part[wn][T::row(wm, mt) + lane] = top[mt];
+        }
+        product_barrier<63>();
 #pragma unroll
-  for (int mt = 0; mt < T::TM; ++mt) {
+        for (int mt = 0; mt < TM; ++mt) {
+          const int r = T::row(wm, mt) + (lane & 15);
 #pragma unroll
-    for (int w = 0; w < WGN; ++w) top[mt] = fmaxf(top[mt], part[w * BM + r0 + 16 * mt]);
-    if (wn == 0 && lane < 16) whole[r0 + 16 * mt] = top[mt];
-    sum[mt] = 0.f;
-    // the target's logit
-    const int32_t row = ti * BM + r0 + 16 * mt;
-    if (row < p.tokens) {
-      const int64_t t = p.targets[row] - (int64_t)tj * BN - wn * T::WN - 4 * (lane >> 4);
+          for (int k = 0; k < WGN; ++k) top[mt] = fmaxf(top[mt], part[k][r]);
+          if (wn == 0 && lane < 16) whole[r] = top[mt];
+          sum[mt] = 0.f;
+          if (T::row(wm, mt) >= rows) continue;
+          // the target's logit
+          if (r < rows) {
+            const int64_t t = p.targets[w.ti * BM + r] - col0;
+            if (t >= 0 && t < T::WN && t < left) {
 #pragma unroll
-      for (int nt = 0; nt < T::TN; ++nt)
+              for (int nt = 0; nt < TN; ++nt)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (t == 16 * nt + j && tj * BN + wn * T::WN + 4 * (lane >> 4) + 16 * nt + j < p.vocab) p.target_z[row] = acc[mt][nt][j];
-    }
-  }
-  each4<T>(tid, [&](int mt, int nt, int r, int c) __attribute__((always_inline)) {
+                for (int j = 0; j < 4; ++j)
+                  if (t == 16 * nt + j) p.target_z[w.ti * BM + r] = acc[mt][nt][j];
+            }
+          }
+          uint2 e[TN];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      acc[mt][nt][j] = __builtin_amdgcn_exp2f((acc[mt][nt][j] - top[mt]) * kLog2e);
-      sum[mt] += acc[mt][nt][j];
-    }
-  });
-  __syncthreads();
+          for (int nt = 0; nt < TN; ++nt) {
 #pragma unroll
-  for (int mt = 0; mt < T::TM; ++mt) {
-    sum[mt] += __shfl_xor(sum[mt], 16);
-    sum[mt] += __shfl_xor(sum[mt], 32);
-    if (lane < 16) part[wn * BM + r0 + 16 * mt] = sum[mt];
-  }
-  __syncthreads();
-  if (tid < rows) {
-    float s = 0.f;
+            for (int j = 0; j < 4; ++j) {
+              acc[mt][nt][j] = __builtin_amdgcn_exp2f((acc[mt][nt][j] - top[mt]) * kLog2e);
+              sum[mt] += acc[mt][nt][j];
+            }
+            e[nt] = f32_to_bf16x4(acc[mt][nt]);
+          }
+          if (p.E) {
+            uint16_t* const to = p.E + (int64_t)(w.ti * BM + r) * p.e_ld;
 #pragma unroll
-    for (int w = 0; w < WGN; ++w) s += part[w * BM + tid];
-    p.stat[(int64_t)(ti * BM + tid) * p.tiles_n + tj] = make_float2(whole[tid], s);
-  }
-  if (!p.E) return;
-  __syncthreads();
-  const auto e = staged<BM, BN>(sm);
-  each4<T>(tid, [&](int mt, int nt, int r, int c) __attribute__((always_inline)) { *e.at(r, c) = f32_to_bf16x4(acc[mt][nt]); });
-  staged_barrier();
-  // columns past the vocabulary up to e_cols: exp(-inf) = 0
-  tile_out<BM, BN, 512>(e, p.E + (int64_t)ti * BM * p.e_ld, p.e_ld, rows, tid,
-                        [&](int c) { return tj * BN + 8 * c < p.e_cols ? tj * BN + 8 * c : -1; });
+            for (int nt = 0; nt < TN; nt += 2) {
+              // columns past the vocabulary up to e_cols: exp(-inf) = 0
+              const int32_t c = w.tj * BN + wn * T::WN + 16 * nt + pair_column(lane);
+              const uint4 v = pair_up(e[nt], e[nt + 1]);
+              if (r < rows && c < p.e_cols) *reinterpret_cast<uint4*>(to + c) = v;
+            }
+          }
+        }
+        product_barrier<63>();
+#pragma unroll
+        for (int mt = 0; mt < TM; ++mt) {
+          sum[mt] += __shfl_xor(sum[mt], 16);
+          sum[mt] += __shfl_xor(sum[mt], 32);
+          if (lane < 16) part[wn][T::row(wm, mt) + lane] = sum[mt];
+        }
+        product_barrier<63>();
+        if (tid < rows) {
+          float s = 0.f;
+#pragma unroll
+          for (int k = 0; k < WGN; ++k) s += part[k][tid];
+          p.stat[(int64_t)(w.ti * BM + tid) * p.tiles_n + w.tj] = make_float2(whole[tid], s);
+        }
+        // the next tile's finish writes part again
+        product_barrier<63>();
+      });
 #endif
 }
 
@@ -220,63 +234,82 @@ struct PlainParams {
   int32_t f32, accumulate;
 };
 
-template <int BM, int BN, int NS, int WGN, bool UK, bool VK>
-__global__ void __launch_bounds__(512, NS * (BM + BN) * 128 <= 80 * 1024 ? 4 : 2) plain_kernel(PlainParams p) {
+struct PlainWork {
+  Side u, v;
+  int32_t steps;
+  int32_t ti, tj, split, m, n;
+};
+
+// MORE: with what is added, fp32 results and partial sums (apart, since they take
+// registers that the 256x256 tiles' loop needs).
+template <typename T, bool MORE>
+__global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) plain_kernel(PlainParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  using T = ProductTile<BM, BN, UK, VK, NS, WGN>;
+  constexpr int BM = T::BM, BN = T::BN, TM = T::TM, TN = T::TN;
   __shared__ __attribute__((aligned(1024))) char sm[T::LDS];
-  int64_t id = dealt_tile(p.chunk);
-  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
-  if (id >= tiles * p.splits) return;
-  const int32_t split = __builtin_amdgcn_readfirstlane((int32_t)(id / tiles));
-  id -= split * tiles;
-  int32_t ti, tj;
-  raster(id, p.tiles_m, p.tiles_n, p.group, &ti, &tj);
-  const int tid = threadIdx.x;
-  const int32_t s0 = split * p.ksplit, steps = min(p.ksplit, p.ksteps - s0);
-  const int32_t m = min(BM, p.m - ti * BM), n = min(BN, p.n - tj * BN);
-  const Side u = UK ? Side{p.U + (int64_t)ti * BM * p.ldu, p.ldu, m, p.ku}
-                    : Side{p.U + ti * BM, p.ldu, min(BM, p.mu - ti * BM), p.ku};
-  const Side v = VK ? Side{p.V + (int64_t)tj * BN * p.ldv, p.ldv, n, p.kv}
-                    : Side{p.V + tj * BN, p.ldv, min(BN, p.nv - tj * BN), p.kv};
-  // a range ends where the next begins
-  const int32_t end = (s0 + steps) * 64;
-  f32x4 acc[T::TM][T::TN];
-  product<T>(Side{u.base, u.ld, u.extent, min(u.k, end)}, Side{v.base, v.ld, v.extent, min(v.k, end)}, s0 * 64, steps, acc,
-             sm, tid, [](int r) { return r; });
-  if (p.part) {
-    float* const to = p.part + ((int64_t)split * p.m + ti * BM) * p.n + tj * BN;
-    each4<T>(tid, [&](int mt, int nt, int r, int c) __attribute__((always_inline)) {
-      if (r < m && c < n) *reinterpret_cast<f32x4*>(to + (int64_t)r * p.n + c) = acc[mt][nt];
-    });
-    return;
-  }
-  const int64_t corner = (int64_t)ti * BM * p.ld_out + tj * BN;
-  const float* const add = p.add ? p.add + (int64_t)ti * BM * p.n + tj * BN : nullptr;
-  if (p.f32) {
-    float* const to = static_cast<float*>(p.out) + corner;
-    each4<T>(tid, [&](int mt, int nt, int r, int c) __attribute__((always_inline)) {
-      if (r >= m || c >= n) return;
-      f32x4* at = reinterpret_cast<f32x4*>(to + r * p.ld_out + c);
-      f32x4 o = acc[mt][nt];
-      if (add) o += *reinterpret_cast<const f32x4*>(add + (int64_t)r * p.n + c);
-      if (p.accumulate) o += *at;
-      *at = o;
-    });
-    return;
-  }
-  uint16_t* const to = static_cast<uint16_t*>(p.out) + corner;
-  const auto s = staged<BM, BN>(sm);
-  each4<T>(tid, [&](int mt, int nt, int r, int c) __attribute__((always_inline)) {
-    f32x4 o = acc[mt][nt];
-    if (r < m && c < n) {
-      if (add) o += *reinterpret_cast<const f32x4*>(add + (int64_t)r * p.n + c);
-      if (p.accumulate) o += bf16x4_to_f32(*reinterpret_cast<const uint2*>(to + r * p.ld_out + c));
-    }
-    *s.at(r, c) = f32_to_bf16x4(o);
-  });
-  staged_barrier();
-  tile_out<BM, BN, 512>(s, to, p.ld_out, m, tid, [&](int c) { return 8 * c < n ? 8 * c : -1; });
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / T::WGN, wn = wave % T::WGN;
+  const int32_t tiles = p.tiles_m * p.tiles_n;
+  product_tiles<T, PlainWork>(
+      p.ldu, p.ldv, sm, tid,
+      [&](int i, PlainWork* w) __attribute__((always_inline)) {
+        const int32_t id = dealt_tile(i, p.chunk);
+        if (id >= tiles * p.splits) return false;
+        w->split = __builtin_amdgcn_readfirstlane(id / tiles);
+        raster(id - w->split * tiles, p.tiles_m, p.tiles_n, p.group, &w->ti, &w->tj);
+        // a range ends where the next begins
+        const int32_t k0 = w->split * p.ksplit * 64, k = p.ksplit * 64;
+        const int32_t ku = min(p.ku - k0, k), kv = min(p.kv - k0, k);
+        w->steps = product_steps<T>(max(ku, kv));
+        w->m = min(BM, p.m - w->ti * BM);
+        w->n = min(BN, p.n - w->tj * BN);
+        w->u = T::UK ? Side{p.U + (int64_t)w->ti * BM * p.ldu + k0, w->m, ku}
+                     : Side{p.U + (int64_t)k0 * p.ldu + w->ti * BM, min(BM, p.mu - w->ti * BM), ku};
+        w->v = T::VK ? Side{p.V + (int64_t)w->tj * BN * p.ldv + k0, w->n, kv}
+                     : Side{p.V + (int64_t)k0 * p.ldv + w->tj * BN, min(BN, p.nv - w->tj * BN), kv};
+        return true;
+      },
+      [](int r) { return r; },
+      [&](const PlainWork& w, f32x4 (&acc)[TM][TN]) __attribute__((always_inline)) {
+        const int64_t row0 = (int64_t)w.ti * BM;
+        const int32_t col0 = w.tj * BN;
+#pragma unroll
+        for (int mt = 0; mt < TM; ++mt) {
+          const int r = T::row(wm, mt) + (lane & 15);
+          const bool live = r < w.m;
+          if (MORE && (p.part || p.f32)) {
+            const int64_t at = p.part ? ((int64_t)w.split * p.m + row0 + r) * p.n + col0 : (row0 + r) * p.ld_out + col0;
+            float* const to = (p.part ? p.part : static_cast<float*>(p.out)) + at;
+#pragma unroll
+            for (int nt = 0; nt < TN; ++nt) {
+              const int32_t c = wn * T::WN + 16 * nt + 4 * (lane >> 4);
+              if (!live || c >= w.n) continue;
+              f32x4* const one = reinterpret_cast<f32x4*>(to + c);
+              *one = p.accumulate && !p.part ? *one + acc[mt][nt] : acc[mt][nt];
+            }
+            continue;
+          }
+          uint16_t* const to = static_cast<uint16_t*>(p.out) + (row0 + r) * p.ld_out + col0;
+          const float* const add = p.add + (row0 + r) * p.n + col0;
+#pragma unroll
+          for (int nt = 0; nt < TN; nt += 2) {
+            f32x4 a = acc[mt][nt], b = acc[mt][nt + 1];
+            const int32_t c4 = wn * T::WN + 16 * nt + 4 * (lane >> 4), c = wn * T::WN + 16 * nt + pair_column(lane);
+            if (MORE && p.add && live) {
+              if (c4 < w.n) a += *reinterpret_cast<const f32x4*>(add + c4);
+              if (c4 + 16 < w.n) b += *reinterpret_cast<const f32x4*>(add + c4 + 16);
+            }
+            if (MORE && p.accumulate) {
+              uint2 x, y;
+              pair_down(live && c < w.n ? *reinterpret_cast<const uint4*>(to + c) : make_uint4(0, 0, 0, 0), &x, &y);
+              a += bf16x4_to_f32(x);
+              b += bf16x4_to_f32(y);
+            }
+            const uint4 v = pair_up(f32_to_bf16x4(a), f32_to_bf16x4(b));
+            if (live && c < w.n) *reinterpret_cast<uint4*>(to + c) = v;
+          }
+        }
+      });
 #endif
 }
 
@@ -308,10 +341,16 @@ hipError_t launch_plain(const ProductForm& f, PlainParams p, hipStream_t stream)
   p.chunk = f.chunk;
   p.splits = f.splits;
   p.ksplit = f.ksplit;
-  const dim3 grid((unsigned)f.workgroups), block(512);
-  if (f.tile_m == 64) hipLaunchKernelGGL((plain_kernel<64, 128, 2, 4, UK, VK>), grid, block, 0, stream, p);
-  else if (f.tile_m == 256) hipLaunchKernelGGL((plain_kernel<256, 256, 2, 4, UK, VK>), grid, block, 0, stream, p);
-  else hipLaunchKernelGGL((plain_kernel<128, 128, 2, 4, UK, VK>), grid, block, 0, stream, p);
+  const auto launch = [&](auto tile) {
+    using T = decltype(tile);
+    if (p.part || p.f32 || p.add || p.accumulate)
+      hipLaunchKernelGGL((plain_kernel<T, true>), dim3((unsigned)f.workgroups), dim3(T::THREADS), 0, stream, p);
+    else
+      hipLaunchKernelGGL((plain_kernel<T, false>), dim3((unsigned)f.workgroups), dim3(T::THREADS), 0, stream, p);
+  };
+  if (f.tile_m == 256) launch(ProductTile<256, 256, UK, VK, 2, 8, 4, false, true>{});     // KC: columns of P', whole 64s
+  else if (f.tile_m == 128) launch(ProductTile<128, 128, UK, VK, 2, 8, 2>{});
+  else if constexpr (UK) launch(ProductTile<64, 128, UK, VK, 2, 8, 2, true>{});
   return hipGetLastError();
 }
 
@@ -358,10 +397,14 @@ hipError_t launch_cross_entropy(const VocabShape& s, const VocabCall& c, void* w
     lp.group = z.group;
     lp.chunk = z.chunk;
     lp.scale = s.scale;
-    const dim3 grid((unsigned)z.workgroups);
-    if (z.tile_m == 64) hipLaunchKernelGGL((logits_kernel<64, 128, 2, 4>), grid, dim3(512), 0, stream, lp);
-    else if (z.tile_m == 256) hipLaunchKernelGGL((logits_kernel<256, 256, 2, 4>), grid, dim3(512), 0, stream, lp);
-    else hipLaunchKernelGGL((logits_kernel<128, 128, 2, 4>), grid, dim3(512), 0, stream, lp);
+    const auto logits = [&](auto tile) {
+      using T = decltype(tile);
+      hipLaunchKernelGGL(logits_kernel<T>, dim3((unsigned)z.workgroups), dim3(T::THREADS), 0, stream, lp);
+    };
+    if (z.tile_m == 256 && s.hidden % 64 == 0) logits(ProductTile<256, 256, true, true, 2, 8, 4, false, true>{});
+    else if (z.tile_m == 256) logits(ProductTile<256, 256, true, true, 2, 8, 4>{});
+    else if (z.tile_m == 128) logits(ProductTile<128, 128, true, true, 2, 8, 2>{});
+    else logits(ProductTile<64, 128, true, true, 2, 8, 2, true>{});
     if (hipError_t e = hipGetLastError()) return e;
     CombineParams cp{};
     cp.stat = stat;

@@ -3,9 +3,9 @@
 //   forward  Z = X W_e^T, Y = act(Z) or act(gate) * up
 //   grad     D = dY W_e, dX = D or dZ of X = act(Z), act(gate) * up
 //   wgrad    dW_e = dY_e^T X_e (+ dW_e)
-// The row counts are on the device only: a launch has as many workgroups as the
-// counts can take at most, and each finds its tile from ends by a scan over the
-// experts' tiles, one thread an expert.
+// The row counts are on the device only: every workgroup makes a table of the
+// experts' rows and tiles in LDS and takes its tiles from it. Each weight is read by the row tiles of its expert, which run next to each
+// other on one XCD.
 #include "product.hpp"
 
 #include "train_kernels.hpp"
@@ -23,238 +23,464 @@ struct GroupedParams {
   int64_t w_stride;         // of W, or dW
   int32_t rows, experts, n, k;     // columns of the product, its K (wgrad: rows of dW in n, columns in k)
   int32_t tiles_m, tiles_n, chunk;
+  int32_t splits;           // K ranges of a tile
+  float* part;              // with ranges: their fp32 products, [splits][rows (wgrad: dW's)][columns]
   int32_t act, f32, accumulate;
 };
 
-// Rows of expert e; whatever ends holds, within 0 .. rows.
-__device__ __forceinline__ void expert_rows(const GroupedParams& p, int e, int32_t* first, int32_t* n) {
-  const int32_t lo = e ? min(max(p.ends[e - 1], 0), p.rows) : 0, hi = min(max(p.ends[e], 0), p.rows);
-  *first = lo;
-  *n = max(hi - lo, 0);
-}
-
-struct RowTile {
-  int32_t expert, first, rows, tj;     // first: row of the tile, rows: of it
+// Each expert's first row, rows, and row tiles of the experts before it.
+struct ExpertTable {
+  int32_t first[kGroupedMaxExperts], rows[kGroupedMaxExperts], before[kGroupedMaxExperts];
+  int32_t total;
+  int32_t order[64];       // of up to 64 experts: those with more rows first
 };
 
-// Tile `id` of the experts' row tiles, expert by expert, column by column.
-template <int BM, int THREADS>
-__device__ __forceinline__ bool row_tile(const GroupedParams& p, int64_t id, int32_t* sh, int tid, RowTile* t) {
-  const int lane = tid & 63, wave = tid >> 6;
-  int32_t first = 0, n = 0;
-  if (tid < p.experts) expert_rows(p, tid, &first, &n);
-  const int32_t tiles = (n + BM - 1) / BM;
-  int32_t sum = tiles;
+// The sum or maximum over a wave's lanes before a lane and its own.
+template <typename F>
+__device__ __forceinline__ int32_t wave_scan(int32_t v, int lane, F&& f) {
 #pragma unroll
   for (int x = 1; x < 64; x <<= 1) {
-    const int32_t other = __shfl_up(sum, x);
-    if (lane >= x) sum += other;
+    const int32_t other = __shfl_up(v, x);
+    if (lane >= x) v = f(v, other);
   }
-  if (lane == 63) sh[wave] = sum;
-  __syncthreads();
-  int32_t before = 0, total = 0;
+  return v;
+}
+
+// The table for tiles of BM rows, made by the first wave; the number of row tiles.
+// Whatever ends holds, the experts' rows lie one behind the other within 0 ..
+// p.rows: the tiles are as many as the launch expects at most, and inside the
+// matrices.
+template <int BM>
+__device__ __forceinline__ int32_t make_table(const GroupedParams& p, ExpertTable& t, int tid) {
+  if (tid < 64) {
+    int32_t end[kGroupedMaxExperts / 64];
 #pragma unroll
-  for (int w = 0; w < THREADS / 64; ++w) {
-    if (w < wave) before += sh[w];
-    total += sh[w];
-  }
-  if (id >= (int64_t)total * p.tiles_n) return false;
-  const int32_t row = (int32_t)(id / p.tiles_n), from = before + sum - tiles;
-  if (row >= from && row < from + tiles) {
-    sh[8] = tid;
-    sh[9] = from;
-    sh[10] = tiles;
-    sh[11] = first;
-    sh[12] = n;
+    for (int i = 0; i < kGroupedMaxExperts / 64; ++i)
+      end[i] = 64 * i + tid < p.experts ? min(max(p.ends[64 * i + tid], 0), p.rows) : 0;
+    int32_t past = 0, before = 0;       // of the experts so far
+#pragma unroll
+    for (int i = 0; i < kGroupedMaxExperts / 64; ++i) {
+      if (64 * i >= p.experts) break;
+      const int32_t to = max(past, wave_scan(end[i], tid, [](int32_t a, int32_t b) { return max(a, b); }));
+      const int32_t prev = __shfl_up(to, 1), first = tid ? prev : past;
+      const int32_t tiles = (to - first + BM - 1) / BM;
+      const int32_t sum = before + wave_scan(tiles, tid, [](int32_t a, int32_t b) { return a + b; });
+      t.first[64 * i + tid] = first;
+      t.rows[64 * i + tid] = to - first;
+      t.before[64 * i + tid] = sum - tiles;
+      past = __shfl(to, 63);
+      before = __shfl(sum, 63);
+    }
+    if (tid == 0) t.total = before;
+    if (p.experts <= 64) {
+      int32_t rank = 0;
+      for (int e = 0; e < p.experts; ++e) rank += t.rows[e] > t.rows[tid] || (t.rows[e] == t.rows[tid] && e < tid);
+      if (tid < p.experts) t.order[rank] = tid;
+    }
   }
   __syncthreads();
-  const int32_t local = (int32_t)(id - (int64_t)sh[9] * p.tiles_n), of = sh[10];
-  const int32_t tj = local / of, ti = local - tj * of;
-  t->expert = __builtin_amdgcn_readfirstlane(sh[8]);
-  t->first = __builtin_amdgcn_readfirstlane(sh[11] + ti * BM);
-  t->rows = __builtin_amdgcn_readfirstlane(min(BM, sh[12] - ti * BM));
-  t->tj = __builtin_amdgcn_readfirstlane(tj);
-  return true;
+  return __builtin_amdgcn_readfirstlane(t.total);
+}
+
+// The last expert with at most `row` row tiles before it: the one that has it.
+__device__ __forceinline__ int32_t expert_of(const ExpertTable& t, int32_t experts, int32_t row, int lane) {
+  int32_t count = 0;
+  for (int e = 0; e < experts; e += 64)
+    count += __popcll(__ballot(e + lane < experts && t.before[e + lane] <= row));
+  return __builtin_amdgcn_readfirstlane(count - 1);
+}
+
+struct RowWork {
+  Side u, v;
+  int32_t steps;
+  int32_t first, rows, tj;     // rows of the matrices, column tile
+  int32_t split;
+};
+
+// A range of a tile's K in fp32: one row of it at `to`, columns < n.
+template <typename T, typename Col>
+__device__ __forceinline__ void partial_row(float* to, const f32x4 (&acc)[T::TN], bool live, int32_t n, int wn, int lane, Col&& col) {
+#pragma unroll
+  for (int nt = 0; nt < T::TN; ++nt) {
+    const int32_t c = col(wn * T::WN + 16 * nt) + 4 * (lane >> 4);
+    if (live && c < n) *reinterpret_cast<f32x4*>(to + c) = acc[nt];
+  }
 }
 
 // Y (and Z) of a tile. A gated tile's columns alternate in groups of 16, gate
 // and up, which a lane holds in neighbouring accumulators.
 template <typename T, bool GATED>
-__device__ __forceinline__ void forward_out(const GroupedParams& p, f32x4 (&acc)[T::TM][T::TN], char* sm, const RowTile& t,
-                                            int tid) {
-  constexpr int BM = T::BM, BN = T::BN, OUT = GATED ? BN / 2 : BN;
-  const int32_t half = p.n / 2;
+__device__ __forceinline__ void forward_out(const GroupedParams& p, const RowWork& t, f32x4 (&acc)[T::TM][T::TN], int tid) {
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / T::WGN, wn = wave % T::WGN;
+  const int32_t half = p.n / 2, cols = GATED ? half : p.n;
   uint16_t* const Y = static_cast<uint16_t*>(p.out) + t.first * p.ld_out;
-  if (p.Z) {
-    const auto z = staged<BM, BN>(sm);
-    each4<T>(tid, [&](int mt, int nt, int r, int c) __attribute__((always_inline)) { *z.at(r, c) = f32_to_bf16x4(acc[mt][nt]); });
-    staged_barrier();
-    tile_out<BM, BN, T::THREADS>(z, p.Z + t.first * p.ld_z, p.ld_z, t.rows, tid, [&](int c) {
-      if constexpr (!GATED) return t.tj * BN + 8 * c < p.n ? t.tj * BN + 8 * c : -1;
-      const int32_t n = t.tj * OUT + (c >> 2) * 16 + (c & 1) * 8;
-      return n < half ? n + (c & 2 ? half : 0) : -1;
-    });
-    staged_barrier();
-  }
-  const auto y = staged<BM, OUT>(sm);
+  uint16_t* const Z = p.Z + t.first * p.ld_z;
   const ActCoef k = act_coef(p.act);
+  const int at = pair_column(lane);
   with_act(p.act, [&](auto cls) __attribute__((always_inline)) {
     constexpr int C = decltype(cls)::value;
-    each4<T>(tid, [&](int mt, int nt, int r, int c) __attribute__((always_inline)) {
-      if constexpr (GATED) {
-        if (nt & 1) return;
-        f32x4 o;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[j] = act_value<C>(k, acc[mt][nt][j]) * acc[mt][nt + 1][j];
-        *y.at(r, (c >> 1 & ~15) + (c & 15)) = f32_to_bf16x4(o);
-      } else {
-        f32x4 o;
+    for (int mt = 0; mt < T::TM; ++mt) {
+      const int r = T::row(wm, mt) + (lane & 15);
+      if (T::row(wm, mt) >= t.rows) break;
+      const bool live = r < t.rows;
+      if (p.Z) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[j] = act_value<C>(k, acc[mt][nt][j]);
-        *y.at(r, c) = f32_to_bf16x4(o);
+        for (int nt = 0; nt < T::TN; nt += 2) {
+          const uint4 z = pair_up(f32_to_bf16x4(acc[mt][nt]), f32_to_bf16x4(acc[mt][nt + 1]));
+          const int32_t c = wn * T::WN + 16 * nt;
+          if constexpr (GATED) {      // even 16s of lanes hold the gate's columns, odd ones the up columns
+            const int32_t n = t.tj * (T::BN / 2) + c / 2 + 8 * (lane >> 5);
+            if (live && n < half) *reinterpret_cast<uint4*>(Z + r * p.ld_z + n + (lane & 16 ? half : 0)) = z;
+          } else {
+            const int32_t n = t.tj * T::BN + c + at;
+            if (live && n < p.n) *reinterpret_cast<uint4*>(Z + r * p.ld_z + n) = z;
+          }
+        }
       }
-    });
+      uint2 y[T::TN];
+#pragma unroll
+      for (int nt = 0; nt < T::TN; ++nt) {
+        if (GATED && (nt & 1)) continue;
+        f32x4 o;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          o[j] = act_value<C>(k, acc[mt][nt][j]);
+          if constexpr (GATED) o[j] *= acc[mt][nt + 1][j];
+        }
+        y[GATED ? nt / 2 : nt] = f32_to_bf16x4(o);
+      }
+      constexpr int TY = GATED ? T::TN / 2 : T::TN;
+      static_assert(TY % 2 == 0, "pairs");
+#pragma unroll
+      for (int nt = 0; nt < TY; nt += 2) {
+        const int32_t n = (t.tj * T::BN + wn * T::WN) / (GATED ? 2 : 1) + 16 * nt + at;
+        const uint4 v = pair_up(y[nt], y[nt + 1]);
+        if (live && n < cols) *reinterpret_cast<uint4*>(Y + r * p.ld_out + n) = v;
+      }
+    }
   });
-  staged_barrier();
-  const int32_t cols = GATED ? half : p.n;
-  tile_out<BM, OUT, T::THREADS>(y, Y, p.ld_out, t.rows, tid,
-                                [&](int c) { return t.tj * OUT + 8 * c < cols ? t.tj * OUT + 8 * c : -1; });
 }
 
 // dX or dZ of a tile. Z's gate columns come first, then its up columns, and so
 // dZ's.
 template <typename T, bool GATED>
-__device__ __forceinline__ void grad_out(const GroupedParams& p, f32x4 (&acc)[T::TM][T::TN], char* sm, const RowTile& t,
-                                         int tid) {
-  constexpr int BM = T::BM, BN = T::BN;
-  const auto s = staged<BM, BN>(sm);
+__device__ __forceinline__ void grad_out(const GroupedParams& p, const RowWork& t, f32x4 (&acc)[T::TM][T::TN], int tid) {
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / T::WGN, wn = wave % T::WGN;
   uint16_t* const out = static_cast<uint16_t*>(p.out) + t.first * p.ld_out;
   const uint16_t* const Z = p.Z + t.first * p.ld_z;
-  const auto col = [&](int c) { return t.tj * BN + 8 * c < p.n ? t.tj * BN + 8 * c : -1; };
-  const auto up_col = [&](int c) { return t.tj * BN + 8 * c < p.n ? p.n + t.tj * BN + 8 * c : -1; };
   const ActCoef k = act_coef(p.act);
-  uint2 up[T::TM][T::TN];
-  if constexpr (GATED) {
-    tile_in<BM, BN, T::THREADS>(s, Z, p.ld_z, t.rows, tid, up_col);
-    staged_barrier();
-    each4<T>(tid, [&](int mt, int nt, int r, int c) __attribute__((always_inline)) { up[mt][nt] = *s.at(r, c); });
-    staged_barrier();
-  }
-  if (GATED || p.act != ACT_NONE) {
-    tile_in<BM, BN, T::THREADS>(s, Z, p.ld_z, t.rows, tid, col);
-    staged_barrier();
-  }
+  const int32_t n0 = t.tj * T::BN + wn * T::WN + pair_column(lane);
   with_act(p.act, [&](auto cls) __attribute__((always_inline)) {
     constexpr int C = decltype(cls)::value;
-    each4<T>(tid, [&](int mt, int nt, int r, int c) __attribute__((always_inline)) {
-      const f32x4 d = acc[mt][nt];
-      f32x4 o = d;
-      if constexpr (GATED || C != ACT_CLASS_NONE) {
-        const f32x4 z = bf16x4_to_f32(*s.at(r, c));
-        f32x4 u, w;
-        if constexpr (GATED) u = bf16x4_to_f32(up[mt][nt]);
+    constexpr bool kThrough = GATED || C != ACT_CLASS_NONE;
+    constexpr int TP = T::TN / 2;
+    // Z of one row of 16x16 tiles is on its way while the one before is worked on
+    uint4 zg[2][TP], zu[2][TP];
+    auto fetch = [&](int mt) __attribute__((always_inline)) {
+      const int r = T::row(wm, mt) + (lane & 15);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float slope;
-          const float value = act_value_grad<C>(k, z[j], &slope);
-          if constexpr (GATED) {
-            w[j] = d[j] * value;
-            o[j] = d[j] * u[j] * slope;
-          } else {
-            o[j] = d[j] * slope;
-          }
+      for (int i = 0; i < TP; ++i) {
+        const int32_t n = n0 + 32 * i;
+        zg[mt & 1][i] = zu[mt & 1][i] = make_uint4(0, 0, 0, 0);
+        if (r < t.rows && n < p.n) {
+          zg[mt & 1][i] = *reinterpret_cast<const uint4*>(Z + r * p.ld_z + n);
+          if constexpr (GATED) zu[mt & 1][i] = *reinterpret_cast<const uint4*>(Z + r * p.ld_z + p.n + n);
         }
-        if constexpr (GATED) up[mt][nt] = f32_to_bf16x4(w);
       }
-      *s.at(r, c) = f32_to_bf16x4(o);
-    });
+    };
+    if constexpr (kThrough) fetch(0);
+#pragma unroll
+    for (int mt = 0; mt < T::TM; ++mt) {
+      if (T::row(wm, mt) >= t.rows) break;
+      const int r = T::row(wm, mt) + (lane & 15);
+      if (kThrough && mt + 1 < T::TM) fetch(mt + 1);
+#pragma unroll
+      for (int i = 0; i < TP; ++i) {
+        uint2 o[2], w[2], g[2], u[2];
+        if constexpr (kThrough) pair_down(zg[mt & 1][i], &g[0], &g[1]);
+        if constexpr (GATED) pair_down(zu[mt & 1][i], &u[0], &u[1]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const f32x4 d = acc[mt][2 * i + h];
+          f32x4 x = d, y;
+          if constexpr (kThrough) {
+            const f32x4 z = bf16x4_to_f32(g[h]);
+            f32x4 up;
+            if constexpr (GATED) up = bf16x4_to_f32(u[h]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              float slope;
+              const float value = act_value_grad<C>(k, z[j], &slope);
+              if constexpr (GATED) {
+                y[j] = d[j] * value;
+                x[j] = d[j] * up[j] * slope;
+              } else {
+                x[j] = d[j] * slope;
+              }
+            }
+            if constexpr (GATED) w[h] = f32_to_bf16x4(y);
+          }
+          o[h] = f32_to_bf16x4(x);
+        }
+        const int32_t n = n0 + 32 * i;
+        const uint4 a = pair_up(o[0], o[1]);
+        if (r < t.rows && n < p.n) *reinterpret_cast<uint4*>(out + r * p.ld_out + n) = a;
+        if constexpr (GATED) {
+          const uint4 b = pair_up(w[0], w[1]);
+          if (r < t.rows && n < p.n) *reinterpret_cast<uint4*>(out + r * p.ld_out + p.n + n) = b;
+        }
+      }
+    }
   });
-  staged_barrier();
-  tile_out<BM, BN, T::THREADS>(s, out, p.ld_out, t.rows, tid, col);
-  if constexpr (GATED) {
-    staged_barrier();
-    each4<T>(tid, [&](int mt, int nt, int r, int c) __attribute__((always_inline)) { *s.at(r, c) = up[mt][nt]; });
-    staged_barrier();
-    tile_out<BM, BN, T::THREADS>(s, out, p.ld_out, t.rows, tid, up_col);
-  }
 }
 
-template <int BM, int BN, int NS, int WGN, bool GRAD, bool GATED>
-__global__ void __launch_bounds__(512, NS * (BM + BN) * 128 <= 80 * 1024 ? 4 : 2) grouped_rows_kernel(GroupedParams p) {
+template <typename T, bool GRAD, bool GATED>
+__global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) grouped_rows_kernel(GroupedParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  using T = ProductTile<BM, BN, true, !GRAD, NS, WGN>;
-  __shared__ __attribute__((aligned(1024))) char sm[T::LDS];
-  const int tid = threadIdx.x;
-  RowTile t;
-  if (!row_tile<BM, 512>(p, dealt_tile(p.chunk), reinterpret_cast<int32_t*>(sm), tid, &t)) return;
-  __syncthreads();
-  const uint16_t* W = p.V + t.expert * p.w_stride;
-  const Side u{p.U + t.first * p.ldu, p.ldu, t.rows, p.k};
-  Side v;
-  // a gated tile's V rows: BN / 2 gate rows from row `first` on and the up rows half of the weight later
+  __shared__ __attribute__((aligned(65536))) char sm[T::LDS];
+  __shared__ ExpertTable table;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int32_t tiles = make_table<T::BM>(p, table, tid) * p.tiles_n;
+  // a gated tile's V rows: BN / 2 gate rows from row `from` on and the up rows half of the weight later
   constexpr bool kPairs = GATED && !GRAD;
-  const int32_t first = kPairs ? t.tj * (BN / 2) : t.tj * BN;
-  if constexpr (GRAD) v = Side{W + first, p.ldv, min(BN, p.n - first), p.k};
-  else v = Side{W + first * p.ldv, p.ldv, kPairs ? p.n - first : min(BN, p.n - first), p.k};
   const int32_t half = p.n / 2;
-  f32x4 acc[T::TM][T::TN];
-  product<T>(u, v, 0, (p.k + 63) / 64, acc, sm, tid, [&](int r) {
-    if constexpr (!kPairs) return r;
-    return (r >> 5) * 16 + (r & 15) + (r & 16 ? half : 0);
-  });
-  if constexpr (GRAD) grad_out<T, GATED>(p, acc, sm, t, tid);
-  else forward_out<T, GATED>(p, acc, sm, t, tid);
+  product_tiles<T, RowWork>(
+      p.ldu, p.ldv, sm, tid,
+      [&](int i, RowWork* w) __attribute__((always_inline)) {
+        int32_t id = dealt_tile(i, p.chunk);
+        if (id >= tiles * p.splits) return false;
+        w->split = 0;
+        int32_t k0 = 0, k = p.k;
+        if (p.splits > 1) {
+          w->split = __builtin_amdgcn_readfirstlane(id / tiles);
+          id -= w->split * tiles;
+          const int32_t per = ((p.k + 63) / 64 + p.splits - 1) / p.splits * 64;
+          k0 = __builtin_amdgcn_readfirstlane(w->split * per);
+          k = __builtin_amdgcn_readfirstlane(max(min(per, p.k - k0), 0));
+        }
+        const int32_t e = expert_of(table, p.experts, __builtin_amdgcn_readfirstlane(id / p.tiles_n), lane);
+        const int32_t rows = __builtin_amdgcn_readfirstlane(table.rows[e]), of = (rows + T::BM - 1) / T::BM;
+        const int32_t local = id - __builtin_amdgcn_readfirstlane(table.before[e]) * p.tiles_n;
+        const int32_t tj = __builtin_amdgcn_readfirstlane(local / of), ti = local - tj * of;
+        w->tj = tj;
+        w->first = __builtin_amdgcn_readfirstlane(table.first[e]) + ti * T::BM;
+        w->rows = min(T::BM, rows - ti * T::BM);
+        w->steps = product_steps<T>(k);
+        w->u = Side{p.U + w->first * p.ldu + k0, w->rows, k};
+        const int32_t from = kPairs ? tj * (T::BN / 2) : tj * T::BN;
+        const uint16_t* W = p.V + e * p.w_stride;
+        w->v = GRAD ? Side{W + k0 * p.ldv + from, min(T::BN, p.n - from), k}
+                    : Side{W + from * p.ldv + k0, kPairs ? p.n - from : min(T::BN, p.n - from), k};
+        return true;
+      },
+      [&](int r) __attribute__((always_inline)) { return kPairs ? (r >> 5) * 16 + (r & 15) + (r & 16 ? half : 0) : r; },
+      [&](const RowWork& w, f32x4 (&acc)[T::TM][T::TN]) __attribute__((always_inline)) {
+        if (p.part) {
+          const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / T::WGN, wn = wave % T::WGN;
+#pragma unroll
+          for (int mt = 0; mt < T::TM; ++mt) {
+            const int r = T::row(wm, mt) + (lane & 15);
+            float* const to = p.part + ((int64_t)w.split * p.rows + w.first + r) * p.n;
+            if constexpr (kPairs) {
+              // tile columns alternate, 16 gate and 16 up ones
+              partial_row<T>(to, acc[mt], r < w.rows, p.n, wn, lane, [&](int c) {
+                const int32_t n = w.tj * (T::BN / 2) + c / 2 - (c & 16) / 2;
+                return n >= half ? p.n : n + (c & 16 ? half : 0);
+              });
+            } else {
+              partial_row<T>(to, acc[mt], r < w.rows, p.n, wn, lane, [&](int c) { return w.tj * T::BN + c; });
+            }
+          }
+          return;
+        }
+        if constexpr (GRAD) grad_out<T, GATED>(p, w, acc, tid);
+        else forward_out<T, GATED>(p, w, acc, tid);
+      });
 #endif
 }
+
+struct WgradWork {
+  Side u, v;
+  int32_t steps;
+  int32_t m, n;                // of the tile
+  int32_t row, col;            // its corner, row of all experts' dW
+  int32_t split, expert;
+};
 
 // dW tiles: rows of dW from dY's columns, columns from X's, K over the expert's rows.
-template <int BM, int BN, int NS, int WGN>
-__global__ void __launch_bounds__(512, NS * (BM + BN) * 128 <= 80 * 1024 ? 4 : 2) grouped_wgrad_kernel(GroupedParams p) {
+// What is done with one, apart, since together they take registers that the 256x256
+// tiles' loop needs.
+enum WgradOut { WGRAD_BF16, WGRAD_F32, WGRAD_ANY };
+template <typename T, WgradOut OUT>
+__global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) grouped_wgrad_kernel(GroupedParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  using T = ProductTile<BM, BN, false, false, NS, WGN>;
-  __shared__ __attribute__((aligned(1024))) char sm[T::LDS];
-  const int tid = threadIdx.x;
-  const int64_t id = dealt_tile(p.chunk);
+  __shared__ __attribute__((aligned(65536))) char sm[T::LDS];
+  __shared__ ExpertTable table;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  make_table<T::BM>(p, table, tid);
   const int32_t per = p.tiles_m * p.tiles_n;
-  if (id >= (int64_t)per * p.experts) return;
-  const int32_t e = __builtin_amdgcn_readfirstlane((int32_t)(id / per)), local = (int32_t)(id - (int64_t)e * per);
-  const int32_t tj = __builtin_amdgcn_readfirstlane(local / p.tiles_m), ti = local - tj * p.tiles_m;
-  int32_t first, rows;
-  expert_rows(p, e, &first, &rows);
-  first = __builtin_amdgcn_readfirstlane(first);
-  rows = __builtin_amdgcn_readfirstlane(rows);
-  const int32_t m = min(BM, p.n - ti * BM), n = min(BN, p.k - tj * BN);
-  f32x4 acc[T::TM][T::TN];
-  if (rows > 0) {
-    product<T>(Side{p.U + first * p.ldu + ti * BM, p.ldu, m, rows}, Side{p.V + first * p.ldv + tj * BN, p.ldv, n, rows}, 0,
-               (rows + 63) / 64, acc, sm, tid, [](int r) { return r; });
-  } else {
-    if (p.accumulate) return;
+  const int32_t tiles = per * p.experts;
+  product_tiles<T, WgradWork>(
+      p.ldu, p.ldv, sm, tid,
+      [&](int i, WgradWork* w) __attribute__((always_inline)) {
+        int32_t id = dealt_tile(i, p.chunk);
+        if (id >= tiles * p.splits) return false;
+        w->split = __builtin_amdgcn_readfirstlane(p.splits > 1 ? id / tiles : 0);
+        id -= w->split * tiles;
+        // few experts' tiles are few for a workgroup: the longest first
+        const int32_t nth = __builtin_amdgcn_readfirstlane(id / per), local = id - nth * per;
+        const int32_t e = p.experts <= 64 ? __builtin_amdgcn_readfirstlane(table.order[nth]) : nth;
+        const int32_t tj = __builtin_amdgcn_readfirstlane(local / p.tiles_m), ti = local - tj * p.tiles_m;
+        int32_t first = __builtin_amdgcn_readfirstlane(table.first[e]), rows = __builtin_amdgcn_readfirstlane(table.rows[e]);
+        if (p.splits > 1) {
+          const int32_t range = ((rows + 63) / 64 + p.splits - 1) / p.splits * 64;
+          const int32_t k0 = __builtin_amdgcn_readfirstlane(min(w->split * range, rows));
+          first += k0;
+          rows = __builtin_amdgcn_readfirstlane(min(range, rows - k0));
+        }
+        w->m = min(T::BM, p.n - ti * T::BM);
+        w->n = min(T::BN, p.k - tj * T::BN);
+        w->steps = product_steps<T>(rows);
+        w->u = Side{p.U + first * p.ldu + ti * T::BM, w->m, rows};
+        w->v = Side{p.V + first * p.ldv + tj * T::BN, w->n, rows};
+        w->row = ti * T::BM;
+        w->col = tj * T::BN;
+        w->expert = e;
+        return true;
+      },
+      [](int r) { return r; },
+      [&](const WgradWork& w, f32x4 (&acc)[T::TM][T::TN]) __attribute__((always_inline)) {
+        const int wm = wave / T::WGN, wn = wave % T::WGN;
+        const int64_t corner = w.expert * p.w_stride + (int64_t)w.row * p.ld_out + w.col;
 #pragma unroll
-    for (int i = 0; i < T::TM; ++i)
+        for (int mt = 0; mt < T::TM; ++mt) {
+          const int r = T::row(wm, mt) + (lane & 15);
+          const bool live = r < w.m;
+          if (OUT == WGRAD_ANY && p.part) {
+            float* const to = p.part + (((int64_t)w.split * p.experts + w.expert) * p.n + w.row + r) * p.k + w.col;
+            partial_row<T>(to, acc[mt], live, w.n, wn, lane, [](int c) { return c; });
+            continue;
+          }
+          if (OUT == WGRAD_F32 || (OUT == WGRAD_ANY && p.f32)) {
+            float* const to = static_cast<float*>(p.out) + corner + r * p.ld_out;
 #pragma unroll
-      for (int j = 0; j < T::TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int nt = 0; nt < T::TN; ++nt) {
+              const int32_t c = wn * T::WN + 16 * nt + 4 * (lane >> 4);
+              if (!live || c >= w.n) continue;
+              f32x4* at = reinterpret_cast<f32x4*>(to + c);
+              *at = OUT == WGRAD_ANY && p.accumulate ? *at + acc[mt][nt] : acc[mt][nt];
+            }
+          } else {
+            uint16_t* const to = static_cast<uint16_t*>(p.out) + corner + r * p.ld_out;
+#pragma unroll
+            for (int nt = 0; nt < T::TN; nt += 2) {
+              const int32_t c = wn * T::WN + 16 * nt + pair_column(lane);
+              f32x4 a = acc[mt][nt], b = acc[mt][nt + 1];
+              if (OUT == WGRAD_ANY && p.accumulate) {
+                uint2 x, y;
+                pair_down(live && c < w.n ? *reinterpret_cast<const uint4*>(to + c) : make_uint4(0, 0, 0, 0), &x, &y);
+                a += bf16x4_to_f32(x);
+                b += bf16x4_to_f32(y);
+              }
+              const uint4 v = pair_up(f32_to_bf16x4(a), f32_to_bf16x4(b));
+              if (live && c < w.n) *reinterpret_cast<uint4*>(to + c) = v;
+            }
+          }
+        }
+      });
+#endif
+}
+
+// The ranges' sums in order and what their product's finish does, eight columns a
+// thread: FORWARD of Y, GRAD of dX, WGRAD of dW.
+template <int DIRECTION, bool GATED>
+__global__ void __launch_bounds__(256) grouped_sum_kernel(GroupedParams p) {
+  constexpr bool kForward = DIRECTION == GROUPED_FORWARD;
+  const int32_t cols = DIRECTION == GROUPED_WGRAD ? p.k : p.n, half = p.n / 2, out = kForward && GATED ? half : cols;
+  const int32_t width = out / 8;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, all = DIRECTION == GROUPED_WGRAD ? (int64_t)p.experts * p.n : p.rows;
+  const int64_t r = at / width;
+  const int32_t c = (int32_t)(at - r * width) * 8;
+  if (r >= all) return;
+  if constexpr (DIRECTION != GROUPED_WGRAD) {
+    // rows behind the last expert's were not computed and stay as they are
+    int32_t end = 0;
+    for (int e = 0; e < p.experts; ++e) end = max(end, p.ends[e]);
+    if (r >= end) return;
   }
-  const int64_t corner = e * p.w_stride + (int64_t)ti * BM * p.ld_out + tj * BN;
-  if (p.f32) {
-    float* const to = static_cast<float*>(p.out) + corner;
-    each4<T>(tid, [&](int mt, int nt, int r, int c) __attribute__((always_inline)) {
-      if (r >= m || c >= n) return;
-      f32x4* at = reinterpret_cast<f32x4*>(to + r * p.ld_out + c);
-      *at = p.accumulate ? *at + acc[mt][nt] : acc[mt][nt];
-    });
+  const auto sum8 = [&](int32_t col, f32x4 (&v)[2]) {
+    v[0] = v[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const float* from = p.part + r * cols + col;
+#pragma unroll 4
+    for (int32_t i = 0; i < p.splits; ++i) {
+      v[0] += reinterpret_cast<const f32x4*>(from + i * all * cols)[0];
+      v[1] += reinterpret_cast<const f32x4*>(from + i * all * cols)[1];
+    }
+  };
+  const auto store8 = [](uint16_t* to, const f32x4 (&v)[2]) {
+    const uint2 a = f32_to_bf16x4(v[0]), b = f32_to_bf16x4(v[1]);
+    *reinterpret_cast<uint4*>(to) = make_uint4(a.x, a.y, b.x, b.y);
+  };
+  const auto load8 = [](const uint16_t* from, f32x4 (&v)[2]) {
+    const uint4 a = *reinterpret_cast<const uint4*>(from);
+    v[0] = bf16x4_to_f32(make_uint2(a.x, a.y));
+    v[1] = bf16x4_to_f32(make_uint2(a.z, a.w));
+  };
+  f32x4 v[2], u[2];
+  sum8(c, v);
+  if constexpr (DIRECTION == GROUPED_WGRAD) {
+    const int64_t e = r / p.n, to = e * p.w_stride + (r - e * p.n) * p.ld_out + c;
+    if (p.f32) {
+      f32x4* const dst = reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + to);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) dst[i] = p.accumulate ? dst[i] + v[i] : v[i];
+    } else {
+      uint16_t* const dst = static_cast<uint16_t*>(p.out) + to;
+      if (p.accumulate) {
+        load8(dst, u);
+        v[0] += u[0];
+        v[1] += u[1];
+      }
+      store8(dst, v);
+    }
     return;
   }
-  uint16_t* const to = static_cast<uint16_t*>(p.out) + corner;
-  const auto s = staged<BM, BN>(sm);
-  each4<T>(tid, [&](int mt, int nt, int r, int c) __attribute__((always_inline)) {
-    f32x4 o = acc[mt][nt];
-    if (p.accumulate && r < m && c < n) o += bf16x4_to_f32(*reinterpret_cast<const uint2*>(to + r * p.ld_out + c));
-    *s.at(r, c) = f32_to_bf16x4(o);
+  const ActCoef k = act_coef(p.act);
+  uint16_t* const to = static_cast<uint16_t*>(p.out) + r * p.ld_out + c;
+  uint16_t* const Z = p.Z + r * p.ld_z + c;
+  with_act(p.act, [&](auto cls) __attribute__((always_inline)) {
+    constexpr int C = decltype(cls)::value;
+    if constexpr (kForward) {
+      if constexpr (GATED) sum8(half + c, u);
+      if (p.Z) {
+        store8(Z, v);
+        if constexpr (GATED) store8(Z + half, u);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[i >> 2][i & 3] = act_value<C>(k, v[i >> 2][i & 3]);
+        if constexpr (GATED) v[i >> 2][i & 3] *= u[i >> 2][i & 3];
+      }
+    } else if constexpr (GATED || C != ACT_CLASS_NONE) {
+      f32x4 z[2], y[2];
+      load8(Z, z);
+      if constexpr (GATED) load8(Z + p.n, u);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float slope;
+        const float d = v[i >> 2][i & 3], value = act_value_grad<C>(k, z[i >> 2][i & 3], &slope);
+        if constexpr (GATED) {
+          y[i >> 2][i & 3] = d * value;
+          v[i >> 2][i & 3] = d * u[i >> 2][i & 3] * slope;
+        } else {
+          v[i >> 2][i & 3] = d * slope;
+        }
+      }
+      if constexpr (GATED) store8(to + p.n, y);
+    }
+    store8(to, v);
   });
-  staged_barrier();
-  tile_out<BM, BN, T::THREADS>(s, to, p.ld_out, m, tid, [&](int c) { return 8 * c < n ? 8 * c : -1; });
-#endif
 }
 
 }  // namespace
@@ -276,30 +502,55 @@ hipError_t launch_grouped(const GroupedShape& s, const GroupedCall& c, int direc
   p.tiles_m = f.tiles_m;
   p.tiles_n = f.tiles_n;
   p.chunk = f.chunk;
+  p.splits = f.splits;
+  p.part = f.splits > 1 ? static_cast<float*>(ws) : nullptr;
   p.act = s.act;
   p.f32 = c.f32;
   p.accumulate = c.accumulate;
-  const dim3 grid((unsigned)f.workgroups), block(512);
+  p.n = (int32_t)(direction == GROUPED_GRAD ? s.in : s.out);
+  p.k = (int32_t)(direction == GROUPED_GRAD ? s.out : s.in);
+  p.ldv = s.w_ld;
   if (direction == GROUPED_WGRAD) {
     p.ldv = c.b_ld;
     p.ld_out = s.w_ld;
-    p.n = (int32_t)s.out;
-    p.k = (int32_t)s.in;
-    hipLaunchKernelGGL((grouped_wgrad_kernel<128, 128, 2, 4>), grid, block, 0, stream, p);
-    return hipGetLastError();
   }
-  p.ldv = s.w_ld;
-  if (direction == GROUPED_FORWARD) {
-    p.n = (int32_t)s.out;
-    p.k = (int32_t)s.in;
-    if (s.gated) hipLaunchKernelGGL((grouped_rows_kernel<128, 128, 2, 4, false, true>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((grouped_rows_kernel<128, 128, 2, 4, false, false>), grid, block, 0, stream, p);
+  const unsigned groups = (unsigned)f.workgroups;
+  const auto rows = [&](auto tile, auto grad) {
+    using T = decltype(tile);
+    constexpr bool G = decltype(grad)::value;
+    if (s.gated) hipLaunchKernelGGL((grouped_rows_kernel<T, G, true>), dim3(groups), dim3(T::THREADS), 0, stream, p);
+    else hipLaunchKernelGGL((grouped_rows_kernel<T, G, false>), dim3(groups), dim3(T::THREADS), 0, stream, p);
+  };
+  const auto wgrad = [&](auto tile) {
+    using T = decltype(tile);
+    if (p.accumulate || p.part) hipLaunchKernelGGL((grouped_wgrad_kernel<T, WGRAD_ANY>), dim3(groups), dim3(T::THREADS), 0, stream, p);
+    else if (p.f32) hipLaunchKernelGGL((grouped_wgrad_kernel<T, WGRAD_F32>), dim3(groups), dim3(T::THREADS), 0, stream, p);
+    else hipLaunchKernelGGL((grouped_wgrad_kernel<T, WGRAD_BF16>), dim3(groups), dim3(T::THREADS), 0, stream, p);
+  };
+  const std::true_type yes;
+  const std::false_type no;
+  if (direction == GROUPED_WGRAD) {
+    if (f.tile_n == 256) wgrad(ProductTile<256, 256, false, false, 2, 8, 4>{});
+    else wgrad(ProductTile<128, 128, false, false, 2, 8, 2>{});
+  } else if (direction == GROUPED_FORWARD) {
+    if (f.tile_m == 256) rows(ProductTile<256, 256, true, true, 2, 8, 4, true>{}, no);
+    else if (f.tile_m == 128) rows(ProductTile<128, 128, true, true, 2, 8, 2, true>{}, no);
+    else rows(ProductTile<64, 128, true, true, 2, 8, 2, true>{}, no);
   } else {
-    p.n = (int32_t)s.in;
-    p.k = (int32_t)s.out;
-    if (s.gated) hipLaunchKernelGGL((grouped_rows_kernel<128, 128, 2, 4, true, true>), grid, block, 0, stream, p);
-    else hipLaunchKernelGGL((grouped_rows_kernel<128, 128, 2, 4, true, false>), grid, block, 0, stream, p);
+    if (f.tile_m == 256) rows(ProductTile<256, 256, true, false, 2, 8, 4, true>{}, yes);
+    else if (f.tile_m == 128) rows(ProductTile<128, 128, true, false, 2, 8, 2, true>{}, yes);
+    else rows(ProductTile<64, 128, true, false, 2, 8, 2, true>{}, yes);
   }
+  if (hipError_t e = hipGetLastError()) return e;
+  if (f.splits == 1) return hipSuccess;
+  const int64_t rows8 = direction == GROUPED_WGRAD ? (int64_t)p.experts * p.n : p.rows;
+  const int64_t cols8 = direction == GROUPED_WGRAD ? p.k / 8 : direction == GROUPED_FORWARD && s.gated ? p.n / 16 : p.n / 8;
+  const dim3 sums((unsigned)((rows8 * cols8 + 255) / 256));
+  if (direction == GROUPED_WGRAD) hipLaunchKernelGGL((grouped_sum_kernel<GROUPED_WGRAD, false>), sums, dim3(256), 0, stream, p);
+  else if (direction == GROUPED_FORWARD && s.gated) hipLaunchKernelGGL((grouped_sum_kernel<GROUPED_FORWARD, true>), sums, dim3(256), 0, stream, p);
+  else if (direction == GROUPED_FORWARD) hipLaunchKernelGGL((grouped_sum_kernel<GROUPED_FORWARD, false>), sums, dim3(256), 0, stream, p);
+  else if (s.gated) hipLaunchKernelGGL((grouped_sum_kernel<GROUPED_GRAD, true>), sums, dim3(256), 0, stream, p);
+  else hipLaunchKernelGGL((grouped_sum_kernel<GROUPED_GRAD, false>), sums, dim3(256), 0, stream, p);
   return hipGetLastError();
 }
 
