@@ -634,7 +634,8 @@ typedef struct ccl_adamw_tensor {
  * returns), and the values that 8-bit moments stand for (m, v: n elements of
  * fp32 or bf16, which holds them exactly while they are normal; either may be
  * NULL). Buffers may start at any element; whole 16 bytes (8 for 8-bit moments)
- * are faster. One launch for every 48 tensors of a kind, no workspace.
+ * are faster. One launch for every 68 tensors of a kind (54 with 8-bit moments),
+ * no workspace.
  * Errors: CCL_ERR_INVALID_ARG (NULL argument, negative sizes or sizes above 2^40,
  * an unknown type, moment_bits other than 8 and 32, betas outside [0, 1), eps
  * negative or not finite, lr or weight_decay not finite, step below 1 without

@@ -30,8 +30,9 @@ int64_t resident(int64_t tiles, int per_cu) { return std::min<int64_t>(up(std::m
 //            uneven), 65536 372 / 369, 8192 over one of 4096 -> 4096 235 / 288
 //   wgrad    32768 over 128 of 2048 -> 1536 387 / 451, 8192 over one 223 / 288, 65536
 //            over 4 of 256 -> 256 334 / 181 (4 tiles an expert)
-// 64x128 ones where few rows come to an expert: 8 rows 24.6 us against 26.6, 64 rows
-// 68.2 / 71.2 (forward as above), at 32 rows an expert 212 / 195.
+// 64x128 ones, with a third stage on its way, where few rows come to an expert (against
+// 128x128): 64 rows 58 / 71 (forward as above), 1024 165 / 187, 8192 199 / 230, 12000
+// 220 / 223, its grad 133 / 126.
 GroupedForm grouped_form(const GroupedShape& s, int64_t rows, int direction) {
   GroupedForm f;
   const bool wgrad = direction == GROUPED_WGRAD;
@@ -46,7 +47,7 @@ GroupedForm grouped_form(const GroupedShape& s, int64_t rows, int direction) {
                                  (direction == GROUPED_FORWARD && mean >= 192 && large >= 512))
     f.tile_m = f.tile_n = 256;
   else {
-    f.tile_m = wgrad || mean >= 24 ? 128 : 64;
+    f.tile_m = wgrad || mean >= 80 ? 128 : 64;
     f.tile_n = 128;
   }
   const int per_cu = f.tile_m == 256 ? 1 : 2;

@@ -59,9 +59,8 @@ ProductForm vocab_dx_form(const VocabShape& s, int64_t tokens);
 ProductForm vocab_dw_form(const VocabShape& s, int64_t tokens);
 
 // ---- AdamW ----
-constexpr int kAdamwTensors = 48;             // of a launch: their table is a kernel argument of 4 KB at most
+constexpr int kAdamwTensors[2] = {68, 54};    // of a launch (moments of 32, 8 bits): their table is a kernel argument
 constexpr int kAdamwBlock = 128;              // elements of 8-bit moments that share a scale
-constexpr int64_t kAdamwChunk = 8192;         // elements of a workgroup
 
 // 1 - beta^step and its like, the same bits on the host and the device: by
 // squaring, in double.

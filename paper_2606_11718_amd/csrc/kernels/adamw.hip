@@ -16,6 +16,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "train_kernels.hpp"
 
@@ -25,9 +26,23 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
+// A tensor in the kernel's arguments, 4 KB of which hold kAdamwTensors.
+struct Entry32 {
+  void* param;
+  const void* grad;
+  void *m, *v;
+  uint16_t* copy;
+  int64_t n;
+  float weight_decay;
+  int32_t first;           // its first workgroup
+};
+struct Entry8 : Entry32 {
+  uint8_t *m_scale, *v_scale;
+};
+template <bool BITS8>
 struct AdamwTable {
-  AdamwTensor t[kAdamwTensors];
-  int32_t first[kAdamwTensors];    // the tensor's first workgroup
+  static constexpr int kTensors = kAdamwTensors[BITS8];
+  std::conditional_t<BITS8, Entry8, Entry32> t[kTensors];
 };
 struct AdamwParams {
   const float *grad_scale, *lr_ptr;
@@ -36,7 +51,7 @@ struct AdamwParams {
   int64_t step;
   float b1, c1, b2, c2, eps;       // c: 1 - b
   float rate, root;                // lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
-  int32_t count;
+  int32_t count, chunk;            // elements of a workgroup
 };
 
 // The same 32 bits for the same element and step.
@@ -203,18 +218,18 @@ __device__ __forceinline__ uint2 encode8(const float (&x)[8], int top, const uin
 __device__ __forceinline__ bool aligned_to(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 template <bool P16, bool G16, bool BITS8>
-__global__ void __launch_bounds__(256) adamw_kernel(AdamwTable table, AdamwParams a) {
+__global__ void __launch_bounds__(256) adamw_kernel(AdamwTable<BITS8> table, AdamwParams a) {
 // Products and sums round one by one, as their formulas say: the 8-bit codes are
 // the same wherever they are computed.
 #pragma clang fp contract(off)
   int lo = 0, hi = a.count - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
-    if (table.first[mid] <= (int32_t)blockIdx.x) lo = mid;
+    if (table.t[mid].first <= (int32_t)blockIdx.x) lo = mid;
     else hi = mid - 1;
   }
-  const AdamwTensor& t = table.t[lo];
-  const int64_t n = t.n, from = (int64_t)((int32_t)blockIdx.x - table.first[lo]) * kAdamwChunk;
+  const auto& t = table.t[lo];
+  const int64_t n = t.n, from = (int64_t)((int32_t)blockIdx.x - t.first) * a.chunk;
   const float gs = a.grad_scale ? *a.grad_scale : 1.f;
   if (!(__builtin_fabsf(gs) < INFINITY)) return;      // a step to be left out
   double lr = a.lr;
@@ -230,7 +245,7 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwTable table, AdamwParam
   const uint32_t seed = (uint32_t)step * 0x3C6EF373u;
   const bool fit = aligned_to(t.param, 16) && aligned_to(t.grad, 16) && aligned_to(t.m, BITS8 ? 8 : 16) &&
                    aligned_to(t.v, BITS8 ? 8 : 16) && aligned_to(t.copy, 16);
-  const int64_t end = from + kAdamwChunk < n ? from + kAdamwChunk : n;
+  const int64_t end = from + a.chunk < n ? from + a.chunk : n;
   for (int64_t at = from + threadIdx.x * 8; at - threadIdx.x % 16 * 8 < end; at += 256 * 8) {
     const int left = (int)(end - at < 8 ? end - at : 8);     // may be none in a block's last threads
     const bool whole = fit && left == 8;
@@ -296,6 +311,47 @@ __global__ void __launch_bounds__(256) moments_kernel(int64_t n, const uint8_t* 
 
 }  // namespace
 
+namespace {
+
+template <bool P16, bool G16, bool BITS8>
+hipError_t launch(AdamwParams a, const AdamwTensor* tensors, int64_t count, hipStream_t stream) {
+  using Table = AdamwTable<BITS8>;
+  static_assert(sizeof(Table) + sizeof(AdamwParams) <= 4096, "kernel arguments");
+  for (int64_t i = 0; i < count;) {
+    Table table;
+    int64_t groups = 0, elems = 0;
+    int k = 0;
+    // 8192 elements of a workgroup; 2048, one pass, while that is few workgroups
+    for (int64_t j = i; j < count && j < i + Table::kTensors; ++j) elems += tensors[j].n;
+    a.chunk = elems <= 2048 * 4096 ? 2048 : 8192;
+    for (; i < count && k < Table::kTensors; ++i) {
+      const AdamwTensor& s = tensors[i];
+      const int64_t need = (s.n + a.chunk - 1) / a.chunk;
+      if (k && groups + need > 0x7fffffff) break;
+      auto& t = table.t[k++];
+      t.param = s.param;
+      t.grad = s.grad;
+      t.m = s.m;
+      t.v = s.v;
+      t.copy = s.copy;
+      t.n = s.n;
+      t.weight_decay = s.weight_decay;
+      t.first = (int32_t)groups;
+      if constexpr (BITS8) {
+        t.m_scale = s.m_scale;
+        t.v_scale = s.v_scale;
+      }
+      groups += need;
+    }
+    a.count = k;
+    hipLaunchKernelGGL((adamw_kernel<P16, G16, BITS8>), dim3((unsigned)groups), dim3(256), 0, stream, table, a);
+    if (hipError_t e = hipGetLastError()) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
 hipError_t launch_adamw(const AdamwStep& s, const AdamwTensor* tensors, int64_t count, bool p_bf16, bool g_bf16, bool bits8,
                         hipStream_t stream) {
   AdamwParams a{};
@@ -315,28 +371,13 @@ hipError_t launch_adamw(const AdamwStep& s, const AdamwTensor* tensors, int64_t 
     a.rate = (float)(s.lr / (1.0 - power_of(s.beta1, s.step)));
     a.root = (float)(1.0 / sqrt(1.0 - power_of(s.beta2, s.step)));
   }
-  void (*kernel)(AdamwTable, AdamwParams) =
-      p_bf16 ? (g_bf16 ? (bits8 ? adamw_kernel<true, true, true> : adamw_kernel<true, true, false>)
-                       : (bits8 ? adamw_kernel<true, false, true> : adamw_kernel<true, false, false>))
-             : (g_bf16 ? (bits8 ? adamw_kernel<false, true, true> : adamw_kernel<false, true, false>)
-                       : (bits8 ? adamw_kernel<false, false, true> : adamw_kernel<false, false, false>));
-  static_assert(sizeof(AdamwTable) + sizeof(AdamwParams) <= 4096, "kernel arguments");
-  for (int64_t i = 0; i < count;) {
-    AdamwTable table;
-    int64_t groups = 0;
-    int k = 0;
-    for (; i < count && k < kAdamwTensors; ++i) {
-      const int64_t need = (tensors[i].n + kAdamwChunk - 1) / kAdamwChunk;
-      if (k && groups + need > 0x7fffffff) break;
-      table.t[k] = tensors[i];
-      table.first[k++] = (int32_t)groups;
-      groups += need;
-    }
-    a.count = k;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(256), 0, stream, table, a);
-    if (hipError_t e = hipGetLastError()) return e;
-  }
-  return hipSuccess;
+  const auto kind = [&](auto p16, auto g16) {
+    constexpr bool P = decltype(p16)::value, G = decltype(g16)::value;
+    return bits8 ? launch<P, G, true>(a, tensors, count, stream) : launch<P, G, false>(a, tensors, count, stream);
+  };
+  const std::true_type yes;
+  const std::false_type no;
+  return p_bf16 ? (g_bf16 ? kind(yes, yes) : kind(yes, no)) : (g_bf16 ? kind(no, yes) : kind(no, no));
 }
 
 hipError_t launch_adamw_moments(int64_t n, const uint8_t* m, const uint8_t* m_scale, const uint8_t* v, const uint8_t* v_scale,

@@ -156,31 +156,41 @@ struct CombineParams {
   float scale, dloss_scale;
 };
 
-// One wave a token: the tiles' sums brought to their common maximum. For dW the
-// tokens' x are copied without those that add nothing to it: 0 times whatever a
-// padding row holds need not be 0.
+// A workgroup a token: the tiles' sums brought to their common maximum (the same
+// order whatever the rest). For dW the tokens' x are copied without those that add
+// nothing to it: 0 times whatever a padding row holds need not be 0.
 __global__ void __launch_bounds__(256) combine_kernel(CombineParams p) {
-  const int32_t row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (row >= p.tokens) return;
+  __shared__ float2 waves[4];
+  const int32_t row = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const float2* s = p.stat + (int64_t)row * p.tiles_n;
-  float top = -INFINITY;
-  for (int i = lane; i < p.tiles_n; i += 64) top = fmaxf(top, s[i].x);
-#pragma unroll
-  for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
-  float sum = 0.f;
-  for (int i = lane; i < p.tiles_n; i += 64) sum += s[i].y * __builtin_amdgcn_exp2f((s[i].x - top) * kLog2e);
-#pragma unroll
-  for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x);
-  const float lse = top + logf(sum);
   const int64_t t = p.targets[row];
   const bool live = t >= 0 && t < p.vocab;
   const float g = live ? (p.dloss ? p.dloss[row] : 1.f) * p.dloss_scale * p.scale : 0.f;
+  float top = -INFINITY, sum = 0.f;
+  const auto join = [&](float2 o) {
+    const float m = fmaxf(top, o.x);
+    // a side without terms has a maximum of -inf, and 0 terms
+    sum = (sum == 0.f ? 0.f : sum * __builtin_amdgcn_exp2f((top - m) * kLog2e)) +
+          (o.y == 0.f ? 0.f : o.y * __builtin_amdgcn_exp2f((o.x - m) * kLog2e));
+    top = m;
+  };
+#pragma unroll 4
+  for (int i = tid; i < p.tiles_n; i += 256) join(s[i]);
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) join(make_float2(__shfl_xor(top, x), __shfl_xor(sum, x)));
+  if (lane == 0) waves[tid >> 6] = make_float2(top, sum);
   if (p.rows) {
     const uint4* from = reinterpret_cast<const uint4*>(p.X + row * p.x_ld);
     uint4* to = reinterpret_cast<uint4*>(p.rows + (int64_t)row * p.hidden);
-    for (int i = lane; i < p.hidden / 8; i += 64) to[i] = g != 0.f ? from[i] : make_uint4(0, 0, 0, 0);
+    for (int i = tid; i < p.hidden / 8; i += 256) to[i] = g != 0.f ? from[i] : make_uint4(0, 0, 0, 0);
   }
-  if (lane) return;
+  __syncthreads();
+  if (tid) return;
+  top = waves[0].x;
+  sum = waves[0].y;
+#pragma unroll
+  for (int w = 1; w < 4; ++w) join(waves[w]);
+  const float lse = top + logf(sum);
   if (p.loss) p.loss[row] = live ? lse - p.target_z[row] : 0.f;
   if (p.lse) p.lse[row] = lse;
   if (p.factor) p.factor[row] = make_float2(lse, g);
@@ -404,7 +414,7 @@ hipError_t launch_cross_entropy(const VocabShape& s, const VocabCall& c, void* w
     if (z.tile_m == 256 && s.hidden % 64 == 0) logits(ProductTile<256, 256, true, true, 2, 8, 4, false, true>{});
     else if (z.tile_m == 256) logits(ProductTile<256, 256, true, true, 2, 8, 4>{});
     else if (z.tile_m == 128) logits(ProductTile<128, 128, true, true, 2, 8, 2>{});
-    else logits(ProductTile<64, 128, true, true, 2, 8, 2, true>{});
+    else logits(ProductTile<64, 128, true, true, 3, 8, 2, true>{});
     if (hipError_t e = hipGetLastError()) return e;
     CombineParams cp{};
     cp.stat = stat;
@@ -423,7 +433,7 @@ hipError_t launch_cross_entropy(const VocabShape& s, const VocabCall& c, void* w
     cp.rows = c.dw ? rows : nullptr;
     cp.hidden = (int32_t)s.hidden;
     cp.dloss_scale = c.dloss_scale;
-    hipLaunchKernelGGL(combine_kernel, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, stream, cp);
+    hipLaunchKernelGGL(combine_kernel, dim3((unsigned)n), dim3(256), 0, stream, cp);
     if (hipError_t e = hipGetLastError()) return e;
     if (!c.grad) continue;
     ScaleParams sp{};

@@ -535,11 +535,11 @@ hipError_t launch_grouped(const GroupedShape& s, const GroupedCall& c, int direc
   } else if (direction == GROUPED_FORWARD) {
     if (f.tile_m == 256) rows(ProductTile<256, 256, true, true, 2, 8, 4, true>{}, no);
     else if (f.tile_m == 128) rows(ProductTile<128, 128, true, true, 2, 8, 2, true>{}, no);
-    else rows(ProductTile<64, 128, true, true, 2, 8, 2, true>{}, no);
+    else rows(ProductTile<64, 128, true, true, 3, 8, 2, true>{}, no);
   } else {
     if (f.tile_m == 256) rows(ProductTile<256, 256, true, false, 2, 8, 4, true>{}, yes);
     else if (f.tile_m == 128) rows(ProductTile<128, 128, true, false, 2, 8, 2, true>{}, yes);
-    else rows(ProductTile<64, 128, true, false, 2, 8, 2, true>{}, yes);
+    else rows(ProductTile<64, 128, true, false, 3, 8, 2, true>{}, yes);
   }
   if (hipError_t e = hipGetLastError()) return e;
   if (f.splits == 1) return hipSuccess;

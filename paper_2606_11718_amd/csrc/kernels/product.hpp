@@ -64,7 +64,7 @@ struct ProductTile {
 // Waves a SIMD with the workgroups of a CU that the LDS allows (with up to 8 KB of a
 // kernel's own).
 template <typename T>
-constexpr int waves_per_simd() { return T::NW / 4 * (T::LDS <= 72 * 1024 ? 2 : 1); }
+constexpr int waves_per_simd() { return T::NW / 4 * (T::LDS <= 73 * 1024 ? 2 : 1); }
 
 // The loads of one side: per-lane offsets, the same for every tile, and the stage
 // that comes next.
@@ -186,8 +186,8 @@ __device__ __forceinline__ int32_t product_steps(int32_t k) { return max((k + 63
 #if defined(__HIP_DEVICE_COMPILE__)
 // This workgroup's tiles one after the other. next(i, &work) gives its i-th, a
 // struct with the Sides u and v and the number of steps (uniform; false: no
-// more; also called one beyond); finish(work, acc) takes the fp32 sums, and may
-// use LDS outside sm, T::LDS bytes, 1024-byte aligned. ldu, ldv: elements between
+// more; also called one beyond); finish(work, acc) takes the fp32 sums, and may use LDS
+// outside sm, T::LDS bytes, 1024-byte aligned. ldu, ldv: elements between
 // memory rows; vmap: the memory row of a KC V tile row.
 //
 // A half's MFMAs go tile row by tile row of U: as soon as a row's are issued, its
