@@ -63,6 +63,8 @@ __global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) logits_kernel
       [&](const LogitsWork& w, f32x4 (&acc)[TM][TN]) __attribute__((always_inline)) {
         const int32_t rows = w.u.extent, col0 = w.tj * BN + wn * T::WN + 4 * (lane >> 4);
         const int32_t left = p.vocab - col0;         // columns from the lane's first on
+        const TileMatrix<TN / 2, T::ROWS> E(p.E + (int64_t)w.ti * BM * p.e_ld + w.tj * BN, p.e_ld, p.E ? rows : 0,
+                                            p.e_cols - w.tj * BN, T::row(wm, 0) + (lane & 15), wn * T::WN + pair_column(lane));
         // rows' maxima over a wave's columns, then over the waves
         float top[TM], sum[TM];
 #pragma unroll
@@ -112,14 +114,9 @@ __global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) logits_kernel
             e[nt] = f32_to_bf16x4(acc[mt][nt]);
           }
           if (p.E) {
-            uint16_t* const to = p.E + (int64_t)(w.ti * BM + r) * p.e_ld;
+            // columns past the vocabulary up to e_cols: exp(-inf) = 0
 #pragma unroll
-            for (int nt = 0; nt < TN; nt += 2) {
-              // columns past the vocabulary up to e_cols: exp(-inf) = 0
-              const int32_t c = w.tj * BN + wn * T::WN + 16 * nt + pair_column(lane);
-              const uint4 v = pair_up(e[nt], e[nt + 1]);
-              if (r < rows && c < p.e_cols) *reinterpret_cast<uint4*>(to + c) = v;
-            }
+            for (int i = 0; i < TN / 2; ++i) E.store(mt, i, pair_up(e[2 * i], e[2 * i + 1]));
           }
         }
         product_barrier<63>();
@@ -283,6 +280,9 @@ __global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) plain_kernel(
       [&](const PlainWork& w, f32x4 (&acc)[TM][TN]) __attribute__((always_inline)) {
         const int64_t row0 = (int64_t)w.ti * BM;
         const int32_t col0 = w.tj * BN;
+        const TileMatrix<TN / 2, T::ROWS> out(static_cast<uint16_t*>(p.out) + row0 * p.ld_out + col0, p.ld_out,
+                                              p.part || p.f32 ? 0 : w.m, w.n, T::row(wm, 0) + (lane & 15),
+                                              wn * T::WN + pair_column(lane));
 #pragma unroll
         for (int mt = 0; mt < TM; ++mt) {
           const int r = T::row(wm, mt) + (lane & 15);
@@ -299,24 +299,22 @@ __global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) plain_kernel(
             }
             continue;
           }
-          uint16_t* const to = static_cast<uint16_t*>(p.out) + (row0 + r) * p.ld_out + col0;
           const float* const add = p.add + (row0 + r) * p.n + col0;
 #pragma unroll
-          for (int nt = 0; nt < TN; nt += 2) {
-            f32x4 a = acc[mt][nt], b = acc[mt][nt + 1];
-            const int32_t c4 = wn * T::WN + 16 * nt + 4 * (lane >> 4), c = wn * T::WN + 16 * nt + pair_column(lane);
+          for (int i = 0; i < TN / 2; ++i) {
+            f32x4 a = acc[mt][2 * i], b = acc[mt][2 * i + 1];
+            const int32_t c4 = wn * T::WN + 32 * i + 4 * (lane >> 4);
             if (MORE && p.add && live) {
               if (c4 < w.n) a += *reinterpret_cast<const f32x4*>(add + c4);
               if (c4 + 16 < w.n) b += *reinterpret_cast<const f32x4*>(add + c4 + 16);
             }
             if (MORE && p.accumulate) {
               uint2 x, y;
-              pair_down(live && c < w.n ? *reinterpret_cast<const uint4*>(to + c) : make_uint4(0, 0, 0, 0), &x, &y);
+              pair_down(out.load(mt, i), &x, &y);
               a += bf16x4_to_f32(x);
               b += bf16x4_to_f32(y);
             }
-            const uint4 v = pair_up(f32_to_bf16x4(a), f32_to_bf16x4(b));
-            if (live && c < w.n) *reinterpret_cast<uint4*>(to + c) = v;
+            out.store(mt, i, pair_up(f32_to_bf16x4(a), f32_to_bf16x4(b)));
           }
         }
       });

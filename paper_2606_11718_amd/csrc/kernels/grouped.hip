@@ -112,52 +112,52 @@ __device__ __forceinline__ void partial_row(float* to, const f32x4 (&acc)[T::TN]
 template <typename T, bool GATED>
 __device__ __forceinline__ void forward_out(const GroupedParams& p, const RowWork& t, f32x4 (&acc)[T::TM][T::TN], int tid) {
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / T::WGN, wn = wave % T::WGN;
-  const int32_t half = p.n / 2, cols = GATED ? half : p.n;
-  uint16_t* const Y = static_cast<uint16_t*>(p.out) + t.first * p.ld_out;
-  uint16_t* const Z = p.Z + t.first * p.ld_z;
+  constexpr int TY = GATED ? T::TN / 2 : T::TN, kHalf = GATED ? 2 : 1;
+  static_assert(TY % 2 == 0, "pairs");
+  const int32_t cols = p.n / kHalf, corner = t.tj * T::BN / kHalf;      // of Y
+  const int row0 = T::row(wm, 0) + (lane & 15);
+  const TileMatrix<TY / 2, T::ROWS> Y(static_cast<uint16_t*>(p.out) + t.first * p.ld_out + corner, p.ld_out, t.rows,
+                                      cols - corner, row0, wn * T::WN / kHalf + pair_column(lane));
   const ActCoef k = act_coef(p.act);
-  const int at = pair_column(lane);
+  if (p.Z) {
+    const uint16_t* const z = p.Z + t.first * p.ld_z + corner;
+    // gated: even 16s of lanes hold a pair's gate columns and odd ones its up columns,
+    // half a Z further on; pairs are 16 columns apart
+    const int32_t half = GATED && lane & 16 ? cols : 0;
+    TileMatrix<T::TN / 2, T::ROWS> Z(z, p.ld_z, t.rows, GATED ? p.n - corner : cols - corner, row0,
+                                     wn * T::WN / kHalf + (GATED ? 8 * (lane >> 5) + half : pair_column(lane)));
+    if constexpr (GATED) {
+#pragma unroll
+      for (int i = 0; i < T::TN / 2; ++i) {
+        const int32_t c = wn * T::WN / 2 + 8 * (lane >> 5) + 16 * i;
+        Z.at[i] = c < cols - corner ? (uint32_t)(row0 * (int32_t)p.ld_z + c + half) * 2u : 0x80000000u;
+      }
+    }
+#pragma unroll
+    for (int mt = 0; mt < T::TM; ++mt) {
+      if (T::row(wm, mt) >= t.rows) break;
+#pragma unroll
+      for (int i = 0; i < T::TN / 2; ++i) Z.store(mt, i, pair_up(f32_to_bf16x4(acc[mt][2 * i]), f32_to_bf16x4(acc[mt][2 * i + 1])));
+    }
+  }
   with_act(p.act, [&](auto cls) __attribute__((always_inline)) {
     constexpr int C = decltype(cls)::value;
 #pragma unroll
     for (int mt = 0; mt < T::TM; ++mt) {
-      const int r = T::row(wm, mt) + (lane & 15);
       if (T::row(wm, mt) >= t.rows) break;
-      const bool live = r < t.rows;
-      if (p.Z) {
+      uint2 y[TY];
 #pragma unroll
-        for (int nt = 0; nt < T::TN; nt += 2) {
-          const uint4 z = pair_up(f32_to_bf16x4(acc[mt][nt]), f32_to_bf16x4(acc[mt][nt + 1]));
-          const int32_t c = wn * T::WN + 16 * nt;
-          if constexpr (GATED) {      // even 16s of lanes hold the gate's columns, odd ones the up columns
-            const int32_t n = t.tj * (T::BN / 2) + c / 2 + 8 * (lane >> 5);
-            if (live && n < half) *reinterpret_cast<uint4*>(Z + r * p.ld_z + n + (lane & 16 ? half : 0)) = z;
-          } else {
-            const int32_t n = t.tj * T::BN + c + at;
-            if (live && n < p.n) *reinterpret_cast<uint4*>(Z + r * p.ld_z + n) = z;
-          }
-        }
-      }
-      uint2 y[T::TN];
-#pragma unroll
-      for (int nt = 0; nt < T::TN; ++nt) {
-        if (GATED && (nt & 1)) continue;
+      for (int i = 0; i < TY; ++i) {
         f32x4 o;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          o[j] = act_value<C>(k, acc[mt][nt][j]);
-          if constexpr (GATED) o[j] *= acc[mt][nt + 1][j];
+          o[j] = act_value<C>(k, acc[mt][kHalf * i][j]);
+          if constexpr (GATED) o[j] *= acc[mt][2 * i + 1][j];
         }
-        y[GATED ? nt / 2 : nt] = f32_to_bf16x4(o);
+        y[i] = f32_to_bf16x4(o);
       }
-      constexpr int TY = GATED ? T::TN / 2 : T::TN;
-      static_assert(TY % 2 == 0, "pairs");
 #pragma unroll
-      for (int nt = 0; nt < TY; nt += 2) {
-        const int32_t n = (t.tj * T::BN + wn * T::WN) / (GATED ? 2 : 1) + 16 * nt + at;
-        const uint4 v = pair_up(y[nt], y[nt + 1]);
-        if (live && n < cols) *reinterpret_cast<uint4*>(Y + r * p.ld_out + n) = v;
-      }
+      for (int i = 0; i < TY / 2; ++i) Y.store(mt, i, pair_up(y[2 * i], y[2 * i + 1]));
     }
   });
 }
@@ -167,68 +167,66 @@ __device__ __forceinline__ void forward_out(const GroupedParams& p, const RowWor
 template <typename T, bool GATED>
 __device__ __forceinline__ void grad_out(const GroupedParams& p, const RowWork& t, f32x4 (&acc)[T::TM][T::TN], int tid) {
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / T::WGN, wn = wave % T::WGN;
-  uint16_t* const out = static_cast<uint16_t*>(p.out) + t.first * p.ld_out;
-  const uint16_t* const Z = p.Z + t.first * p.ld_z;
+  constexpr int TP = T::TN / 2;
+  const int32_t corner = t.tj * T::BN, cols = p.n - corner;
+  const int row0 = T::row(wm, 0) + (lane & 15), col0 = wn * T::WN + pair_column(lane);
+  uint16_t* const o = static_cast<uint16_t*>(p.out) + t.first * p.ld_out + corner;
+  const uint16_t* const z = p.Z + t.first * p.ld_z + corner;
+  using Matrix = TileMatrix<TP, T::ROWS>;
+  const Matrix out(o, p.ld_out, t.rows, cols, row0, col0);
   const ActCoef k = act_coef(p.act);
-  const int32_t n0 = t.tj * T::BN + wn * T::WN + pair_column(lane);
   with_act(p.act, [&](auto cls) __attribute__((always_inline)) {
     constexpr int C = decltype(cls)::value;
-    constexpr bool kThrough = GATED || C != ACT_CLASS_NONE;
-    constexpr int TP = T::TN / 2;
-    // Z of one row of 16x16 tiles is on its way while the one before is worked on
-    uint4 zg[2][TP], zu[2][TP];
-    auto fetch = [&](int mt) __attribute__((always_inline)) {
-      const int r = T::row(wm, mt) + (lane & 15);
+    if constexpr (!GATED && C == ACT_CLASS_NONE) {
 #pragma unroll
-      for (int i = 0; i < TP; ++i) {
-        const int32_t n = n0 + 32 * i;
-        zg[mt & 1][i] = zu[mt & 1][i] = make_uint4(0, 0, 0, 0);
-        if (r < t.rows && n < p.n) {
-          zg[mt & 1][i] = *reinterpret_cast<const uint4*>(Z + r * p.ld_z + n);
-          if constexpr (GATED) zu[mt & 1][i] = *reinterpret_cast<const uint4*>(Z + r * p.ld_z + p.n + n);
-        }
+      for (int mt = 0; mt < T::TM; ++mt) {
+        if (T::row(wm, mt) >= t.rows) break;
+#pragma unroll
+        for (int i = 0; i < TP; ++i) out.store(mt, i, pair_up(f32_to_bf16x4(acc[mt][2 * i]), f32_to_bf16x4(acc[mt][2 * i + 1])));
       }
-    };
-    if constexpr (kThrough) fetch(0);
+    } else {
+      const Matrix out_up(o + p.n, p.ld_out, GATED ? t.rows : 0, cols, row0, col0);
+      const Matrix Z(z, p.ld_z, t.rows, cols, row0, col0), Z_up(z + p.n, p.ld_z, GATED ? t.rows : 0, cols, row0, col0);
+      // Z of one row of 16x16 tiles is on its way while the one before is worked on
+      uint4 zg[2][TP], zu[2][TP];
+      auto fetch = [&](int mt) __attribute__((always_inline)) {
 #pragma unroll
-    for (int mt = 0; mt < T::TM; ++mt) {
-      if (T::row(wm, mt) >= t.rows) break;
-      const int r = T::row(wm, mt) + (lane & 15);
-      if (kThrough && mt + 1 < T::TM) fetch(mt + 1);
+        for (int i = 0; i < TP; ++i) {
+          zg[mt & 1][i] = Z.load(mt, i);
+          if constexpr (GATED) zu[mt & 1][i] = Z_up.load(mt, i);
+        }
+      };
+      fetch(0);
 #pragma unroll
-      for (int i = 0; i < TP; ++i) {
-        uint2 o[2], w[2], g[2], u[2];
-        if constexpr (kThrough) pair_down(zg[mt & 1][i], &g[0], &g[1]);
-        if constexpr (GATED) pair_down(zu[mt & 1][i], &u[0], &u[1]);
+      for (int mt = 0; mt < T::TM; ++mt) {
+        if (T::row(wm, mt) >= t.rows) break;
+        if (mt + 1 < T::TM) fetch(mt + 1);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const f32x4 d = acc[mt][2 * i + h];
-          f32x4 x = d, y;
-          if constexpr (kThrough) {
-            const f32x4 z = bf16x4_to_f32(g[h]);
-            f32x4 up;
+        for (int i = 0; i < TP; ++i) {
+          uint2 x[2], w[2], g[2], u[2];
+          pair_down(zg[mt & 1][i], &g[0], &g[1]);
+          if constexpr (GATED) pair_down(zu[mt & 1][i], &u[0], &u[1]);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const f32x4 d = acc[mt][2 * i + h], gate = bf16x4_to_f32(g[h]);
+            f32x4 dg, du, up;
             if constexpr (GATED) up = bf16x4_to_f32(u[h]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               float slope;
-              const float value = act_value_grad<C>(k, z[j], &slope);
+              const float value = act_value_grad<C>(k, gate[j], &slope);
               if constexpr (GATED) {
-                y[j] = d[j] * value;
-                x[j] = d[j] * up[j] * slope;
+                du[j] = d[j] * value;
+                dg[j] = d[j] * up[j] * slope;
               } else {
-                x[j] = d[j] * slope;
+                dg[j] = d[j] * slope;
               }
             }
-            if constexpr (GATED) w[h] = f32_to_bf16x4(y);
+            x[h] = f32_to_bf16x4(dg);
+            if constexpr (GATED) w[h] = f32_to_bf16x4(du);
           }
-          o[h] = f32_to_bf16x4(x);
-        }
-        const int32_t n = n0 + 32 * i;
-        const uint4 a = pair_up(o[0], o[1]);
-        if (r < t.rows && n < p.n) *reinterpret_cast<uint4*>(out + r * p.ld_out + n) = a;
-        if constexpr (GATED) {
-          const uint4 b = pair_up(w[0], w[1]);
-          if (r < t.rows && n < p.n) *reinterpret_cast<uint4*>(out + r * p.ld_out + p.n + n) = b;
+          out.store(mt, i, pair_up(x[0], x[1]));
+          if constexpr (GATED) out_up.store(mt, i, pair_up(w[0], w[1]));
         }
       }
     }
@@ -353,6 +351,9 @@ __global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) grouped_wgrad
       [&](const WgradWork& w, f32x4 (&acc)[T::TM][T::TN]) __attribute__((always_inline)) {
         const int wm = wave / T::WGN, wn = wave % T::WGN;
         const int64_t corner = w.expert * p.w_stride + (int64_t)w.row * p.ld_out + w.col;
+        const TileMatrix<T::TN / 2, T::ROWS> dw(static_cast<uint16_t*>(p.out) + corner, p.ld_out,
+                                                p.f32 || p.part ? 0 : w.m, w.n, T::row(wm, 0) + (lane & 15),
+                                                wn * T::WN + pair_column(lane));
 #pragma unroll
         for (int mt = 0; mt < T::TM; ++mt) {
           const int r = T::row(wm, mt) + (lane & 15);
@@ -372,19 +373,16 @@ __global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) grouped_wgrad
               *at = OUT == WGRAD_ANY && p.accumulate ? *at + acc[mt][nt] : acc[mt][nt];
             }
           } else {
-            uint16_t* const to = static_cast<uint16_t*>(p.out) + corner + r * p.ld_out;
 #pragma unroll
-            for (int nt = 0; nt < T::TN; nt += 2) {
-              const int32_t c = wn * T::WN + 16 * nt + pair_column(lane);
-              f32x4 a = acc[mt][nt], b = acc[mt][nt + 1];
+            for (int i = 0; i < T::TN / 2; ++i) {
+              f32x4 a = acc[mt][2 * i], b = acc[mt][2 * i + 1];
               if (OUT == WGRAD_ANY && p.accumulate) {
                 uint2 x, y;
-                pair_down(live && c < w.n ? *reinterpret_cast<const uint4*>(to + c) : make_uint4(0, 0, 0, 0), &x, &y);
+                pair_down(dw.load(mt, i), &x, &y);
                 a += bf16x4_to_f32(x);
                 b += bf16x4_to_f32(y);
               }
-              const uint4 v = pair_up(f32_to_bf16x4(a), f32_to_bf16x4(b));
-              if (live && c < w.n) *reinterpret_cast<uint4*>(to + c) = v;
+              dw.store(mt, i, pair_up(f32_to_bf16x4(a), f32_to_bf16x4(b)));
             }
           }
         }

@@ -59,6 +59,7 @@ struct ProductTile {
   static_assert(UK || !SKIP, "rows are skipped on a KC side");
   // Tile row mt of a wave, in rows of the tile. KC: a wave's rows are spread, so
   // that a tile with few valid rows keeps all waves at work.
+  static constexpr int ROWS = UK ? 16 * WGM : 16;        // between a wave's tile rows
   __device__ static __forceinline__ int row(int wm, int mt) { return UK ? 16 * (WGM * mt + wm) : WM * wm + 16 * mt; }
 };
 // Waves a SIMD with the workgroups of a CU that the LDS allows (with up to 8 KB of a
@@ -410,6 +411,32 @@ __device__ __forceinline__ void raster(int32_t id, int32_t tiles_m, int32_t tile
 
 // The column (in two tiles' 32) of a lane's eight.
 __device__ __forceinline__ int pair_column(int lane) { return 16 * ((lane >> 4) & 1) + 8 * (lane >> 5); }
+
+// A lane's eights of a wave's tiles in a bf16 matrix: rows < rows and columns < cols
+// from `corner` on exist (at most 2^30 bytes of them); what lies past them reads as 0
+// and is not stored. row0, col0: the lane's row and first column. NP pairs of 16x16
+// tiles side by side, rows of them STEP apart. (Offsets and the bounds in a descriptor:
+// a third of the vector instructions of 64-bit addresses and comparisons.)
+template <int NP, int STEP>
+struct TileMatrix {
+  __amdgpu_buffer_rsrc_t memory;
+  uint32_t at[NP];
+  uint32_t step;
+  __device__ __forceinline__ TileMatrix(const uint16_t* corner, int64_t ld, int32_t rows, int32_t cols, int32_t row0, int32_t col0) {
+    const int32_t bytes = rows > 0 && cols > 0 ? (int32_t)((rows - 1) * ld + cols) * 2 : 0;
+    memory = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(corner), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+    step = (uint32_t)(STEP * ld * 2);
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+      at[i] = col0 + 32 * i < cols ? (uint32_t)(row0 * (int32_t)ld + col0 + 32 * i) * 2u : 0x80000000u;
+  }
+  __device__ __forceinline__ void store(int mt, int i, uint4 v) const {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, v), memory, (int)(at[i] + mt * step), 0, 0);
+  }
+  __device__ __forceinline__ uint4 load(int mt, int i) const {
+    return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(memory, (int)(at[i] + mt * step), 0, 0));
+  }
+};
 
 __device__ __forceinline__ void swap16(uint32_t& a, uint32_t& b) {
   const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
