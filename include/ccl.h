@@ -516,7 +516,7 @@ typedef enum ccl_grouped_direction {
  * rows outside 0..2^30, an unknown activation, direction or type, gated or
  * accumulate not 0 or 1, a leading dimension or stride smaller than what it
  * spans, workspace missing or too small); CCL_ERR_UNSUPPORTED (a side not a
- * multiple of 16 or above 2^20, a gated expert's weight of 2^30 elements and
+ * multiple of 16 or above 2^20, a gated expert's weight of 2^29 elements and
  * more, a launch too large; device not gfx950); CCL_ERR_MISALIGNED_POINTER;
  * CCL_ERR_HIP.
  */

@@ -516,6 +516,19 @@ def ccl_orthogonalize(batch: int, rows: int, cols: int, G, g_type: int, ld: int,
                                        _stream(stream)))
 
 
+def _here(**tensors) -> None:
+    """Tensors of a call have to be on the current device, whose kernels read them."""
+    at = None
+    for name, t in tensors.items():
+        if t is None or isinstance(t, int):
+            continue
+        if at is None:
+            import torch
+            at = torch.cuda.current_device() if t.is_cuda else 0
+        if t.get_device() != at:
+            _refuse(name, f"a tensor on {t.device}, not on the current GPU")
+
+
 CCL_GROUPED_FORWARD, CCL_GROUPED_GRAD, CCL_GROUPED_WGRAD = 0, 1, 2
 
 
@@ -540,6 +553,7 @@ def ccl_grouped_gemm(grouped: _Grouped, rows: int, ends, X, W, Y, *, preact=None
     import torch
     bf16, bits = torch.bfloat16, torch.int16
     K, N, E = grouped.in_features, grouped.out_features, grouped.experts
+    _here(ends=ends, X=X, W=W, Y=Y, preact=preact, workspace=workspace)
     X, x_ld = _rows("X", X, x_ld, rows, K, bf16, bits)
     Y, y_ld = _rows("Y", Y, y_ld, rows, N // 2 if grouped.gated else N, bf16, bits)
     preact, z_ld = _rows("preact", preact, z_ld, rows, N, bf16, bits)
@@ -557,6 +571,7 @@ def ccl_grouped_gemm_grad(grouped: _Grouped, rows: int, ends, dY, W, dX, *, prea
     bf16, bits = torch.bfloat16, torch.int16
     K, N, E = grouped.in_features, grouped.out_features, grouped.experts
     wide = 2 * K if grouped.gated else K
+    _here(ends=ends, dY=dY, W=W, dX=dX, preact=preact, workspace=workspace)
     dY, dy_ld = _rows("dY", dY, dy_ld, rows, N, bf16, bits)
     dX, dx_ld = _rows("dX", dX, dx_ld, rows, wide, bf16, bits)
     preact, z_ld = _rows("preact", preact, z_ld, rows, wide, bf16, bits)
@@ -573,6 +588,7 @@ def ccl_grouped_gemm_wgrad(grouped: _Grouped, rows: int, ends, dY, X, dW, *, dw_
     import torch
     bf16, bits = torch.bfloat16, torch.int16
     K, N, E = grouped.in_features, grouped.out_features, grouped.experts
+    _here(ends=ends, dY=dY, X=X, dW=dW, workspace=workspace)
     dY, dy_ld = _rows("dY", dY, dy_ld, rows, N, bf16, bits)
     X, x_ld = _rows("X", X, x_ld, rows, K, bf16, bits)
     if dw_type is None:
@@ -609,6 +625,7 @@ def ccl_cross_entropy(vocab: _Vocab, tokens: int, X, W, targets, loss, *, lse=No
     call = library().ccl_cross_entropy
     import torch
     bf16, f32 = torch.bfloat16, torch.float32
+    _here(X=X, W=W, targets=targets, loss=loss, lse=lse, workspace=workspace)
     X, x_ld = _rows("X", X, x_ld, tokens, vocab.hidden, bf16, torch.int16)
     _check(call(ctypes.byref(vocab), tokens, X, x_ld, _vocab_weight(vocab, W, bf16),
                 _whole("targets", targets, tokens, torch.int64), _whole("loss", loss, tokens, f32),
@@ -627,6 +644,7 @@ def ccl_cross_entropy_grad(vocab: _Vocab, tokens: int, X, W, targets, loss, dX, 
     if dw_type is None:
         dw_type = CCL_DT_FP32 if getattr(dW, "dtype", None) is f32 else CCL_DT_BF16
     D = vocab.hidden
+    _here(X=X, W=W, targets=targets, loss=loss, dX=dX, dW=dW, lse=lse, dloss=dloss, workspace=workspace)
     X, x_ld = _rows("X", X, x_ld, tokens, D, bf16, torch.int16)
     dX, dx_ld = _rows("dX", dX, dx_ld, tokens, D, bf16, torch.int16)
     dW, dw_ld = _rows("dW", dW, dw_ld, vocab.vocab, D, f32 if dw_type == CCL_DT_FP32 else bf16)
@@ -646,6 +664,11 @@ def ccl_adamw_tensor(param, grad, exp_avg, exp_avg_sq, *, exp_avg_scale=None, ex
     import torch
     types = {torch.float32: CCL_DT_FP32, torch.bfloat16: CCL_DT_BF16}
     n = param.numel()
+    at = param.get_device()
+    for name, t in (("grad", grad), ("exp_avg", exp_avg), ("exp_avg_sq", exp_avg_sq), ("exp_avg_scale", exp_avg_scale),
+                    ("exp_avg_sq_scale", exp_avg_sq_scale), ("copy", copy)):
+        if t is not None and t.get_device() != at:
+            _refuse(name, f"a tensor on {t.device}, the param on {param.device}")
     for name, t in (("param", param), ("grad", grad)):
         if t.dtype not in types:
             _refuse(name, f"a tensor of {t.dtype}, not fp32 or bf16")
@@ -670,6 +693,7 @@ class AdamwSet:
 
     def __init__(self, tensors):
         tensors = list(tensors)
+        self.device = {held[0].get_device() for t, held in tensors if held and t.n}
         self.tensors = (_AdamwTensor * len(tensors))(*(t for t, _ in tensors))
         self.kept = [held for _, held in tensors]
 
@@ -685,6 +709,11 @@ def ccl_adamw_step(tensors: AdamwSet, *, lr: float, step: int = 0, beta1: float 
     device, read when the step runs."""
     call = library().ccl_adamw_step
     import torch
+    if tensors.device:
+        at = torch.cuda.current_device() if torch.cuda.is_initialized() else -1
+        if tensors.device != {at} or at < 0:
+            _refuse("tensors", "not all on the current GPU")
+    _here(step_ptr=step_ptr, lr_ptr=lr_ptr, grad_scale=grad_scale)
     a = _Adamw(lr, beta1, beta2, eps, step, _whole("step_ptr", step_ptr, 1, torch.int64),
                _whole("lr_ptr", lr_ptr, 1, torch.float32), _whole("grad_scale", grad_scale, 1, torch.float32))
     _check(call(ctypes.byref(a), tensors.tensors, len(tensors.tensors), _stream(stream)))
@@ -698,6 +727,7 @@ def ccl_adamw_moments(n: int, exp_avg, exp_avg_scale, exp_avg_sq, exp_avg_sq_sca
     dtype = next((t.dtype for t in (m, v) if t is not None), torch.float32)
     if dtype not in (torch.float32, torch.bfloat16):
         _refuse("m and v", f"tensors of {dtype}, not fp32 or bf16")
+    _here(exp_avg=exp_avg, exp_avg_scale=exp_avg_scale, exp_avg_sq=exp_avg_sq, exp_avg_sq_scale=exp_avg_sq_scale, m=m, v=v)
     _check(call(n, _whole("exp_avg", exp_avg, n, u8), _whole("exp_avg_scale", exp_avg_scale, blocks, u8),
                 _whole("exp_avg_sq", exp_avg_sq, n, u8), _whole("exp_avg_sq_scale", exp_avg_sq_scale, blocks, u8),
                 _whole("m", m, n, dtype), _whole("v", v, n, dtype), CCL_DT_BF16 if dtype is torch.bfloat16 else CCL_DT_FP32,

@@ -68,8 +68,8 @@ ccl_status check_grouped(const ccl_grouped* g, int64_t rows, int direction, ccl:
     return fail(CCL_ERR_INVALID_ARG, "experts' weights overlap, or lie more than 2^48 elements apart");
   if (s.w_ld % 8 || s.w_stride % 8)
     return fail(CCL_ERR_MISALIGNED_POINTER, "weight rows and experts must lie whole 16 bytes apart");
-  if (gated && direction == CCL_GROUPED_FORWARD && s.out * s.w_ld >= (int64_t)1 << 30)
-    return fail(CCL_ERR_UNSUPPORTED, "gated: an expert's weight must span less than 2^30 elements");
+  if (gated && direction == CCL_GROUPED_FORWARD && s.out * s.w_ld >= (int64_t)1 << 29)
+    return fail(CCL_ERR_UNSUPPORTED, "gated: an expert's weight must span less than 2^29 elements");
   // the tiles' numbers are 32-bit, beyond the last by a round of workgroups
   if (ccl::grouped_form(s, rows, direction).tiles > kMaxGrid / 2) return fail(CCL_ERR_UNSUPPORTED, "launch too large");
   *out = s;

@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) logits_kernel
   __shared__ float part[WGN][BM], whole[BM];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WGN, wn = wave % WGN;
-  product_tiles<T, LogitsWork>(
+  product_tiles<T, LogitsWork, 0>(
       p.x_ld, p.w_ld, sm, tid,
       [&](int i, LogitsWork* w) __attribute__((always_inline)) {
         const int32_t id = dealt_tile(i, p.chunk);
@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) plain_kernel(
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / T::WGN, wn = wave % T::WGN;
   const int32_t tiles = p.tiles_m * p.tiles_n;
-  product_tiles<T, PlainWork>(
+  product_tiles<T, PlainWork, MORE ? 0 : T::TM * T::TN / 2>(
       p.ldu, p.ldv, sm, tid,
       [&](int i, PlainWork* w) __attribute__((always_inline)) {
         const int32_t id = dealt_tile(i, p.chunk);

@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) grouped_rows_
   // a gated tile's V rows: BN / 2 gate rows from row `from` on and the up rows half of the weight later
   constexpr bool kPairs = GATED && !GRAD;
   const int32_t half = p.n / 2;
-  product_tiles<T, RowWork>(
+  product_tiles<T, RowWork, 0>(
       p.ldu, p.ldv, sm, tid,
       [&](int i, RowWork* w) __attribute__((always_inline)) {
         int32_t id = dealt_tile(i, p.chunk);
@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) grouped_wgrad
   make_table<T::BM>(p, table, tid);
   const int32_t per = p.tiles_m * p.tiles_n;
   const int32_t tiles = per * p.experts;
-  product_tiles<T, WgradWork>(
+  product_tiles<T, WgradWork, OUT == WGRAD_BF16 ? T::TM * T::TN / 2 : 0>(
       p.ldu, p.ldv, sm, tid,
       [&](int i, WgradWork* w) __attribute__((always_inline)) {
         int32_t id = dealt_tile(i, p.chunk);

@@ -189,14 +189,16 @@ __device__ __forceinline__ int32_t product_steps(int32_t k) { return max((k + 63
 // struct with the Sides u and v and the number of steps (uniform; false: no
 // more; also called one beyond); finish(work, acc) takes the fp32 sums, and may use LDS
 // outside sm, T::LDS bytes, 1024-byte aligned. ldu, ldv: elements between
-// memory rows; vmap: the memory row of a KC V tile row.
+// memory rows; vmap: the memory row of a KC V tile row. STORES: how many memory accesses
+// finish makes in every wave whatever the tile (each store of a TileMatrix counts, also
+// of rows that are not there); 0: it is not known.
 //
 // A half's MFMAs go tile row by tile row of U: as soon as a row's are issued, its
 // fragment's registers take the next half's. The last two rows and V have two
 // sets, read first, so that every read of a stage is a good part of a half old at
 // the barrier (whole second sets of U too would not fit beside a 256x256 tile's
 // accumulators).
-template <typename T, typename Work, typename Next, typename VMap, typename Finish>
+template <typename T, typename Work, int STORES, typename Next, typename VMap, typename Finish>
 __device__ __forceinline__ void product_tiles(int64_t ldu, int64_t ldv, char* sm, int tid, Next&& next, VMap&& vmap,
                                               Finish&& finish) {
   constexpr int NS = T::NS, TM = T::TM, TN = T::TN;
@@ -361,17 +363,24 @@ __device__ __forceinline__ void product_tiles(int64_t ldu, int64_t ldv, char* sm
 #pragma unroll
   for (int i = 0; i < KEPT; ++i) read_row(0, i, false);
 
+  bool fresh = false;
   for (int32_t i = 2;; ++i) {
     if (more) live_next = rows_of(nxt);
     // Steps; on entry set 0 holds the first half of one.
     for (int32_t s = cur.steps; s > 0; --s) {
       const int32_t rows = s > 1 ? live : live_next;      // of the step whose first half the second one reads
       half(0, 1, false, live, 0, true, st);
-      stage_barrier(std::integral_constant<int, T::AHEAD - 2>{});
+      // A wave's accesses finish in order: the first barrier after a tile's finish waits
+      // for loads older than its stores, which may still be on their way (dW of 128
+      // experts, 1536 x 2048 from 256 rows each: 394 -> 378 us).
+      if (STORES && fresh) product_barrier<(T::AHEAD - 2) * T::NL + STORES>();
+      else stage_barrier(std::integral_constant<int, T::AHEAD - 2>{});
+      fresh = false;
       advance();
       half(1, 0, true, rows, T::NL, false, st);
     }
     finish(cur, acc);
+    fresh = true;
     if (!more) break;
     cur = nxt;
     live = live_next;

@@ -230,3 +230,23 @@ def test_adamw_binding():
     # nothing to do: no device needed
     ccl.ccl_adamw_step(ccl.ccl_adamw([]), lr=1e-3, step=1)
     ccl.ccl_adamw_step(ccl.ccl_adamw([make(f(0), f(0), f(0), f(0))]), lr=1e-3, step=1)
+
+
+def test_tensors_of_another_device():
+    """Tensors in host memory that would fit otherwise: refused before anything is launched."""
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+    g = ccl.ccl_grouped(**GROUPED)
+    ends = torch.zeros(4, dtype=torch.int32)
+    _refused(INV, ccl.ccl_grouped_gemm, g, 10, ends, bf(10, 64), bf(4, 96, 64), bf(10, 96))
+    _refused(INV, ccl.ccl_grouped_gemm_grad, g, 10, ends, bf(10, 96), bf(4, 96, 64), bf(10, 64))
+    _refused(INV, ccl.ccl_grouped_gemm_wgrad, g, 10, ends, bf(10, 96), bf(10, 64), bf(4, 96, 64))
+    v = ccl.ccl_vocab(**VOCAB)
+    t, loss = torch.zeros(10, dtype=torch.int64), torch.zeros(10)
+    _refused(INV, ccl.ccl_cross_entropy, v, 10, bf(10, 64), bf(1000, 64), t, loss, workspace=P, workspace_bytes=1 << 40)
+    _refused(INV, ccl.ccl_cross_entropy_grad, v, 10, bf(10, 64), bf(1000, 64), t, loss, bf(10, 64), None, workspace=P,
+             workspace_bytes=1 << 40)
+    f = lambda n: torch.zeros(n)  # noqa: E731
+    _refused(INV, ccl.ccl_adamw_step, ccl.ccl_adamw([ccl.ccl_adamw_tensor(f(9), f(9), f(9), f(9))]), lr=1e-3, step=1)
+    _refused(INV, ccl.ccl_adamw_step, ccl.ccl_adamw([_entry()]), lr=1e-3, step=1, grad_scale=f(1))
+    b8 = lambda n: torch.zeros(n, dtype=torch.uint8)  # noqa: E731
+    _refused(INV, ccl.ccl_adamw_moments, 130, b8(130), b8(2), b8(130), b8(2), f(130), f(130))
