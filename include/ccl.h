@@ -544,7 +544,9 @@ ccl_status ccl_grouped_gemm_wgrad(const ccl_grouped* grouped, int64_t rows, cons
  *   P_v = g * scale * (exp(z_v - lse) - [v = target])
  * A target outside 0 .. vocab - 1 (-100, say) marks a token that does not
  * count: its loss is 0, its dX is 0 and it adds nothing to dW, whatever its x
- * holds; lse is its own. A weight g of 0 is taken so too (the loss is not).
+ * holds; lse is its own. A weight g of 0 is taken so too (the loss is not). A
+ * logit of -inf is a term of 0; one that is NaN or +inf makes its token's loss, lse
+ * and dX NaN, and with that dW.
  * The logits are never in memory: a block of `block` tokens at a time, tiles of
  * them are reduced to fp32 maxima and sums, and where a gradient is asked for
  * exp(z - tile maximum) is kept in bf16 for the block, 2 bytes a logit.
@@ -614,7 +616,8 @@ typedef struct ccl_adamw {
   const int64_t* step_ptr;      /* device: read in place of step, for captured calls; or NULL */
   const float* lr_ptr;          /* device: read in place of lr; or NULL */
   const float* grad_scale;      /* device: 1 / loss scale, a clipping factor; NULL: 1. Where it is
-                                   not finite the step is left out: nothing is written */
+                                   not finite, or *lr_ptr is not, or *step_ptr is
+                                   below 1, the step is left out: nothing is written */
 } ccl_adamw;
 
 typedef struct ccl_adamw_tensor {
@@ -623,7 +626,7 @@ typedef struct ccl_adamw_tensor {
   void *exp_avg, *exp_avg_sq;   /* fp32, or bytes with moment_bits 8 */
   uint8_t *exp_avg_scale, *exp_avg_sq_scale;  /* (n + 127) / 128 bytes with moment_bits 8, else not read */
   void* copy;                   /* bf16, or NULL */
-  int64_t n;                    /* elements, 0 .. 2^40 */
+  int64_t n;                    /* elements, 0 .. 2^34 */
   ccl_dtype param_type, grad_type;  /* CCL_DT_FP32 or CCL_DT_BF16 */
   int32_t moment_bits;          /* 32 or 8 */
   float weight_decay;
@@ -636,12 +639,13 @@ typedef struct ccl_adamw_tensor {
  * NULL). Buffers may start at any element; whole 16 bytes (8 for 8-bit moments)
  * are faster. One launch for every 68 tensors of a kind (54 with 8-bit moments),
  * no workspace.
- * Errors: CCL_ERR_INVALID_ARG (NULL argument, negative sizes or sizes above 2^40,
+ * Errors: CCL_ERR_INVALID_ARG (NULL argument, a count outside 0 .. 2^20, an n
+ * outside 0 .. 2^34,
  * an unknown type, moment_bits other than 8 and 32, betas outside [0, 1), eps
  * negative or not finite, lr or weight_decay not finite, step below 1 without
- * step_ptr, params, moments or copies that overlap); CCL_ERR_MISALIGNED_POINTER;
- * CCL_ERR_UNSUPPORTED (ccl_adamw_moments: a launch too large; device not
- * gfx950); CCL_ERR_HIP.
+ * step_ptr, params, moments, scales or copies that overlap); CCL_ERR_MISALIGNED_POINTER;
+ * CCL_ERR_UNSUPPORTED (device not gfx950); CCL_ERR_HIP (also where the host's
+ * memory runs out).
  */
 ccl_status ccl_adamw_step(const ccl_adamw* adamw, const ccl_adamw_tensor* tensors, int64_t count,
                           void* stream);

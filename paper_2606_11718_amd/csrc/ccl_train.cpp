@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <exception>
 #include <string>
 #include <vector>
 
@@ -19,6 +20,8 @@ using namespace ccl::api;
 namespace {
 
 constexpr int64_t kMaxGrid = 0x7fffffff;
+constexpr int64_t kMaxElems = (int64_t)1 << 34;   // of a tensor: 2048 a workgroup are fewer than 2^32 threads
+constexpr int64_t kMaxTensors = 1 << 20;
 constexpr int64_t kMaxLd = (int64_t)1 << 21;      // 256 rows stay within 31-bit byte offsets
 constexpr int64_t kMaxStride = (int64_t)1 << 48;
 
@@ -115,7 +118,7 @@ bool overlap(std::vector<Span>& spans) {
 }
 
 ccl_status check_adamw_tensor(const ccl_adamw_tensor& t) {
-  if (t.n < 0 || t.n > (int64_t)1 << 40) return fail(CCL_ERR_INVALID_ARG, "a tensor's elements must be in 0..2^40");
+  if (t.n < 0 || t.n > kMaxElems) return fail(CCL_ERR_INVALID_ARG, "a tensor's elements must be in 0..2^34");
   if ((t.param_type != CCL_DT_FP32 && t.param_type != CCL_DT_BF16) || (t.grad_type != CCL_DT_FP32 && t.grad_type != CCL_DT_BF16))
     return fail(CCL_ERR_INVALID_ARG, "param and grad must be fp32 or bf16");
   if (t.moment_bits != 8 && t.moment_bits != 32) return fail(CCL_ERR_INVALID_ARG, "moments have 8 or 32 bits");
@@ -313,8 +316,9 @@ ccl_status ccl_cross_entropy_grad(const ccl_vocab* vocab, int64_t tokens, const 
   return hip_status(ccl::launch_cross_entropy(s, c, workspace, static_cast<hipStream_t>(stream)), "cross entropy gradient launch");
 }
 
-ccl_status ccl_adamw_step(const ccl_adamw* adamw, const ccl_adamw_tensor* tensors, int64_t count, void* stream) {
-  if (!adamw || count < 0 || (count && !tensors)) return fail(CCL_ERR_INVALID_ARG, "NULL argument, or a negative count");
+ccl_status ccl_adamw_step(const ccl_adamw* adamw, const ccl_adamw_tensor* tensors, int64_t count, void* stream) try {
+  if (!adamw || (count > 0 && !tensors)) return fail(CCL_ERR_INVALID_ARG, "NULL argument");
+  if (count < 0 || count > kMaxTensors) return fail(CCL_ERR_INVALID_ARG, "count must be in 0..2^20");
   if (!std::isfinite(adamw->lr) || !(adamw->beta1 >= 0 && adamw->beta1 < 1) || !(adamw->beta2 >= 0 && adamw->beta2 < 1) ||
       !(adamw->eps >= 0) || !std::isfinite(adamw->eps))
     return fail(CCL_ERR_INVALID_ARG, "lr must be finite, the betas in [0, 1), eps finite and not negative");
@@ -323,21 +327,24 @@ ccl_status ccl_adamw_step(const ccl_adamw* adamw, const ccl_adamw_tensor* tensor
     return fail(CCL_ERR_MISALIGNED_POINTER, "a pointer is not aligned to its elements");
   std::vector<ccl::AdamwTensor> kinds[8];
   std::vector<Span> written;
-  written.reserve(4 * (size_t)count);
-  for (int pass = 0; pass < 4; ++pass)      // one kind of buffer after the other: most callers' are in order
+  written.reserve(6 * (size_t)count);
+  for (int pass = 0; pass < 6; ++pass)      // one kind of buffer after the other: most callers' are in order
     for (int64_t i = 0; i < count; ++i) {
       const ccl_adamw_tensor& t = tensors[i];
       if (pass == 0)
         if (ccl_status s = check_adamw_tensor(t)) return s;
       if (t.n == 0) continue;
-      const int64_t moment = t.moment_bits == 8 ? 1 : 4;
+      const int64_t moment = t.moment_bits == 8 ? t.n : 4 * t.n;
+      const int64_t blocks = t.moment_bits == 8 ? (t.n + ccl::kAdamwBlock - 1) / ccl::kAdamwBlock : 0;
       const auto add = [&](const void* p, int64_t bytes) {
-        if (p) written.push_back({reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (uintptr_t)(bytes * t.n)});
+        if (p) written.push_back({reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (uintptr_t)bytes});
       };
-      if (pass == 0) add(t.param, t.param_type == CCL_DT_FP32 ? 4 : 2);
+      if (pass == 0) add(t.param, t.param_type == CCL_DT_FP32 ? 4 * t.n : 2 * t.n);
       if (pass == 1) add(t.exp_avg, moment);
       if (pass == 2) add(t.exp_avg_sq, moment);
-      if (pass == 3) add(t.copy, 2);
+      if (pass == 3) add(t.copy, 2 * t.n);
+      if (pass == 4 && blocks) add(t.exp_avg_scale, blocks);
+      if (pass == 5 && blocks) add(t.exp_avg_sq_scale, blocks);
     }
   if (overlap(written)) return fail(CCL_ERR_INVALID_ARG, "buffers that the step writes overlap (a tensor given twice?)");
   if (written.empty()) return ok();
@@ -364,18 +371,19 @@ ccl_status ccl_adamw_step(const ccl_adamw* adamw, const ccl_adamw_tensor* tensor
                                            static_cast<hipStream_t>(stream)))
         return hip_status(e, "adamw launch");
   return ok();
+} catch (const std::exception& e) {
+  return fail(CCL_ERR_HIP, e.what());
 }
 
 ccl_status ccl_adamw_moments(int64_t n, const uint8_t* exp_avg, const uint8_t* exp_avg_scale, const uint8_t* exp_avg_sq,
                              const uint8_t* exp_avg_sq_scale, void* m, void* v, ccl_dtype type, void* stream) {
-  if (n < 0 || n > (int64_t)1 << 40) return fail(CCL_ERR_INVALID_ARG, "n must be in 0..2^40");
+  if (n < 0 || n > kMaxElems) return fail(CCL_ERR_INVALID_ARG, "n must be in 0..2^34");
   if (type != CCL_DT_FP32 && type != CCL_DT_BF16) return fail(CCL_ERR_INVALID_ARG, "the values are fp32 or bf16");
   if (n == 0 || (!m && !v)) return ok();
   if ((m && (!exp_avg || !exp_avg_scale)) || (v && (!exp_avg_sq || !exp_avg_sq_scale)))
     return fail(CCL_ERR_INVALID_ARG, "NULL argument");
   if (!aligned(m, type == CCL_DT_FP32 ? 4 : 2) || !aligned(v, type == CCL_DT_FP32 ? 4 : 2))
     return fail(CCL_ERR_MISALIGNED_POINTER, "a pointer is not aligned to its elements");
-  if ((n + 2047) / 2048 > kMaxGrid) return fail(CCL_ERR_UNSUPPORTED, "launch too large");
   if (ccl_status s = check_device()) return s;
   return hip_status(ccl::launch_adamw_moments(n, exp_avg, exp_avg_scale, exp_avg_sq, exp_avg_sq_scale, m, v,
                                               type == CCL_DT_BF16, static_cast<hipStream_t>(stream)),

@@ -238,6 +238,7 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwTable<BITS8> table, Ada
   if (a.lr_ptr || a.step_ptr) {
     if (a.lr_ptr) lr = *a.lr_ptr;
     if (a.step_ptr) step = *a.step_ptr;
+    if (!(__builtin_fabs(lr) < (double)INFINITY) || step < 1) return;
     rate = (float)(lr / (1.0 - power_of(a.beta1, step)));
     root = (float)(1.0 / sqrt(1.0 - power_of(a.beta2, step)));
   }
@@ -327,7 +328,7 @@ hipError_t launch(AdamwParams a, const AdamwTensor* tensors, int64_t count, hipS
     for (; i < count && k < Table::kTensors; ++i) {
       const AdamwTensor& s = tensors[i];
       const int64_t need = (s.n + a.chunk - 1) / a.chunk;
-      if (k && groups + need > 0x7fffffff) break;
+      if (k && groups + need > 0xffffff) break;       // fewer than 2^32 threads
       auto& t = table.t[k++];
       t.param = s.param;
       t.grad = s.grad;

@@ -6,7 +6,7 @@
 //   logits   tiles of X W^T that stay in registers: each leaves the maximum m
 //            and sum of exp(z - m) of every row (fp32), the target's z, and for
 //            the gradient e = exp(z - m) in bf16
-//   combine  rows' lse and loss from the tiles' m and sums, in tile order
+//   combine  rows' lse and loss from the tiles' m and sums, in a fixed order
 //   scale    e -> P', in place: e exp(m - lse) g scale; the target's p - 1 is
 //            expm1(z_t - lse) of the fp32 z_t, since from a rounded p it would
 //            lose everything where p is near 1
@@ -14,6 +14,8 @@
 // Logits in fp32 exist nowhere in memory; P' is kept for a block, 2 bytes each,
 // so that neither gradient has to recompute them (6 T D V operations rather
 // than 8). Rounded to bf16: e, P' (2^-8 each at most), dX and dW once.
+#include <algorithm>
+
 #include "product.hpp"
 
 #include "train_kernels.hpp"
@@ -90,6 +92,8 @@ __global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) logits_kernel
 #pragma unroll
           for (int k = 0; k < WGN; ++k) top[mt] = fmaxf(top[mt], part[k][r]);
           if (wn == 0 && lane < 16) whole[r] = top[mt];
+          // all of a tile's logits -inf: terms of 0, not of exp(-inf + inf)
+          top[mt] = top[mt] == -INFINITY ? 0.f : top[mt];
           sum[mt] = 0.f;
           if (T::row(wm, mt) >= rows) continue;
           // the target's logit
@@ -335,10 +339,10 @@ __global__ void __launch_bounds__(256) ranges_kernel(const float* part, int32_t 
 
 // dW without tokens.
 __global__ void __launch_bounds__(256) zero_kernel(char* out, int64_t rows, int64_t row_chunks, int64_t ld_bytes) {
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (at >= rows * row_chunks) return;
-  const int64_t r = at / row_chunks;
-  *reinterpret_cast<uint4*>(out + r * ld_bytes + (at - r * row_chunks) * 16) = make_uint4(0, 0, 0, 0);
+  for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < rows * row_chunks; at += (int64_t)gridDim.x * 256) {
+    const int64_t r = at / row_chunks;
+    *reinterpret_cast<uint4*>(out + r * ld_bytes + (at - r * row_chunks) * 16) = make_uint4(0, 0, 0, 0);
+  }
 }
 
 template <bool UK, bool VK>
@@ -351,10 +355,14 @@ hipError_t launch_plain(const ProductForm& f, PlainParams p, hipStream_t stream)
   p.ksplit = f.ksplit;
   const auto launch = [&](auto tile) {
     using T = decltype(tile);
-    if (p.part || p.f32 || p.add || p.accumulate)
-      hipLaunchKernelGGL((plain_kernel<T, true>), dim3((unsigned)f.workgroups), dim3(T::THREADS), 0, stream, p);
-    else
-      hipLaunchKernelGGL((plain_kernel<T, false>), dim3((unsigned)f.workgroups), dim3(T::THREADS), 0, stream, p);
+    // dX is nothing more than its product, in ranges or not: 256x256 tiles have none
+    if constexpr (!UK || T::BM < 256) {
+      if (p.part || p.f32 || p.add || p.accumulate) {
+        hipLaunchKernelGGL((plain_kernel<T, true>), dim3((unsigned)f.workgroups), dim3(T::THREADS), 0, stream, p);
+        return;
+      }
+    }
+    hipLaunchKernelGGL((plain_kernel<T, false>), dim3((unsigned)f.workgroups), dim3(T::THREADS), 0, stream, p);
   };
   if (f.tile_m == 256) launch(ProductTile<256, 256, UK, VK, 2, 8, 4, false, true>{});     // KC: columns of P', whole 64s
   else if (f.tile_m == 128) launch(ProductTile<128, 128, UK, VK, 2, 8, 2>{});
@@ -368,8 +376,8 @@ hipError_t launch_cross_entropy(const VocabShape& s, const VocabCall& c, void* w
   if (c.tokens == 0) {
     if (!c.grad || !c.dw || c.accumulate) return hipSuccess;
     const int64_t size = c.dw_f32 ? 4 : 2, chunks = s.hidden * size / 16;
-    hipLaunchKernelGGL(zero_kernel, dim3((unsigned)((s.vocab * chunks + 255) / 256)), dim3(256), 0, stream,
-                       static_cast<char*>(c.dw), s.vocab, chunks, c.dw_ld * size);
+    hipLaunchKernelGGL(zero_kernel, dim3((unsigned)std::min<int64_t>((s.vocab * chunks + 255) / 256, 65536)), dim3(256), 0,
+                       stream, static_cast<char*>(c.dw), s.vocab, chunks, c.dw_ld * size);
     return hipGetLastError();
   }
   const VocabForm f = vocab_form(s, c.tokens, c.grad);

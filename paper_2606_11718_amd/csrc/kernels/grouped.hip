@@ -4,8 +4,8 @@
 //   grad     D = dY W_e, dX = D or dZ of X = act(Z), act(gate) * up
 //   wgrad    dW_e = dY_e^T X_e (+ dW_e)
 // The row counts are on the device only: every workgroup makes a table of the
-// experts' rows and tiles in LDS and takes its tiles from it. Each weight is read by the row tiles of its expert, which run next to each
-// other on one XCD.
+// experts' rows and tiles in LDS and takes its tiles from it. Each weight is read by
+// the row tiles of its expert, which run next to each other on one XCD.
 #include "product.hpp"
 
 #include "train_kernels.hpp"
@@ -89,6 +89,10 @@ __device__ __forceinline__ int32_t expert_of(const ExpertTable& t, int32_t exper
     count += __popcll(__ballot(e + lane < experts && t.before[e + lane] <= row));
   return __builtin_amdgcn_readfirstlane(count - 1);
 }
+
+// 256x256 tiles are taken where they fill the CUs: their K is never in ranges.
+template <typename T>
+constexpr bool kRanges = T::BM < 256;
 
 struct RowWork {
   Side u, v;
@@ -247,10 +251,10 @@ __global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) grouped_rows_
       p.ldu, p.ldv, sm, tid,
       [&](int i, RowWork* w) __attribute__((always_inline)) {
         int32_t id = dealt_tile(i, p.chunk);
-        if (id >= tiles * p.splits) return false;
+        if (id >= (kRanges<T> ? tiles * p.splits : tiles)) return false;
         w->split = 0;
         int32_t k0 = 0, k = p.k;
-        if (p.splits > 1) {
+        if (kRanges<T> && p.splits > 1) {
           w->split = __builtin_amdgcn_readfirstlane(id / tiles);
           id -= w->split * tiles;
           const int32_t per = ((p.k + 63) / 64 + p.splits - 1) / p.splits * 64;
@@ -274,7 +278,7 @@ __global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) grouped_rows_
       },
       [&](int r) __attribute__((always_inline)) { return kPairs ? (r >> 5) * 16 + (r & 15) + (r & 16 ? half : 0) : r; },
       [&](const RowWork& w, f32x4 (&acc)[T::TM][T::TN]) __attribute__((always_inline)) {
-        if (p.part) {
+        if (kRanges<T> && p.part) {
           const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / T::WGN, wn = wave % T::WGN;
 #pragma unroll
           for (int mt = 0; mt < T::TM; ++mt) {
@@ -307,8 +311,8 @@ struct WgradWork {
 };
 
 // dW tiles: rows of dW from dY's columns, columns from X's, K over the expert's rows.
-// What is done with one, apart, since together they take registers that the 256x256
-// tiles' loop needs.
+// What is done with a tile is a kernel of its own each, since together they take
+// registers that the 256x256 tiles' loop needs.
 enum WgradOut { WGRAD_BF16, WGRAD_F32, WGRAD_ANY };
 template <typename T, WgradOut OUT>
 __global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) grouped_wgrad_kernel(GroupedParams p) {
@@ -358,7 +362,7 @@ __global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) grouped_wgrad
         for (int mt = 0; mt < T::TM; ++mt) {
           const int r = T::row(wm, mt) + (lane & 15);
           const bool live = r < w.m;
-          if (OUT == WGRAD_ANY && p.part) {
+          if (kRanges<T> && OUT == WGRAD_ANY && p.part) {
             float* const to = p.part + (((int64_t)w.split * p.experts + w.expert) * p.n + w.row + r) * p.k + w.col;
             partial_row<T>(to, acc[mt], live, w.n, wn, lane, [](int c) { return c; });
             continue;

@@ -1,0 +1,82 @@
+"""The gfx950 assembly of the training operators' kernels, built here from source (no
+GPU needed): direct-to-LDS loads that share an M0 write carry the instruction
+offsets 0, 1024, ... in that order (see test_host_isa); no packed fp32 arithmetic; and
+scratch memory only in the few kernels of 256x256 tiles, whose accumulators take half of the registers, and
+there at most what a handful of values take."""
+import os
+import re
+import shutil
+import subprocess
+from concurrent.futures import ThreadPoolExecutor
+
+import pytest
+
+from paper_2606_11718_amd import build as B
+from tests.test_host_isa_operators import _runs
+
+SOURCES = ("grouped", "cross_entropy", "adamw")
+
+
+@pytest.fixture(scope="module")
+def kernels(tmp_path_factory):
+    """{kernel symbol: (its lines, bytes of scratch)}"""
+    if shutil.which(B.HIPCC) is None and not os.path.exists(B.HIPCC):
+        pytest.skip("hipcc not available")
+    out = tmp_path_factory.mktemp("isa")
+
+    def compile_(name):
+        path = out / (name + ".s")
+        r = subprocess.run([B.HIPCC] + B.HIP_FLAGS + ["-x", "hip", "--cuda-device-only", "-S",
+                                                      os.path.join(B.CSRC, "kernels", name + ".hip"), "-o", str(path)],
+                           capture_output=True, text=True)
+        assert r.returncode == 0, r.stderr[-3000:]
+        text = path.read_text()
+        found = {}
+        for m in re.finditer(r"^(_ZN\w+):", text, re.M):
+            lines = [ln.strip() for ln in text[m.end():text.index(".Lfunc_end", m.end())].splitlines()]
+            size = re.search(rf"\.name:\s+{m.group(1)}\n\s+\.private_segment_fixed_size:\s+(\d+)", text)
+            if size:
+                found[m.group(1)] = (lines, int(size.group(1)))
+        return found
+
+    with ThreadPoolExecutor(len(SOURCES)) as pool:
+        return {k: v for found in pool.map(compile_, SOURCES) for k, v in found.items()}
+
+
+# (kernel, tile): (kernels, lengths of their load runs)
+KINDS = {
+    ("grouped_rows_kernel", "64ELi128"): (4, {1, 2}), ("grouped_rows_kernel", "128ELi128"): (4, {2}),
+    ("grouped_rows_kernel", "256ELi256"): (4, {4}), ("grouped_wgrad_kernel", "128ELi128"): (3, {2}),
+    ("grouped_wgrad_kernel", "256ELi256"): (3, {4}), ("logits_kernel", "64ELi128"): (1, {1, 2}),
+    ("logits_kernel", "128ELi128"): (1, {2}), ("logits_kernel", "256ELi256"): (2, {4}), ("plain_kernel", "64ELi128"): (2, {1, 2}),
+    ("plain_kernel", "128ELi128"): (4, {2}), ("plain_kernel", "256ELi256"): (3, {4}),
+}
+
+
+@pytest.mark.parametrize("kind", list(KINDS), ids="-".join)
+def test_load_runs(kernels, kind):
+    count, lengths = KINDS[kind]
+    found = {n: b for n, b in kernels.items() if kind[0] in n and f"ProductTileILi{kind[1]}E" in n}
+    assert len(found) == count, list(found)
+    for name, (body, _) in found.items():
+        runs = _runs(body)
+        assert len(runs) > 5, name
+        assert all(r == [1024 * i for i in range(len(r))] for r in runs), name
+        assert {len(r) for r in runs} == lengths, name
+
+
+def test_every_kernel_with_such_loads_is_looked_at(kernels):
+    of = {k for k, _ in KINDS}
+    assert sum(c for c, _ in KINDS.values()) == len([n for n in kernels if any(k in n for k in of)])
+    for name, (body, _) in kernels.items():
+        assert not _runs(body) or any(k in name for k in of), name
+
+
+def test_scratch(kernels):
+    for name, (_, size) in kernels.items():
+        assert size == 0 or ("ProductTileILi256ELi256E" in name and size <= 40), (name, size)
+
+
+def test_no_packed_fp32(kernels):
+    for name, (body, _) in kernels.items():
+        assert not [ln for ln in body if re.match(r"v_pk_(add|mul|fma)_f32", ln)], name

@@ -1,5 +1,7 @@
 """What the training operators and their queries refuse (every refusal comes
 before the first device call)."""
+import ctypes
+
 import pytest
 import torch
 
@@ -190,7 +192,7 @@ def _entry(**change):
 
 @pytest.mark.parametrize("change,status", [
     (dict(param=None), INV), (dict(grad=None), INV), (dict(exp_avg=None), INV), (dict(exp_avg_sq=None), INV), (dict(n=-1), INV),
-    (dict(n=(1 << 40) + 1), INV), (dict(param_type=1), INV), (dict(grad_type=1), INV), (dict(moment_bits=16), INV),
+    (dict(n=(1 << 34) + 1), INV), (dict(param_type=1), INV), (dict(grad_type=1), INV), (dict(moment_bits=16), INV),
     (dict(moment_bits=8), INV), (dict(moment_bits=8, exp_avg_scale=P), INV), (dict(weight_decay=float("nan")), INV),
     (dict(param=P + 2), MIS), (dict(grad=P + 2), MIS), (dict(exp_avg=P + 2), MIS), (dict(exp_avg_sq=P + 2), MIS),
     (dict(copy=P + 1), MIS), (dict(param=P + 1, param_type=0), MIS), (dict(exp_avg=P), INV), (dict(copy=P + 100), INV),
@@ -204,6 +206,16 @@ def test_adamw_the_same_tensor_twice():
     _refused(INV, ccl.ccl_adamw_step, ccl.ccl_adamw([_entry(), _entry(param=9 * P, exp_avg=10 * P)]), lr=1e-3, step=1)
     _refused(INV, ccl.ccl_adamw_step, ccl.ccl_adamw([_entry(), _entry(param=P - 3996, exp_avg=10 * P, exp_avg_sq=11 * P)]),
              lr=1e-3, step=1)
+    eight = dict(moment_bits=8, exp_avg_scale=5 * P, exp_avg_sq_scale=6 * P)
+    _refused(INV, ccl.ccl_adamw_step, ccl.ccl_adamw([_entry(**{**eight, "exp_avg_sq_scale": 5 * P})]), lr=1e-3, step=1)
+    other = dict(param=9 * P, exp_avg=10 * P, exp_avg_sq=11 * P, exp_avg_scale=12 * P)
+    _refused(INV, ccl.ccl_adamw_step, ccl.ccl_adamw([_entry(**eight), _entry(**{**eight, **other})]), lr=1e-3, step=1)
+
+
+def test_adamw_count():
+    for count in (-1, (1 << 20) + 1, 1 << 62):
+        a = ccl._Adamw(1e-3, 0.9, 0.999, 1e-8, 1, None, None, None)
+        assert ccl.library().ccl_adamw_step(ctypes.byref(a), ctypes.byref(_entry()[0]), count, None) == 1, count
 
 
 @pytest.mark.parametrize("more", [dict(step=0), dict(step=-5), dict(step=1, lr=float("inf")), dict(step=1, beta1=1.0),
