@@ -106,9 +106,15 @@ bool large_tiles(int64_t m, int64_t n, int splits = 1) {
   return up(m, 256) * 256 <= up(m, 128) * 128 * 5 / 4 && up(m, 256) * up(n, 256) * splits >= 256;
 }
 
+// Few tiles wait for memory step by step: 64x128 ones while that is no more than one
+// a CU (1000 tokens of 4096 x 1200 36.5 us, in tiles of 128x128 with as many stages as
+// the LDS holds 41.9, with two 51.2; 135 of 4112 x 1381 36.4 / 43.3 / 58.5), and one
+// 128x128 tile a CU with four stages where two would have two (250 of 4096 x 16000
+// 46 / 65, 200 of 2048 x 16000 27 / 31; the kernel's choice).
 ProductForm vocab_logits_form(const VocabShape& s, int64_t tokens) {
   if (large_tiles(tokens, s.vocab)) return product_form(tokens, s.vocab, 256, 256, up(s.hidden, 64), 1);
-  return product_form(tokens, s.vocab, tokens <= 64 ? 64 : 128, 128, up(s.hidden, 64), 1);
+  const bool few = tokens <= 64 || up(tokens, 64) * up(s.vocab, 128) <= 256;
+  return product_form(tokens, s.vocab, few ? 64 : 128, 128, up(s.hidden, 64), 1);
 }
 
 ProductForm vocab_dx_form(const VocabShape& s, int64_t tokens) {

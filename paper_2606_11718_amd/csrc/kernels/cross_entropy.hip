@@ -419,6 +419,7 @@ hipError_t launch_cross_entropy(const VocabShape& s, const VocabCall& c, void* w
     };
     if (z.tile_m == 256 && s.hidden % 64 == 0) logits(ProductTile<256, 256, true, true, 2, 8, 4, false, true>{});
     else if (z.tile_m == 256) logits(ProductTile<256, 256, true, true, 2, 8, 4>{});
+    else if (z.tile_m == 128 && z.tiles <= 256) logits(ProductTile<128, 128, true, true, 4, 8, 2>{});
     else if (z.tile_m == 128) logits(ProductTile<128, 128, true, true, 2, 8, 2>{});
     else logits(ProductTile<64, 128, true, true, 3, 8, 2, true>{});
     if (hipError_t e = hipGetLastError()) return e;

@@ -23,6 +23,8 @@ def test_loss_cases():
     for tile, cases in F.LOGITS.items():
         for t, D, V in cases:
             assert F.ask("logits", D, V, t)["tile_m"] == tile, (t, D, V)
+    # both numbers of stages
+    assert {F.ask("logits", D, V, t)["tiles"] <= 256 for t, D, V in F.LOGITS[128]} == {True, False}
     for form, cases in F.DX.items():
         for t, D, V in cases:
             got = F.ask("dx", D, V, t)

@@ -46,7 +46,8 @@ GROUPED = {
                    (WGRAD, [70, 0, 130, 1], 2000, 2032, False)],
 }
 # loss: (tokens, hidden, vocab)
-LOGITS = {64: [(1, 2064, 1000), (64, 48, 700)], 128: [(65, 80, 700), (300, 336, 2049)], 256: [(250, 80, 65400), (1000, 128, 16300)]}
+LOGITS = {64: [(1, 2064, 1000), (64, 48, 700), (65, 80, 700), (300, 336, 2049), (64, 32, 40000)],
+          128: [(300, 336, 8001), (130, 16, 16300), (300, 80, 12000)], 256: [(250, 80, 65400), (1000, 128, 16300)]}
 # (tile rows, K ranges or not)
 DX = {(64, True): [(3, 80, 3000), (64, 272, 2100)], (64, False): [(50, 80, 700)], (128, True): [(130, 272, 2100)],
       (128, False): [(130, 80, 700)], (256, False): [(2000, 8176, 300)]}
