@@ -97,8 +97,8 @@ ccl_status check_vocab(const ccl_vocab* v, int64_t tokens, bool grad, ccl::Vocab
   if (s.w_ld % 8) return fail(CCL_ERR_MISALIGNED_POINTER, "rows of W must lie whole 16 bytes apart");
   if (tokens) {
     const ccl::VocabForm f = ccl::vocab_form(s, tokens, grad);
-    if (ccl::vocab_logits_form(s, f.block).tiles > kMaxGrid / 2 || ccl::vocab_dw_form(s, f.block).tiles > kMaxGrid / 2 ||
-        ccl::vocab_dx_form(s, f.block).tiles > kMaxGrid / 2 || (f.block * s.hidden + 1023) / 1024 > kMaxGrid)
+    if (ccl::vocab_logits_form(s, f.block, s.vocab, false).tiles > kMaxGrid / 2 ||
+        ccl::vocab_dw_form(s, f.block, s.vocab, false).tiles > kMaxGrid / 2 || ccl::vocab_dx_form(s, f.block, false).tiles > kMaxGrid / 2 || (f.block * s.hidden + 1023) / 1024 > kMaxGrid)
       return fail(CCL_ERR_UNSUPPORTED, "launch too large");
   }
   *out = s;

@@ -9,10 +9,10 @@ namespace {
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // fp32 tiles of all K ranges of a product, at most: ranges are made while tiles times
-// ranges fit 512 workgroups of 128 x 128.
-constexpr int64_t kPartBytes = (int64_t)512 * 128 * 128 * 4;
+// ranges fit 512 workgroups of 128 x 128, or 256 of 256 x 256.
+constexpr int64_t kPartBytes = (int64_t)512 * 128 * 128 * 4, kLargePartBytes = (int64_t)256 * 256 * 256 * 4;
 constexpr int kMaxRanges = 64;
-int64_t part_bound(int64_t elems) { return std::min<int64_t>(kPartBytes, 4 * kMaxRanges * elems); }
+int64_t part_bound(int64_t elems, int64_t most) { return std::min<int64_t>(most, 4 * kMaxRanges * elems); }
 
 }  // namespace
 
@@ -75,7 +75,8 @@ GroupedForm grouped_form(const GroupedShape& s, int64_t rows, int direction) {
 int64_t grouped_workspace(const GroupedShape& s, int64_t rows, int direction) {
   const int64_t k = direction == GROUPED_WGRAD ? rows : direction == GROUPED_FORWARD ? s.in : s.out;
   if (up(k, 64) < 8 || rows == 0) return 0;
-  return part_bound(direction == GROUPED_WGRAD ? s.experts * s.out * s.in : rows * (direction == GROUPED_FORWARD ? s.out : s.in));
+  return part_bound(direction == GROUPED_WGRAD ? s.experts * s.out * s.in : rows * (direction == GROUPED_FORWARD ? s.out : s.in),
+                    kPartBytes);
 }
 
 namespace {
@@ -101,33 +102,67 @@ ProductForm product_form(int64_t m, int64_t n, int tile_m, int tile_n, int64_t k
 
 }  // namespace
 
-// 256x256 tiles where they are not mostly padding and fill the CUs.
-bool large_tiles(int64_t m, int64_t n, int splits = 1) {
-  return up(m, 256) * 256 <= up(m, 128) * 128 * 5 / 4 && up(m, 256) * up(n, 256) * splits >= 256;
+namespace {
+
+// 256x256 tiles where they are not mostly padding and, `ranges` of them, fill the CUs.
+bool large_tiles(int64_t m, int64_t n, int64_t ranges = 1) {
+  return up(m, 256) * 256 <= up(m, 128) * 128 * 5 / 4 && up(m, 256) * up(n, 256) * ranges >= 256;
 }
+
+// Of n columns (of the vocabulary, or tokens) by m, those whose 256x256 tiles are whole
+// rounds of the 256 CUs, where the tiles of a last round that is not whole are a round
+// or less of 128x128 ones: all otherwise. (Loss of 4096 tokens, 4096 x 4352 144 / 191 us
+// in one piece, of 5461, 576 x 3216 44 / 52; with both gradients 1003 of 2048 x 50257
+// 652 / 685, 1024 of 512 x 20000 131 / 140; no shape tried was slower.)
+int64_t whole_rounds(int64_t n, int64_t m, int64_t k) {
+  const int64_t across = up(m, 256), tiles = across * up(n, 256), whole = tiles / 256 * 256 / across * 256;
+  if (tiles % 256 == 0 || whole == 0 || k < 512 || up(n - whole, 128) * up(m, 128) > 512) return n;
+  return whole;
+}
+
+}  // namespace
+
 
 // Few tiles wait for memory step by step: 64x128 ones while that is no more than one
 // a CU (1000 tokens of 4096 x 1200 36.5 us, in tiles of 128x128 with as many stages as
 // the LDS holds 41.9, with two 51.2; 135 of 4112 x 1381 36.4 / 43.3 / 58.5), and one
 // 128x128 tile a CU with four stages where two would have two (250 of 4096 x 16000
 // 46 / 65, 200 of 2048 x 16000 27 / 31; the kernel's choice).
-ProductForm vocab_logits_form(const VocabShape& s, int64_t tokens) {
-  if (large_tiles(tokens, s.vocab)) return product_form(tokens, s.vocab, 256, 256, up(s.hidden, 64), 1);
-  const bool few = tokens <= 64 || up(tokens, 64) * up(s.vocab, 128) <= 256;
-  return product_form(tokens, s.vocab, few ? 64 : 128, 128, up(s.hidden, 64), 1);
+ProductForm vocab_logits_form(const VocabShape& s, int64_t tokens, int64_t columns, bool large) {
+  if (large) return product_form(tokens, columns, 256, 256, up(s.hidden, 64), 1);
+  const bool few = tokens <= 64 || up(tokens, 64) * up(columns, 128) <= 256;
+  return product_form(tokens, columns, few ? 64 : 128, 128, up(s.hidden, 64), 1);
 }
 
-ProductForm vocab_dx_form(const VocabShape& s, int64_t tokens) {
-  if (large_tiles(tokens, s.hidden)) return product_form(tokens, s.hidden, 256, 256, up(s.vocab, 64), 1);
+int64_t vocab_logits_large(const VocabShape& s, int64_t tokens) {
+  return large_tiles(tokens, s.vocab) ? whole_rounds(s.vocab, tokens, s.hidden) : 0;
+}
+int64_t vocab_dx_large(const VocabShape& s, int64_t tokens) {
+  return large_tiles(tokens, s.hidden) ? whole_rounds(tokens, s.hidden, s.vocab) : 0;
+}
+int64_t vocab_dw_large(const VocabShape& s, int64_t tokens) {
+  return large_tiles(s.vocab, s.hidden) ? whole_rounds(s.vocab, s.hidden, tokens) : 0;
+}
+
+// K ranges of 256x256 tiles against those of 128x128 ones, which are twice as many and
+// leave half as much to add up (loss and both gradients): 1003 tokens of 2048 x 50257
+// 681 / 730, 1024 of 1024 x 128000 908 / 982, 1500 of 2560 x 9000 270 / 278, but where a
+// range is 1000 to 1250 columns 768 of 2048 x 8000 119 / 112, 4096 of 512 x 8000 195 / 174.
+ProductForm vocab_dx_form(const VocabShape& s, int64_t tokens, bool large) {
+  if (large) return product_form(tokens, s.hidden, 256, 256, up(s.vocab, 64), 1);
+  const int64_t larges = up(tokens, 256) * up(s.hidden, 256);
+  const int64_t ranges = std::min<int64_t>(std::min<int64_t>(256 / larges, kMaxRanges), s.vocab / 2048);
+  if (larges * ranges >= 192 && large_tiles(tokens, s.hidden, 256))
+    return product_form(tokens, s.hidden, 256, 256, up(s.vocab, 64), (int)ranges);
   const int tile_m = tokens <= 64 ? 64 : 128;
   const int64_t tiles = up(tokens, tile_m) * up(s.hidden, 128);
   const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / tiles, kMaxRanges), up(s.vocab, 1024)));
   return product_form(tokens, s.hidden, tile_m, 128, up(s.vocab, 64), (int)splits);
 }
 
-ProductForm vocab_dw_form(const VocabShape& s, int64_t tokens) {
-  if (large_tiles(s.vocab, s.hidden)) return product_form(s.vocab, s.hidden, 256, 256, up(tokens, 64), 1);
-  return product_form(s.vocab, s.hidden, 128, 128, up(tokens, 64), 1);
+ProductForm vocab_dw_form(const VocabShape& s, int64_t tokens, int64_t columns, bool large) {
+  const int tile = large ? 256 : 128;
+  return product_form(columns, s.hidden, tile, tile, up(tokens, 64), 1);
 }
 
 VocabForm vocab_form(const VocabShape& s, int64_t tokens, bool grad) {
@@ -150,7 +185,7 @@ VocabForm vocab_form(const VocabShape& s, int64_t tokens, bool grad) {
   if (grad) {
     f.e_at = take(2 * f.block * f.e_ld);
     f.rows_at = take(2 * f.block * s.hidden);
-    f.part_at = take(part_bound(f.block * s.hidden));
+    f.part_at = take(part_bound(f.block * s.hidden, kLargePartBytes));
     f.sum_at = take(f.blocks > 1 ? 4 * s.vocab * s.hidden : 0);
   }
   f.workspace_bytes = at;

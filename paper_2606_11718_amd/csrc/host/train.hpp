@@ -53,10 +53,16 @@ struct VocabForm {
 // a copy of its x,
 // the ranges' partial dX and, where dW is rounded after several blocks, its fp32 sum.
 VocabForm vocab_form(const VocabShape& s, int64_t tokens, bool grad);
-// The products of a block of `tokens`: logits, dX, dW.
-ProductForm vocab_logits_form(const VocabShape& s, int64_t tokens);
-ProductForm vocab_dx_form(const VocabShape& s, int64_t tokens);
-ProductForm vocab_dw_form(const VocabShape& s, int64_t tokens);
+// The products of a block of `tokens`: logits and dW, each in 256x256 tiles over the
+// first vocab_..._large columns of the vocabulary (whole tiles, or all, or 0) and in
+// smaller ones over the others.
+int64_t vocab_logits_large(const VocabShape& s, int64_t tokens);
+int64_t vocab_dw_large(const VocabShape& s, int64_t tokens);
+ProductForm vocab_logits_form(const VocabShape& s, int64_t tokens, int64_t columns, bool large);
+ProductForm vocab_dw_form(const VocabShape& s, int64_t tokens, int64_t columns, bool large);
+// dX of the first vocab_dx_large tokens, and of the others (all, if that is 0), in two calls.
+int64_t vocab_dx_large(const VocabShape& s, int64_t tokens);
+ProductForm vocab_dx_form(const VocabShape& s, int64_t tokens, bool large);
 
 // ---- AdamW ----
 constexpr int kAdamwTensors[2] = {68, 54};    // of a launch (moments of 32, 8 bits): their table is a kernel argument

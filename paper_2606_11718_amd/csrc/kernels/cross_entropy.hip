@@ -28,10 +28,11 @@ struct LogitsParams {
   const uint16_t *X, *W;
   const int64_t* targets;
   float* target_z;         // [tokens]
-  float2* stat;            // [tokens][tiles_n]: maximum, sum
+  float2* stat;            // [tokens][stat_ld], of these tiles: maximum, sum
   uint16_t* E;             // [tokens][e_ld], or null
   int64_t x_ld, w_ld, e_ld;
-  int32_t tokens, vocab, hidden, e_cols;
+  int32_t tokens, vocab, hidden, e_cols;    // vocab, e_cols: from the first column on
+  int32_t first, stat_ld;                   // this launch's first column
   int32_t tiles_m, tiles_n, group, chunk;
   float scale;
 };
@@ -98,7 +99,7 @@ __global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) logits_kernel
           if (T::row(wm, mt) >= rows) continue;
           // the target's logit
           if (r < rows) {
-            const int64_t t = p.targets[w.ti * BM + r] - col0;
+            const int64_t t = p.targets[w.ti * BM + r] - p.first - col0;
             if (t >= 0 && t < T::WN && t < left) {
 #pragma unroll
               for (int nt = 0; nt < TN; ++nt)
@@ -135,7 +136,7 @@ __global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) logits_kernel
           float s = 0.f;
 #pragma unroll
           for (int k = 0; k < WGN; ++k) s += part[k][tid];
-          p.stat[(int64_t)(w.ti * BM + tid) * p.tiles_n + w.tj] = make_float2(whole[tid], s);
+          p.stat[(int64_t)(w.ti * BM + tid) * p.stat_ld + w.tj] = make_float2(whole[tid], s);
         }
         // the next tile's finish writes part again
         product_barrier<63>();
@@ -203,7 +204,8 @@ struct ScaleParams {
   const float* target_z;
   const int64_t* targets;
   int64_t e_ld;
-  int32_t vocab, e_cols, tiles_n, tile_shift;
+  int32_t vocab, e_cols, tiles_n;
+  int32_t large;           // columns in tiles of 256, the others' are 128 wide
 };
 
 // e -> P', eight a thread.
@@ -217,7 +219,8 @@ __global__ void __launch_bounds__(256) scale_kernel(ScaleParams p) {
     return;
   }
   const uint4 e = *at;
-  const float k = __builtin_amdgcn_exp2f((p.stat[(int64_t)row * p.tiles_n + (col >> p.tile_shift)].x - f.x) * kLog2e) * f.y;
+  const int32_t tile = col < p.large ? col >> 8 : ((p.large + 255) >> 8) + ((col - p.large) >> 7);
+  const float k = __builtin_amdgcn_exp2f((p.stat[(int64_t)row * p.tiles_n + tile].x - f.x) * kLog2e) * f.y;
   f32x4 lo = bf16x4_to_f32(make_uint2(e.x, e.y)) * k, hi = bf16x4_to_f32(make_uint2(e.z, e.w)) * k;
   const int64_t t = p.targets[row] - col;
   if (t >= 0 && t < 8) {
@@ -355,14 +358,10 @@ hipError_t launch_plain(const ProductForm& f, PlainParams p, hipStream_t stream)
   p.ksplit = f.ksplit;
   const auto launch = [&](auto tile) {
     using T = decltype(tile);
-    // dX is nothing more than its product, in ranges or not: 256x256 tiles have none
-    if constexpr (!UK || T::BM < 256) {
-      if (p.part || p.f32 || p.add || p.accumulate) {
-        hipLaunchKernelGGL((plain_kernel<T, true>), dim3((unsigned)f.workgroups), dim3(T::THREADS), 0, stream, p);
-        return;
-      }
-    }
-    hipLaunchKernelGGL((plain_kernel<T, false>), dim3((unsigned)f.workgroups), dim3(T::THREADS), 0, stream, p);
+    if (p.part || p.f32 || p.add || p.accumulate)
+      hipLaunchKernelGGL((plain_kernel<T, true>), dim3((unsigned)f.workgroups), dim3(T::THREADS), 0, stream, p);
+    else
+      hipLaunchKernelGGL((plain_kernel<T, false>), dim3((unsigned)f.workgroups), dim3(T::THREADS), 0, stream, p);
   };
   if (f.tile_m == 256) launch(ProductTile<256, 256, UK, VK, 2, 8, 4, false, true>{});     // KC: columns of P', whole 64s
   else if (f.tile_m == 128) launch(ProductTile<128, 128, UK, VK, 2, 8, 2>{});
@@ -393,36 +392,48 @@ hipError_t launch_cross_entropy(const VocabShape& s, const VocabCall& c, void* w
     const int64_t first = b * f.block, n = c.tokens - first < f.block ? c.tokens - first : f.block;
     const uint16_t* X = static_cast<const uint16_t*>(c.x) + first * c.x_ld;
     const uint16_t* W = static_cast<const uint16_t*>(c.w);
-    const ProductForm z = vocab_logits_form(s, n);
+    const int64_t large = vocab_logits_large(s, n);
+    const int32_t tiles_n = (int32_t)((large + 255) / 256 + (s.vocab - large + 127) / 128);
     LogitsParams lp{};
     lp.X = X;
-    lp.W = W;
     lp.targets = c.targets + first;
     lp.target_z = target_z;
-    lp.stat = stat;
-    lp.E = E;
     lp.x_ld = c.x_ld;
     lp.w_ld = s.w_ld;
     lp.e_ld = f.e_ld;
     lp.tokens = (int32_t)n;
-    lp.vocab = (int32_t)s.vocab;
     lp.hidden = (int32_t)s.hidden;
-    lp.e_cols = f.e_cols;
-    lp.tiles_m = z.tiles_m;
-    lp.tiles_n = z.tiles_n;
-    lp.group = z.group;
-    lp.chunk = z.chunk;
     lp.scale = s.scale;
+    lp.stat_ld = tiles_n;
+    ProductForm z;
     const auto logits = [&](auto tile) {
       using T = decltype(tile);
       hipLaunchKernelGGL(logits_kernel<T>, dim3((unsigned)z.workgroups), dim3(T::THREADS), 0, stream, lp);
     };
-    if (z.tile_m == 256 && s.hidden % 64 == 0) logits(ProductTile<256, 256, true, true, 2, 8, 4, false, true>{});
-    else if (z.tile_m == 256) logits(ProductTile<256, 256, true, true, 2, 8, 4>{});
-    else if (z.tile_m == 128 && z.tiles <= 256) logits(ProductTile<128, 128, true, true, 4, 8, 2>{});
-    else if (z.tile_m == 128) logits(ProductTile<128, 128, true, true, 2, 8, 2>{});
-    else logits(ProductTile<64, 128, true, true, 3, 8, 2, true>{});
-    if (hipError_t e = hipGetLastError()) return e;
+    // columns `from` to `to` - 1, tiles `nth` on of a row's
+    const auto part_of = [&](int64_t from, int64_t to, int64_t nth) {
+      z = vocab_logits_form(s, n, to - from, to <= large);
+      lp.W = W + from * s.w_ld;
+      lp.E = E ? E + from : nullptr;
+      lp.first = (int32_t)from;
+      lp.stat = stat + nth;
+      lp.vocab = (int32_t)(to - from);
+      lp.e_cols = (int32_t)((to < s.vocab ? to : f.e_cols) - from);
+      lp.tiles_m = z.tiles_m;
+      lp.tiles_n = z.tiles_n;
+      lp.group = z.group;
+      lp.chunk = z.chunk;
+      if (z.tile_m == 256 && s.hidden % 64 == 0) logits(ProductTile<256, 256, true, true, 2, 8, 4, false, true>{});
+      else if (z.tile_m == 256) logits(ProductTile<256, 256, true, true, 2, 8, 4>{});
+      else if (z.tile_m == 128 && z.tiles <= 256) logits(ProductTile<128, 128, true, true, 4, 8, 2>{});
+      else if (z.tile_m == 128) logits(ProductTile<128, 128, true, true, 2, 8, 2>{});
+      else logits(ProductTile<64, 128, true, true, 3, 8, 2, true>{});
+      return hipGetLastError();
+    };
+    if (large)
+      if (hipError_t e = part_of(0, large, 0)) return e;
+    if (large < s.vocab)
+      if (hipError_t e = part_of(large, s.vocab, (large + 255) / 256)) return e;
     CombineParams cp{};
     cp.stat = stat;
     cp.target_z = target_z;
@@ -433,7 +444,7 @@ hipError_t launch_cross_entropy(const VocabShape& s, const VocabCall& c, void* w
     cp.factor = c.grad ? factor : nullptr;
     cp.tokens = (int32_t)n;
     cp.vocab = (int32_t)s.vocab;
-    cp.tiles_n = z.tiles_n;
+    cp.tiles_n = tiles_n;
     cp.scale = s.scale;
     cp.X = X;
     cp.x_ld = c.x_ld;
@@ -452,41 +463,45 @@ hipError_t launch_cross_entropy(const VocabShape& s, const VocabCall& c, void* w
     sp.e_ld = f.e_ld;
     sp.vocab = (int32_t)s.vocab;
     sp.e_cols = f.e_cols;
-    sp.tiles_n = z.tiles_n;
-    sp.tile_shift = __builtin_ctz(z.tile_n);
+    sp.tiles_n = tiles_n;
+    sp.large = large < s.vocab ? (int32_t)large : f.e_cols;
     hipLaunchKernelGGL(scale_kernel, dim3((unsigned)((f.e_cols / 8 + 255) / 256), (unsigned)n), dim3(256), 0, stream, sp);
     if (hipError_t e = hipGetLastError()) return e;
     if (c.dx) {
-      const ProductForm d = vocab_dx_form(s, n);
       PlainParams p{};
-      p.U = E;
       p.ldu = f.e_ld;
       p.V = W;
       p.ldv = s.w_ld;
-      p.m = (int32_t)n;
       p.n = p.nv = (int32_t)s.hidden;
       p.ku = f.e_cols;
       p.kv = (int32_t)s.vocab;
       p.ksteps = f.e_cols / 64;
-      p.out = static_cast<uint16_t*>(c.dx) + first * c.dx_ld;
       p.ld_out = c.dx_ld;
-      p.part = d.splits > 1 ? part : nullptr;
-      if (hipError_t e = launch_plain<true, false>(d, p, stream)) return e;
-      if (d.splits > 1) {
-        const int64_t elems = n * s.hidden;
+      const int64_t whole = vocab_dx_large(s, n);
+      const auto rows_of = [&](int64_t from, int64_t to) {
+        const ProductForm d = vocab_dx_form(s, to - from, to <= whole);
+        uint16_t* const out = static_cast<uint16_t*>(c.dx) + (first + from) * c.dx_ld;
+        p.U = E + from * f.e_ld;
+        p.m = (int32_t)(to - from);
+        p.out = out;
+        p.part = d.splits > 1 ? part : nullptr;
+        const hipError_t e = launch_plain<true, false>(d, p, stream);
+        if (e || d.splits == 1) return e;
+        const int64_t elems = (to - from) * s.hidden;
         hipLaunchKernelGGL(ranges_kernel, dim3((unsigned)((elems / 4 + 255) / 256)), dim3(256), 0, stream, part, d.splits, elems,
-                           (int32_t)s.hidden, static_cast<uint16_t*>(p.out), c.dx_ld);
-        if (hipError_t e = hipGetLastError()) return e;
-      }
+                           (int32_t)s.hidden, out, c.dx_ld);
+        return hipGetLastError();
+      };
+      if (whole)
+        if (hipError_t e = rows_of(0, whole)) return e;
+      if (whole < n)
+        if (hipError_t e = rows_of(whole, n)) return e;
     }
     if (c.dw) {
       PlainParams p{};
-      p.U = E;
       p.ldu = f.e_ld;
       p.V = rows;
       p.ldv = s.hidden;
-      p.m = (int32_t)s.vocab;
-      p.mu = f.e_cols;
       p.n = p.nv = (int32_t)s.hidden;
       p.ku = p.kv = (int32_t)n;
       p.ksteps = (int32_t)((n + 63) / 64);
@@ -497,7 +512,20 @@ hipError_t launch_cross_entropy(const VocabShape& s, const VocabCall& c, void* w
       p.f32 = c.dw_f32 || !last;
       p.accumulate = c.dw_f32 ? c.accumulate || b > 0 : last ? c.accumulate : b > 0;
       p.add = !c.dw_f32 && last && b > 0 ? sum : nullptr;
-      if (hipError_t e = launch_plain<false, false>(vocab_dw_form(s, n), p, stream)) return e;
+      const int64_t whole = vocab_dw_large(s, n), size = p.f32 ? 4 : 2;
+      const auto rows_of = [&](int64_t from, int64_t to) {
+        PlainParams q = p;
+        q.U = E + from;
+        q.m = (int32_t)(to - from);
+        q.mu = (int32_t)(f.e_cols - from);
+        q.out = static_cast<char*>(p.out) + from * p.ld_out * size;
+        q.add = p.add ? p.add + from * s.hidden : nullptr;
+        return launch_plain<false, false>(vocab_dw_form(s, n, to - from, to <= whole), q, stream);
+      };
+      if (whole)
+        if (hipError_t e = rows_of(0, whole)) return e;
+      if (whole < s.vocab)
+        if (hipError_t e = rows_of(whole, s.vocab)) return e;
     }
   }
   return hipSuccess;

@@ -38,6 +38,17 @@ def test_logits(tokens, D, V):
     TC.run(tokens, D, V, pad=8)
 
 
+@pytest.mark.parametrize("tokens,D,V", F.DX_REST)
+def test_dx_of_whole_rounds_and_the_rest(tokens, D, V):
+    TC.run(tokens, D, V, grad=True, pad=8, only="dX")
+
+
+@pytest.mark.parametrize("dw,accumulate", [("bf16", False), ("fp32", True)])
+@pytest.mark.parametrize("tokens,D,V", [c for cases in F.LOGITS_REST.values() for c in cases] + F.DW_REST)
+def test_whole_rounds_and_the_rest(tokens, D, V, dw, accumulate):
+    TC.run(tokens, D, V, grad=True, pad=8, dw=dw, accumulate=accumulate)
+
+
 @pytest.mark.parametrize("tokens,D,V", [c for cases in F.DX.values() for c in cases])
 def test_dx(tokens, D, V):
     TC.run(tokens, D, V, grad=True, pad=8, only="dX")

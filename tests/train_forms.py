@@ -48,7 +48,11 @@ GROUPED = {
 # loss: (tokens, hidden, vocab)
 LOGITS = {64: [(1, 2064, 1000), (64, 48, 700), (65, 80, 700), (300, 336, 2049), (64, 32, 40000)],
           128: [(300, 336, 8001), (130, 16, 16300), (300, 80, 12000)], 256: [(250, 80, 65400), (1000, 128, 16300)]}
+# 256x256 tiles over whole rounds, 64x128 and 128x128 ones over the columns behind them
+LOGITS_REST = {64: [(1000, 528, 16701)], 128: [(2290, 512, 8257)]}
+DX_REST = [(9000, 2080, 600), (15000, 1040, 2100)]
+DW_REST = [(520, 1040, 13900)]
 # (tile rows, K ranges or not)
 DX = {(64, True): [(3, 80, 3000), (64, 272, 2100)], (64, False): [(50, 80, 700)], (128, True): [(130, 272, 2100)],
-      (128, False): [(130, 80, 700)], (256, False): [(2000, 8176, 300)]}
+      (128, False): [(130, 80, 700)], (256, False): [(2000, 8176, 300)], (256, True): [(400, 1040, 49999)]}
 DW = {128: [(70, 272, 2100)], 256: [(70, 4080, 4001)]}
