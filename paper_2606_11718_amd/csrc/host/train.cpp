@@ -14,11 +14,11 @@ constexpr int64_t kPartBytes = (int64_t)512 * 128 * 128 * 4, kLargePartBytes = (
 constexpr int kMaxRanges = 64;
 int64_t part_bound(int64_t elems, int64_t most) { return std::min<int64_t>(most, 4 * kMaxRanges * elems); }
 
-}  // namespace
-
 // Workgroups that stay and take `tiles` in turn, per_cu of them on a CU; one for
 // every tile where there are fewer (a multiple of 8: XCDs).
 int64_t resident(int64_t tiles, int per_cu) { return std::min<int64_t>(up(std::max<int64_t>(tiles, 1), 8) * 8, 256 * per_cu); }
+
+}  // namespace
 
 // Tiles, measured (us, 256x256 against 128x128 tiles, of which two workgroups share a
 // CU): a large tile moves half as much through LDS for each product, but hides
@@ -100,10 +100,6 @@ ProductForm product_form(int64_t m, int64_t n, int tile_m, int tile_n, int64_t k
   return f;
 }
 
-}  // namespace
-
-namespace {
-
 // 256x256 tiles where they are not mostly padding and, `ranges` of them, fill the CUs.
 bool large_tiles(int64_t m, int64_t n, int64_t ranges = 1) {
   return up(m, 256) * 256 <= up(m, 128) * 128 * 5 / 4 && up(m, 256) * up(n, 256) * ranges >= 256;
@@ -121,7 +117,6 @@ int64_t whole_rounds(int64_t n, int64_t m, int64_t k) {
 }
 
 }  // namespace
-
 
 // Few tiles wait for memory step by step: 64x128 ones while that is no more than one
 // a CU (1000 tokens of 4096 x 1200 36.5 us, in tiles of 128x128 with as many stages as
