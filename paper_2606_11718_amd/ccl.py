@@ -529,6 +529,14 @@ def _here(**tensors) -> None:
             _refuse(name, f"a tensor on {t.device}, not on the current GPU")
 
 
+def _room(workspace, nbytes: int):
+    """The address of a workspace of that many bytes, which a tensor has to hold."""
+    if workspace is not None and not isinstance(workspace, int):
+        if not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < nbytes:
+            _refuse("workspace", f"a tensor that does not hold {nbytes} contiguous bytes")
+    return _ptr(workspace)
+
+
 CCL_GROUPED_FORWARD, CCL_GROUPED_GRAD, CCL_GROUPED_WGRAD = 0, 1, 2
 
 
@@ -559,7 +567,7 @@ def ccl_grouped_gemm(grouped: _Grouped, rows: int, ends, X, W, Y, *, preact=None
     preact, z_ld = _rows("preact", preact, z_ld, rows, N, bf16, bits)
     W = _expert_weights("W", W, E, N, K, grouped.w_ld, grouped.w_stride, bf16)
     _check(call(ctypes.byref(grouped), rows, _whole("ends", ends, E, torch.int32), X, x_ld, W, Y, y_ld, preact, z_ld,
-                _ptr(workspace), workspace_bytes, _stream(stream)))
+                _room(workspace, workspace_bytes), workspace_bytes, _stream(stream)))
 
 
 def ccl_grouped_gemm_grad(grouped: _Grouped, rows: int, ends, dY, W, dX, *, preact=None, dy_ld: int | None = None,
@@ -577,7 +585,7 @@ def ccl_grouped_gemm_grad(grouped: _Grouped, rows: int, ends, dY, W, dX, *, prea
     preact, z_ld = _rows("preact", preact, z_ld, rows, wide, bf16, bits)
     W = _expert_weights("W", W, E, N, K, grouped.w_ld, grouped.w_stride, bf16)
     _check(call(ctypes.byref(grouped), rows, _whole("ends", ends, E, torch.int32), dY, dy_ld, W, dX, dx_ld, preact, z_ld,
-                _ptr(workspace), workspace_bytes, _stream(stream)))
+                _room(workspace, workspace_bytes), workspace_bytes, _stream(stream)))
 
 
 def ccl_grouped_gemm_wgrad(grouped: _Grouped, rows: int, ends, dY, X, dW, *, dw_type: int | None = None,
@@ -596,7 +604,7 @@ def ccl_grouped_gemm_wgrad(grouped: _Grouped, rows: int, ends, dY, X, dW, *, dw_
     dW = _expert_weights("dW", dW, E, N, K, grouped.w_ld, grouped.w_stride,
                          torch.float32 if dw_type == CCL_DT_FP32 else bf16)
     _check(call(ctypes.byref(grouped), rows, _whole("ends", ends, E, torch.int32), dY, dy_ld, X, x_ld, dW, dw_type,
-                int(accumulate), _ptr(workspace), workspace_bytes, _stream(stream)))
+                int(accumulate), _room(workspace, workspace_bytes), workspace_bytes, _stream(stream)))
 
 
 def ccl_vocab(*, hidden: int, vocab: int, scale: float = 1.0, w_ld: int = 0, block: int = 0) -> _Vocab:
@@ -629,7 +637,7 @@ def ccl_cross_entropy(vocab: _Vocab, tokens: int, X, W, targets, loss, *, lse=No
     X, x_ld = _rows("X", X, x_ld, tokens, vocab.hidden, bf16, torch.int16)
     _check(call(ctypes.byref(vocab), tokens, X, x_ld, _vocab_weight(vocab, W, bf16),
                 _whole("targets", targets, tokens, torch.int64), _whole("loss", loss, tokens, f32),
-                _whole("lse", lse, tokens, f32), _ptr(workspace), workspace_bytes, _stream(stream)))
+                _whole("lse", lse, tokens, f32), _room(workspace, workspace_bytes), workspace_bytes, _stream(stream)))
 
 
 def ccl_cross_entropy_grad(vocab: _Vocab, tokens: int, X, W, targets, loss, dX, dW, *, lse=None, dloss=None,
@@ -651,7 +659,7 @@ def ccl_cross_entropy_grad(vocab: _Vocab, tokens: int, X, W, targets, loss, dX, 
     _check(call(ctypes.byref(vocab), tokens, X, x_ld, _vocab_weight(vocab, W, bf16),
                 _whole("targets", targets, tokens, torch.int64), _whole("dloss", dloss, tokens, f32), dloss_scale,
                 _whole("loss", loss, tokens, f32), _whole("lse", lse, tokens, f32), dX, dx_ld, dW, dw_ld, dw_type,
-                int(accumulate), _ptr(workspace), workspace_bytes, _stream(stream)))
+                int(accumulate), _room(workspace, workspace_bytes), workspace_bytes, _stream(stream)))
 
 
 CCL_ADAMW_BLOCK = 128               # elements of 8-bit moments that share a scale

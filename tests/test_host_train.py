@@ -262,3 +262,18 @@ def test_tensors_of_another_device():
     _refused(INV, ccl.ccl_adamw_step, ccl.ccl_adamw([_entry()]), lr=1e-3, step=1, grad_scale=f(1))
     b8 = lambda n: torch.zeros(n, dtype=torch.uint8)  # noqa: E731
     _refused(INV, ccl.ccl_adamw_moments, 130, b8(130), b8(2), b8(130), b8(2), f(130), f(130))
+
+
+def test_workspace_tensors(monkeypatch):
+    """A tensor smaller than the bytes it is given for, or with gaps, is refused, whatever it is on."""
+    monkeypatch.setattr(ccl, "_here", lambda **tensors: None)
+    v = ccl.ccl_vocab(**VOCAB)
+    need = ccl.ccl_cross_entropy_workspace(v, 10, grad=True)
+    bytes_ = lambda n: torch.zeros(n, dtype=torch.uint8)  # noqa: E731
+    for ws in (bytes_(need - 1), bytes_(2 * need)[::2]):
+        for call in (lambda: ccl.ccl_cross_entropy(v, 10, P, P, P, P, workspace=ws, workspace_bytes=need),  # noqa: B023
+                     lambda: ccl.ccl_cross_entropy_grad(v, 10, P, P, P, P, P, P, workspace=ws, workspace_bytes=need),  # noqa: B023
+                     lambda: ccl.ccl_grouped_gemm(ccl.ccl_grouped(**GROUPED), 10, P, P, P, P, workspace=ws,  # noqa: B023
+                                                  workspace_bytes=need)):
+            with pytest.raises(ccl.CCLError, match="contiguous bytes"):
+                call()
