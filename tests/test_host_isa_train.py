@@ -49,7 +49,7 @@ KINDS = {
     ("grouped_rows_kernel", "256ELi256"): (4, {4}), ("grouped_wgrad_kernel", "128ELi128"): (3, {2}),
     ("grouped_wgrad_kernel", "256ELi256"): (3, {4}), ("logits_kernel", "64ELi128"): (1, {1, 2}),
     ("logits_kernel", "128ELi128"): (2, {2}), ("logits_kernel", "256ELi256"): (2, {4}), ("plain_kernel", "64ELi128"): (2, {1, 2}),
-    ("plain_kernel", "128ELi128"): (4, {2}), ("plain_kernel", "256ELi256"): (3, {4}),
+    ("plain_kernel", "128ELi128"): (4, {2}), ("plain_kernel", "256ELi256"): (4, {4}),
 }
 
 
