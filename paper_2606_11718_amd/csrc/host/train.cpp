@@ -28,8 +28,9 @@ int64_t resident(int64_t tiles, int per_cu) { return std::min<int64_t>(up(std::m
 //            218 / 278
 //   grad     32768 over 128 of 768 -> 2048 through SwiGLU 258 / 213 (three tiles a CU,
 //            uneven), 65536 372 / 369, 8192 over one of 4096 -> 4096 235 / 288
-//   wgrad    32768 over 128 of 2048 -> 1536 387 / 451, 8192 over one 223 / 288, 65536
-//            over 4 of 256 -> 256 334 / 181 (4 tiles an expert)
+//   wgrad    32768 over 128 of 2048 -> 1536 376 / 470, 4096 172 / 230, 128 160 / 195,
+//            8192 over one 223 / 288, 65536 over 4 of 256 -> 256 334 / 181 (4 tiles an
+//            expert)
 // 64x128 ones, with a third stage on its way, where few rows come to an expert (against
 // 128x128): 64 rows 58 / 71 (forward as above), 1024 165 / 187, 8192 199 / 230, 12000
 // 220 / 223, its grad 133 / 126.
