@@ -67,6 +67,7 @@ __device__ __forceinline__ int32_t make_table(const GroupedParams& p, ExpertTabl
     for (int i = 0; i < kGroupedMaxExperts / 64; ++i)
       end[i] = 64 * i + tid < p.experts ? min(max(p.ends[64 * i + tid], 0), p.rows) : 0;
     int32_t past = 0, before = 0;       // of the experts so far
+    int32_t mine = 0;                   // the rows of expert tid
 #pragma unroll
     for (int i = 0; i < kGroupedMaxExperts / 64; ++i) {
       if (64 * i >= p.experts) break;
@@ -76,14 +77,19 @@ __device__ __forceinline__ int32_t make_table(const GroupedParams& p, ExpertTabl
       const int32_t sum = before + wave_scan(tiles, tid, [](int32_t a, int32_t b) { return a + b; });
       t.first[64 * i + tid] = first;
       t.rows[64 * i + tid] = to - first;
+      if (i == 0) mine = to - first;
       t.before[64 * i + tid] = sum - tiles;
       past = __shfl(to, 63);
       before = __shfl(sum, 63);
     }
     if (tid == 0) t.total = before;
     if (p.experts <= 64) {
+      // from lane to lane: no lane reads what another one has written to the table before the barrier
       int32_t rank = 0;
-      for (int e = 0; e < p.experts; ++e) rank += t.rows[e] > t.rows[tid] || (t.rows[e] == t.rows[tid] && e < tid);
+      for (int e = 0; e < p.experts; ++e) {
+        const int32_t other = __builtin_amdgcn_readlane(mine, e);
+        rank += other > mine || (other == mine && e < tid);
+      }
       if (tid < p.experts) t.order[rank] = tid;
     }
   }

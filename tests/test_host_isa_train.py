@@ -80,3 +80,14 @@ def test_scratch(kernels):
 def test_no_packed_fp32(kernels):
     for name, (body, _) in kernels.items():
         assert not [ln for ln in body if re.match(r"v_pk_(add|mul|fma)_f32", ln)], name
+
+
+def test_the_experts_table_is_read_behind_its_barrier(kernels):
+    """Its lanes write it to LDS and what they need of one another's comes by lane: nothing is read from LDS ahead of
+    the first barrier."""
+    found = [(n, body) for n, (body, _) in kernels.items() if "grouped_rows_kernel" in n or "grouped_wgrad_kernel" in n]
+    assert len(found) == 18
+    for name, body in found:
+        barrier = next(i for i, ln in enumerate(body) if ln.startswith("s_barrier"))
+        assert any(ln.startswith("ds_write") for ln in body[:barrier]), name
+        assert not [ln for ln in body[:barrier] if ln.startswith("ds_read")], name
