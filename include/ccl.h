@@ -608,7 +608,9 @@ ccl_status ccl_cross_entropy_grad(const ccl_vocab* vocab, int64_t tokens, const 
  * 8 or 15). They are rounded up or down at random, by a hash of the element's
  * place in its tensor and of the step: the same call gives the same bits. A
  * moment that is infinite or NaN is held as NaN, its neighbours are not touched.
- * Zero bytes are moments of 0.
+ * Zero bytes are moments of 0; but a 0 of exp_avg_sq beside an exp_avg that is not 0
+ * is read as the format's smallest value, code 1 (its m is there by such a
+ * rounding, and would be divided by eps alone).
  */
 typedef struct ccl_adamw {
   double lr, beta1, beta2, eps;
@@ -636,7 +638,7 @@ typedef struct ccl_adamw_tensor {
  * The step, of `count` tensors (an array on the host, read before the call
  * returns), and the values that 8-bit moments stand for (m, v: n elements of
  * fp32 or bf16, which holds them exactly while they are normal; either may be
- * NULL). Buffers may start at any element; whole 16 bytes (8 for 8-bit moments)
+ * NULL, and so may its codes; without exp_avg a 0 of exp_avg_sq is 0). Buffers may start at any element; whole 16 bytes (8 for 8-bit moments)
  * are faster. One launch for every 68 tensors of a kind (54 with 8-bit moments),
  * no workspace.
  * Errors: CCL_ERR_INVALID_ARG (NULL argument, a count outside 0 .. 2^20, an n

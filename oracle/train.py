@@ -110,6 +110,11 @@ def moment_decode(codes, scales, exponent_bits):
     return moment_values(exponent_bits)[codes] * np.repeat(factor, BLOCK)[:len(codes)]
 
 
+def v_taken(m_codes, v_codes):
+    """v's codes as they are read beside m's: no 0 under an m that is not."""
+    return np.where((v_codes == 0) & ((m_codes & 0x7F) != 0), 1, v_codes).astype(np.uint8)
+
+
 def chances(n, step):
     """32 bits an element, of its place and the step."""
     i = np.arange(n, dtype=np.uint64)

@@ -728,7 +728,8 @@ def ccl_adamw_step(tensors: AdamwSet, *, lr: float, step: int = 0, beta1: float 
 
 
 def ccl_adamw_moments(n: int, exp_avg, exp_avg_scale, exp_avg_sq, exp_avg_sq_scale, m, v, *, stream=None) -> None:
-    """The values of n 8-bit moments, to m and v (fp32 or bf16 tensors of one type; either may be None)."""
+    """The values of n 8-bit moments, to m and v (fp32 or bf16 tensors of one type; either may be None). With exp_avg, v
+    is what a step reads: not 0 where exp_avg is not."""
     call = library().ccl_adamw_moments
     import torch
     u8, blocks = torch.uint8, -(-n // CCL_ADAMW_BLOCK)

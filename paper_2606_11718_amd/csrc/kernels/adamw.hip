@@ -10,11 +10,15 @@
 //
 // 8-bit moments: 128 elements share a power of two, from the largest exponent
 // among them. m is a sign, 4 exponent and 3 mantissa bits; v, never negative, 5
-// and 3: 34 octaves, so that a small v beside a large one does not become 0
-// under an m that has not. Rounded up or down at random (a hash of the element's
+// and 3: its smallest value has the square root of m's smallest, both 2^-16 of the
+// largest's power of two. Rounded up or down at random (a hash of the element's
 // place and the step, so the same call gives the same bits): b2 = 0.999 moves v
 // by a thousandth of itself a step, which rounding to the nearest of 3 mantissa
-// bits would undo every time.
+// bits would undo every time. Below its smallest value an m is then rounded up with
+// the chance of its ratio to it, its v with that of the ratio's square, so that
+// many live beside a v of 0: there v is taken as its smallest value when it is
+// read, or m would be divided by eps alone (gradients of 1e-5 beside one of 1 in a
+// block: steps of up to 700 learning rates, with that value 1.6, in fp32 1.0).
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -193,6 +197,13 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int n, bool whole, uint2
 
 __device__ __forceinline__ uint32_t code_of(uint2 c, int j) { return ((j < 4 ? c.x : c.y) >> (8 * (j & 3))) & 255; }
 
+// v's codes with 1, the smallest value, in place of 0 where m's code is not a 0.
+__device__ __forceinline__ uint32_t taken_v(uint32_t v, uint32_t m) {
+  const uint32_t live = (m & 0x7f7f7f7fu) + 0x7f7f7f7fu, some = ((v & 0x7f7f7f7fu) + 0x7f7f7f7fu) | v;
+  return v | ((live & ~some & 0x80808080u) >> 7);
+}
+__device__ __forceinline__ uint2 taken_v(uint2 v, uint2 m) { return make_uint2(taken_v(v.x, m.x), taken_v(v.y, m.y)); }
+
 // The largest of a block's 16 threads.
 __device__ __forceinline__ int block_top(const float (&x)[8]) {
   int top = 0;
@@ -257,8 +268,10 @@ __global__ void __launch_bounds__(256) adamw_kernel(AdamwTable<BITS8> table, Ada
     load8<G16>(t.grad, at, left, whole, g);
     if constexpr (BITS8) {
       const int64_t block = at / kAdamwBlock;
-      decode8<4>(load_codes(static_cast<const uint8_t*>(t.m) + at, left, whole), Moment<4>::scale(t.m_scale[block]), m);
-      decode8<5>(load_codes(static_cast<const uint8_t*>(t.v) + at, left, whole), Moment<5>::scale(t.v_scale[block]), v);
+      const uint2 mc = load_codes(static_cast<const uint8_t*>(t.m) + at, left, whole);
+      const uint2 vc = load_codes(static_cast<const uint8_t*>(t.v) + at, left, whole);
+      decode8<4>(mc, Moment<4>::scale(t.m_scale[block]), m);
+      decode8<5>(taken_v(vc, mc), Moment<5>::scale(t.v_scale[block]), v);
     } else {
       load8<false>(t.m, at, left, whole, m);
       load8<false>(t.v, at, left, whole, v);
@@ -302,12 +315,14 @@ __global__ void __launch_bounds__(256) moments_kernel(int64_t n, const uint8_t* 
   if (at >= n) return;
   const int left = (int)(n - at < 8 ? n - at : 8);
   float x[8];
+  const uint2 mc = m ? load_codes(m + at, left, left == 8 && aligned_to(m, 8)) : make_uint2(0, 0);
   if (m_out) {
-    decode8<4>(load_codes(m + at, left, left == 8 && aligned_to(m, 8)), Moment<4>::scale(m_scale[at / kAdamwBlock]), x);
+    decode8<4>(mc, Moment<4>::scale(m_scale[at / kAdamwBlock]), x);
     store8<BF16>(m_out, at, left, left == 8 && aligned_to(m_out, 16), x);
   }
   if (v_out) {
-    decode8<5>(load_codes(v + at, left, left == 8 && aligned_to(v, 8)), Moment<5>::scale(v_scale[at / kAdamwBlock]), x);
+    const uint2 vc = load_codes(v + at, left, left == 8 && aligned_to(v, 8));
+    decode8<5>(taken_v(vc, mc), Moment<5>::scale(v_scale[at / kAdamwBlock]), x);
     store8<BF16>(v_out, at, left, left == 8 && aligned_to(v_out, 16), x);
   }
 }

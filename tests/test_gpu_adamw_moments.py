@@ -1,0 +1,76 @@
+"""8-bit moments of gradients that differ by many powers of two within a block of 128,
+and what a step reads where v's code is 0 under an m that is not.
+
+The smallest m is 2^-16 of the power of two M below the block's largest, the smallest
+v 2^-32 of V: an element at both moves by M / sqrt V, at most sqrt 2 times the largest
+m over the largest v's root. Of exact moments |m^| / sqrt v^ is at most
+(1 - b1) / sqrt((1 - b2) (1 - b1^2 / b2)) = 7.3 (Cauchy and Schwarz), with both
+rounded against it (m an eighth up, v an eighth down) 7.3 sqrt 2 1.125 / sqrt 0.875 =
+12.4; 16 is asked for. (In fp32 no step of these gradients is above 1.01.)
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import train as OT
+from paper_2606_11718_amd import ccl
+from tests.test_gpu_adamw import HYPER, Tensor
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("largest", [1.0, 1e-2])
+@pytest.mark.parametrize("ratio", [1e-4, 2e-5, 1e-5, 1e-6, 1e-7])
+def test_steps_beside_a_large_gradient(ratio, largest):
+    """300 steps of blocks in which one element's gradients are the others' / ratio."""
+    n, lr = 1024, 1e-3
+    rng = np.random.default_rng(21)
+    size = np.full(n, largest * ratio)
+    size[::128] = largest
+    size = torch.from_numpy(size).cuda()
+    t = Tensor(rng, n, bits=8, zero_moments=True)
+    t.p.zero_()
+    s = ccl.ccl_adamw([t.entry()])
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    worst = torch.zeros((), device="cuda")
+    for step in range(1, 301):
+        t.g.copy_(torch.randn(n, device="cuda", generator=gen) * size)
+        before = t.p.clone()
+        ccl.ccl_adamw_step(s, step=step, lr=lr, beta1=0.9, beta2=0.999, eps=1e-8)
+        worst = torch.maximum(worst, (t.p - before).abs().max())
+    assert float(worst) <= 16 * lr, float(worst) / lr
+
+
+def _beside(t):
+    """Every third v of 0, its m of its smallest value or larger, of both signs; some of both 0."""
+    at = np.arange(t.n)
+    t.vc[at % 3 == 0] = 0
+    t.mc[at % 3 == 0] = np.array([1, 129, 40, 0, 128])[at[at % 3 == 0] % 5]
+    t.m.copy_(torch.from_numpy(t.mc))
+    t.v.copy_(torch.from_numpy(t.vc))
+    taken = OT.v_taken(t.mc, t.vc)
+    assert (taken != t.vc).sum() > t.n // 8 and (taken == 0).any()
+    t.m0, t.v0 = OT.moment_decode(t.mc, t.ms, 4), OT.moment_decode(taken, t.vs, 5)
+
+
+@pytest.mark.parametrize("offset", [0, 3])
+def test_a_step_from_v_of_0(offset):
+    t = Tensor(np.random.default_rng(22), 1000, bits=8, offset=offset, decay=0.1)
+    _beside(t)
+    t.g.mul_(2.0 ** -20)     # the smallest v counts beside what the gradient adds
+    t.g0 = t.g0 * np.float32(2.0 ** -20)
+    ccl.ccl_adamw_step(ccl.ccl_adamw([t.entry()]), step=5, **HYPER)
+    t.check(5)
+
+
+@pytest.mark.parametrize("offset", [0, 3])
+def test_values_beside_m(offset):
+    t = Tensor(np.random.default_rng(23), 1000, bits=8, offset=offset)
+    _beside(t)
+    m, v, alone = (torch.empty(t.n, device="cuda") for _ in range(3))
+    ccl.ccl_adamw_moments(t.n, t.m, t.msc, t.v, t.vsc, m, v)
+    assert np.array_equal(m.cpu().numpy(), t.m0.astype(np.float32)) and np.array_equal(v.cpu().numpy(), t.v0.astype(np.float32))
+    ccl.ccl_adamw_moments(t.n, t.m, t.msc, t.v, t.vsc, None, v.zero_())
+    assert np.array_equal(v.cpu().numpy(), t.v0.astype(np.float32))
+    ccl.ccl_adamw_moments(t.n, None, None, t.v, t.vsc, None, alone)
+    assert np.array_equal(alone.cpu().numpy(), OT.moment_decode(t.vc, t.vs, 5).astype(np.float32))

@@ -68,3 +68,11 @@ def test_random_rounding_is_fair(bits):
     step = 2.0 ** -2 / 8
     assert set(np.unique(body)) == {0.28125, 0.3125}
     assert abs(body.mean() - 0.3) < 2 * step / np.sqrt(len(body))
+
+
+def test_v_taken():
+    """Only a v of 0 under a live m is another code, its smallest."""
+    m, v = np.meshgrid(np.arange(256, dtype=np.uint8), np.arange(256, dtype=np.uint8))
+    got = OT.v_taken(m.ravel(), v.ravel()).reshape(m.shape)
+    live = (m != 0) & (m != 128)
+    assert (got[(v == 0) & live] == 1).all() and np.array_equal(got[(v > 0) | ~live], v[(v > 0) | ~live])
