@@ -545,8 +545,10 @@ ccl_status ccl_grouped_gemm_wgrad(const ccl_grouped* grouped, int64_t rows, cons
  * A target outside 0 .. vocab - 1 (-100, say) marks a token that does not
  * count: its loss is 0, its dX is 0 and it adds nothing to dW, whatever its x
  * holds; lse is its own. A weight g of 0 is taken so too (the loss is not). A
- * logit of -inf is a term of 0; one that is NaN or +inf makes its token's loss, lse
- * and dX NaN, and with that dW.
+ * logit of -inf is a term of 0 in the loss and its P_v is 0; one that is NaN or +inf
+ * makes its token's loss, lse and dX NaN, and with that dW. dX sums over finite W: a
+ * w_v that is infinite or NaN in a column makes that column of dX NaN for every token
+ * (0 * w_v), those that do not count included.
  * The logits are never in memory: a block of `block` tokens at a time, tiles of
  * them are reduced to fp32 maxima and sums, and where a gradient is asked for
  * exp(z - tile maximum) is kept in bf16 for the block, 2 bytes a logit.
