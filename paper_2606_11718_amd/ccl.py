@@ -665,12 +665,17 @@ def ccl_cross_entropy_grad(vocab: _Vocab, tokens: int, X, W, targets, loss, dX, 
 CCL_ADAMW_BLOCK = 128               # elements of 8-bit moments that share a scale
 
 
+def _adamw_types() -> dict:
+    import torch
+    return {torch.float32: CCL_DT_FP32, torch.bfloat16: CCL_DT_BF16}
+
+
 def ccl_adamw_tensor(param, grad, exp_avg, exp_avg_sq, *, exp_avg_scale=None, exp_avg_sq_scale=None, copy=None,
                      weight_decay: float = 0.0) -> tuple[_AdamwTensor, tuple]:
     """One tensor of a ccl_adamw set: contiguous tensors of as many elements; uint8 moments (with their scales, one byte
-    for every 128) are 8-bit ones. The set keeps the tensors alive."""
+    for every 128) are 8-bit ones. The set keeps the tensors alive and steps with these, whatever param.grad becomes."""
     import torch
-    types = {torch.float32: CCL_DT_FP32, torch.bfloat16: CCL_DT_BF16}
+    types = _adamw_types()
     n = param.numel()
     at = param.get_device()
     for name, t in (("grad", grad), ("exp_avg", exp_avg), ("exp_avg_sq", exp_avg_sq), ("exp_avg_scale", exp_avg_scale),
@@ -697,7 +702,8 @@ def ccl_adamw_tensor(param, grad, exp_avg, exp_avg_sq, *, exp_avg_scale=None, ex
 
 
 class AdamwSet:
-    """Tensors for ccl_adamw_step, held while it lives."""
+    """Tensors for ccl_adamw_step, held while it lives. A step reads them where they lay when they were given: gradients
+    that have other storage since (as behind torch's zero_grad(), which drops them) are given anew with grads()."""
 
     def __init__(self, tensors):
         tensors = list(tensors)
@@ -705,9 +711,27 @@ class AdamwSet:
         self.tensors = (_AdamwTensor * len(tensors))(*(t for t, _ in tensors))
         self.kept = [held for _, held in tensors]
 
+    def grads(self, grads) -> "AdamwSet":
+        """Other gradients for the tensors, one each in their order, for the steps from here on (a captured step keeps
+        those it was captured with)."""
+        grads, new, types = list(grads), [], _adamw_types()
+        if len(grads) != len(self.tensors):
+            _refuse("grads", f"{len(grads)} gradients for {len(self.tensors)} tensors")
+        for t, held, g in zip(self.tensors, self.kept, grads):
+            if g is None or g.dtype not in types or g.numel() != t.n:
+                _refuse("grads", f"not {t.n} elements of fp32 or bf16")
+            if held and g.device != held[0].device:
+                _refuse("grads", f"a tensor on {g.device}, the param on {held[0].device}")
+            new.append(_whole("grads", g, t.n, g.dtype))
+        for i, (t, g, address) in enumerate(zip(self.tensors, grads, new)):
+            t.grad, t.grad_type = address, types[g.dtype]
+            held = self.kept[i]
+            self.kept[i] = (*held[:1], g, *held[2:])
+        return self
+
 
 def ccl_adamw(tensors) -> AdamwSet:
-    """A set of ccl_adamw_tensor to step together."""
+    """A set of ccl_adamw_tensor to step together; set.grads(...) replaces its gradients."""
     return AdamwSet(tensors)
 
 
