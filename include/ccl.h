@@ -506,7 +506,8 @@ typedef enum ccl_grouped_direction {
  * apart. preact takes Z (bf16) in the forward call, or is NULL; the grad call
  * reads it, and it is not needed (NULL) with CCL_ACT_NONE and gated = 0. Z has
  * out_features columns forward; in the grad call it and dX have in_features,
- * or gated twice as many. dX may be preact itself; nothing else may overlap.
+ * or gated twice as many. dX may be preact itself, with the same leading
+ * dimension; nothing else may overlap.
  * dW is bf16 or fp32, (experts, out_features, in_features); accumulate = 1 adds
  * to it. Matrices and the workspace are 16-byte aligned, leading dimensions
  * multiples of 8, at most 2^21; the workspace (NULL where none is needed) is
@@ -515,10 +516,10 @@ typedef enum ccl_grouped_direction {
  * Errors: CCL_ERR_INVALID_ARG (NULL argument, sizes outside the ranges above or
  * rows outside 0..2^30, an unknown activation, direction or type, gated or
  * accumulate not 0 or 1, a leading dimension or stride smaller than what it
- * spans, workspace missing or too small); CCL_ERR_UNSUPPORTED (a side not a
- * multiple of 16 or above 2^20, a gated expert's weight of 2^29 elements and
- * more, a launch too large; device not gfx950); CCL_ERR_MISALIGNED_POINTER;
- * CCL_ERR_HIP.
+ * spans, dX in place of preact with another one, workspace missing or too
+ * small); CCL_ERR_UNSUPPORTED (a side not a multiple of 16 or above 2^20, a gated
+ * expert's weight of 2^29 elements and more, a launch too large; device not
+ * gfx950); CCL_ERR_MISALIGNED_POINTER; CCL_ERR_HIP.
  */
 ccl_status ccl_grouped_gemm_workspace(const ccl_grouped* grouped, int64_t rows,
                                       ccl_grouped_direction direction, int64_t* workspace_bytes);

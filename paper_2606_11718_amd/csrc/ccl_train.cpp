@@ -192,6 +192,8 @@ ccl_status ccl_grouped_gemm_grad(const ccl_grouped* grouped, int64_t rows, const
   if (ccl_status st = check_matrix("dX", dX, dx_ld, wide, 8)) return st;
   if (through)
     if (ccl_status st = check_matrix("preact", preact, z_ld, wide, 8)) return st;
+  if (through && dX == preact && rows > 1 && dx_ld != z_ld)
+    return fail(CCL_ERR_INVALID_ARG, "dX in place of preact has its leading dimension");
   if (ccl_status st = check_workspace(ccl::grouped_form(s, rows, CCL_GROUPED_GRAD).workspace_bytes, workspace, workspace_bytes))
     return st;
   if (ccl_status st = check_device()) return st;

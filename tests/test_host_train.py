@@ -95,6 +95,14 @@ def test_grouped_grad_needs_what_it_goes_through():
     _refused(INV, ccl.ccl_grouped_gemm_grad, gated, 10, P, P, P, P, preact=P, dx_ld=64)
 
 
+def test_grouped_grad_in_place():
+    """dX is preact: its rows lie where preact's do."""
+    for how, wide in ((dict(activation=ccl.CCL_ACT_SILU), 64), (dict(gated=True), 128)):
+        g = ccl.ccl_grouped(**GROUPED, **how)
+        with pytest.raises(ccl.CCLError, match="in place of preact"):
+            ccl.ccl_grouped_gemm_grad(g, 10, 2 * P, 3 * P, 4 * P, P, preact=P, dx_ld=wide, z_ld=wide + 8)
+
+
 def test_grouped_tensors():
     g = ccl.ccl_grouped(**GROUPED)
     bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
