@@ -91,3 +91,22 @@ def test_the_experts_table_is_read_behind_its_barrier(kernels):
         barrier = next(i for i, ln in enumerate(body) if ln.startswith("s_barrier"))
         assert any(ln.startswith("ds_write") for ln in body[:barrier]), name
         assert not [ln for ln in body[:barrier] if ln.startswith("ds_read")], name
+
+
+def test_counted_stores(kernels):
+    """Kernels whose first barrier behind a tile lets that many memory accesses be on their way (all that came before
+    them, loads among them, is then there): a wave's end of a tile makes at least these, 16-byte stores one after
+    another, with no branch among them and under no lane mask, and the wait has their number."""
+    found = [(n, body) for n, (body, _) in kernels.items() if re.search(r"grouped_wgrad_kernel.*WgradOutE0E|plain_kernel.*EELb0EEE", n)]
+    assert len(found) == 7, [n for n, _ in found]
+    for name, body in found:
+        bm, bn, waves, across = (int(re.search(r"ProductTileILi(\d+)ELi(\d+)ELb\dELb\dELi\dELi(\d)ELi(\d)", name).group(i)) for i in (1, 2, 3, 4))
+        count = (bm * across // (16 * waves)) * (bn // (16 * across)) // 2
+        stores = [i for i, ln in enumerate(body) if ln.startswith("buffer_store_dwordx4")]
+        assert len(stores) == count, (name, len(stores), count)
+        last_product = max(i for i, ln in enumerate(body[:stores[0]]) if ln.startswith("v_mfma"))
+        assert not [ln for ln in body[last_product:stores[-1]] if re.match(r"\S+\s+exec|\S*saveexec|v_cmpx", ln)], name
+        assert not [ln for ln in body[stores[0]:stores[-1]] if re.match(r"s_c?branch|s_setpc|s_barrier|\.LBB", ln)], name
+        waits = [i for i, ln in enumerate(body) if re.match(rf"s_waitcnt vmcnt\({count}\) lgkmcnt\(0\)", ln)]
+        behind = [next(ln for ln in body[i + 1:] if not ln.startswith(";")) for i in waits]
+        assert [ln for ln in behind if ln.startswith(("s_barrier", "s_branch"))], (name, behind)
