@@ -552,10 +552,10 @@ ccl_status ccl_grouped_gemm_wgrad(const ccl_grouped* grouped, int64_t rows, cons
  * (0 * w_v), those that do not count included.
  * The logits are never in memory: a block of `block` tokens at a time, tiles of
  * them are reduced to fp32 maxima and sums, and where a gradient is asked for
- * exp(z - tile maximum) is kept in bf16 for the block, 2 bytes a logit.
- * loss and lse are fp32 of fp32 logits; P is rounded to bf16 twice on its way
- * into the gradients' products (2^-8 relative each at most; the target's P
- * once), whose sums are fp32 in a fixed order.
+ * exp(z - tile maximum) is kept for the block in 16 bits, 10 of them significant.
+ * loss and lse are fp32 of fp32 logits; P is rounded to 10 bits (2^-10 relative at
+ * most; not the target's P) and to bf16 (2^-8) on its way into the gradients'
+ * products, whose sums are fp32 in a fixed order.
  */
 typedef struct ccl_vocab {
   int64_t hidden, vocab;        /* hidden: a multiple of 16 up to 2^20; vocab up to 2^20 */

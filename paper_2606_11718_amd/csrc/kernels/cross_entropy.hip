@@ -5,7 +5,7 @@
 // for a block of tokens at a time:
 //   logits   tiles of X W^T that stay in registers: each leaves the maximum m
 //            and sum of exp(z - m) of every row (fp32), the target's z, and for
-//            the gradient e = exp(z - m) in bf16
+//            the gradient e = exp(z - m) in 16 bits
 //   combine  rows' lse and loss from the tiles' m and sums, in a fixed order
 //   scale    e -> P', in place: e exp(m - lse) g scale; the target's p - 1 is
 //            expm1(z_t - lse) of the fp32 z_t, since from a rounded p it would
@@ -13,7 +13,8 @@
 //   dX, dW   products of P' with W and X
 // Logits in fp32 exist nowhere in memory; P' is kept for a block, 2 bytes each,
 // so that neither gradient has to recompute them (6 T D V operations rather
-// than 8). Rounded to bf16: e, P' (2^-8 each at most), dX and dW once.
+// than 8). Rounded: e to 10 significant bits (2^-10 at most), P' to the products' bf16
+// (2^-8; the target's from fp32), dX and dW once.
 //
 // Bound by the matrix cores where there are many tokens: the loss of 4096 tokens, 8192 x
 // 32768, 1.60 ms (1.38 PFLOP/s); with both gradients 8192 of 2048 x 131072 11.4 ms: 4.0
@@ -28,6 +29,19 @@
 namespace ccl {
 
 namespace {
+
+// e = exp(z - tile maximum) in 16 bits: it is never negative and never above 1, so that
+// its fp32's sign and first exponent bit are 0 and 9 bits of mantissa are left beside
+// all other exponents (half a step: 2^-10, a quarter of bf16's; sums of P' of tokens that
+// are no target are 1.7e-3 from fp32's where bf16 made it 2.2e-3, for 0.1 to 0.5 % more
+// time of loss and gradients). Rounded to nearest, two a word. A NaN need not be held:
+// its token's lse is NaN.
+__device__ __forceinline__ uint32_t held2(float a, float b) {
+  const uint32_t x = (__float_as_uint(a) << 2) + 0x8000u, y = (__float_as_uint(b) << 2) + 0x8000u;
+  return __builtin_amdgcn_perm(y, x, 0x07060302u);
+}
+__device__ __forceinline__ float held_low(uint32_t w) { return __uint_as_float((w & 0xffffu) << 14); }
+__device__ __forceinline__ float held_high(uint32_t w) { return __uint_as_float((w >> 16) << 14); }
 
 struct LogitsParams {
   const uint16_t *X, *W;
@@ -121,7 +135,7 @@ __global__ void __launch_bounds__(T::THREADS, waves_per_simd<T>()) logits_kernel
               acc[mt][nt][j] = __builtin_amdgcn_exp2f((acc[mt][nt][j] - top[mt]) * kLog2e);
               sum[mt] += acc[mt][nt][j];
             }
-            e[nt] = f32_to_bf16x4(acc[mt][nt]);
+            e[nt] = make_uint2(held2(acc[mt][nt][0], acc[mt][nt][1]), held2(acc[mt][nt][2], acc[mt][nt][3]));
           }
           if (p.E) {
             // columns past the vocabulary up to e_cols: exp(-inf) = 0
@@ -226,7 +240,10 @@ __global__ void __launch_bounds__(256) scale_kernel(ScaleParams p) {
   const uint4 e = *at;
   const int32_t tile = col < p.large ? col >> 8 : ((p.large + 255) >> 8) + ((col - p.large) >> 7);
   const float k = __builtin_amdgcn_exp2f((p.stat[(int64_t)row * p.tiles_n + tile].x - f.x) * kLog2e) * f.y;
-  f32x4 lo = bf16x4_to_f32(make_uint2(e.x, e.y)) * k, hi = bf16x4_to_f32(make_uint2(e.z, e.w)) * k;
+  f32x4 lo{held_low(e.x), held_high(e.x), held_low(e.y), held_high(e.y)};
+  f32x4 hi{held_low(e.z), held_high(e.z), held_low(e.w), held_high(e.w)};
+  lo *= k;
+  hi *= k;
   const int64_t t = p.targets[row] - col;
   if (t >= 0 && t < 8) {
     const float v = expm1f(p.target_z[row] - f.x) * f.y;
