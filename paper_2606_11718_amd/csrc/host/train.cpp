@@ -31,6 +31,9 @@ int64_t resident(int64_t tiles, int per_cu) { return std::min<int64_t>(up(std::m
 //   wgrad    32768 over 128 of 2048 -> 1536 376 / 470, 4096 172 / 230, 128 160 / 195,
 //            8192 over one 223 / 288, 65536 over 4 of 256 -> 256 334 / 181 (4 tiles an
 //            expert)
+// All of these sides are multiples of 256, and the rule has no term for padding: a dW
+// of 128 experts of 288 x 288 is taken in 256x256 tiles, which compute 512 x 512 of it
+// (128x128 ones 384 x 384).
 // 64x128 ones, with a third stage on its way, where few rows come to an expert (against
 // 128x128): 64 rows 58 / 71 (forward as above), 1024 165 / 187, 8192 199 / 230, 12000
 // 220 / 223, its grad 133 / 126.

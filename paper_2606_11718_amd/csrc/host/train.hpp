@@ -7,7 +7,7 @@
 namespace ccl {
 
 // ---- experts' products on rows sorted by expert ----
-constexpr int kGroupedMaxExperts = 512;       // one thread each finds a workgroup's tile
+constexpr int kGroupedMaxExperts = 512;       // eight a lane of the wave that makes a workgroup's table
 enum GroupedDirection { GROUPED_FORWARD = 0, GROUPED_GRAD = 1, GROUPED_WGRAD = 2 };
 struct GroupedShape {
   int64_t in = 0, out = 0;                    // K, N: an expert's weight is N x K
@@ -49,9 +49,9 @@ struct VocabForm {
   // bytes into the workspace
   int64_t target_at = 0, factor_at = 0, stat_at = 0, e_at = 0, rows_at = 0, part_at = 0, sum_at = 0, workspace_bytes = 0;
 };
-// The blocks and the workspace, which fewer tokens do not exceed; grad: with exp(z - tile max) kept for a block,
-// a copy of its x,
-// the ranges' partial dX and, where dW is rounded after several blocks, its fp32 sum.
+// The blocks and the workspace, which fewer tokens do not exceed; grad: with
+// exp(z - tile max) kept for a block, a copy of its x, the ranges' partial dX and,
+// where dW is rounded after several blocks, its fp32 sum.
 VocabForm vocab_form(const VocabShape& s, int64_t tokens, bool grad);
 // The products of a block of `tokens`: logits and dW, each in 256x256 tiles over the
 // first vocab_..._large columns of the vocabulary (whole tiles, or all, or 0) and in
@@ -68,8 +68,7 @@ ProductForm vocab_dx_form(const VocabShape& s, int64_t tokens, bool large);
 constexpr int kAdamwTensors[2] = {68, 54};    // of a launch (moments of 32, 8 bits): their table is a kernel argument
 constexpr int kAdamwBlock = 128;              // elements of 8-bit moments that share a scale
 
-// 1 - beta^step and its like, the same bits on the host and the device: by
-// squaring, in double.
+// beta^step, the same bits on the host and the device: by squaring, in double.
 #if defined(__HIPCC__)
 __host__ __device__
 #endif

@@ -173,7 +173,7 @@ struct CombineParams {
   const uint16_t* X;       // rows copied to `rows`, zeros where the factor is 0 (null: not needed)
   uint16_t* rows;
   int64_t x_ld;
-  int32_t tokens, vocab, tiles_n, hidden;
+  int32_t vocab, tiles_n, hidden;
   float scale, dloss_scale;
 };
 
@@ -223,7 +223,7 @@ struct ScaleParams {
   const float* target_z;
   const int64_t* targets;
   int64_t e_ld;
-  int32_t vocab, e_cols, tiles_n;
+  int32_t e_cols, tiles_n;
   int32_t large;           // columns in tiles of 256, the others' are 128 wide
 };
 
@@ -264,7 +264,7 @@ struct PlainParams {
   void* out;               // bf16, or fp32 with f32
   const float* add;        // m x n without gaps, or null
   float* part;             // [splits][m][n], or null
-  int32_t m, n, ku, kv, ksteps;
+  int32_t m, n, ku, kv;
   int32_t mu, nv;          // columns that U and V have (RC sides, whole 16 bytes)
   int32_t tiles_m, tiles_n, group, chunk, splits, ksplit;
   int32_t f32, accumulate;
@@ -464,7 +464,6 @@ hipError_t launch_cross_entropy(const VocabShape& s, const VocabCall& c, void* w
     cp.loss = c.loss ? c.loss + first : nullptr;
     cp.lse = c.lse ? c.lse + first : nullptr;
     cp.factor = c.grad ? factor : nullptr;
-    cp.tokens = (int32_t)n;
     cp.vocab = (int32_t)s.vocab;
     cp.tiles_n = tiles_n;
     cp.scale = s.scale;
@@ -483,7 +482,6 @@ hipError_t launch_cross_entropy(const VocabShape& s, const VocabCall& c, void* w
     sp.target_z = target_z;
     sp.targets = c.targets + first;
     sp.e_ld = f.e_ld;
-    sp.vocab = (int32_t)s.vocab;
     sp.e_cols = f.e_cols;
     sp.tiles_n = tiles_n;
     sp.large = large < s.vocab ? (int32_t)large : f.e_cols;
@@ -497,7 +495,6 @@ hipError_t launch_cross_entropy(const VocabShape& s, const VocabCall& c, void* w
       p.n = p.nv = (int32_t)s.hidden;
       p.ku = f.e_cols;
       p.kv = (int32_t)s.vocab;
-      p.ksteps = f.e_cols / 64;
       p.ld_out = c.dx_ld;
       const int64_t whole = vocab_dx_large(s, n);
       const auto rows_of = [&](int64_t from, int64_t to) {
@@ -526,7 +523,6 @@ hipError_t launch_cross_entropy(const VocabShape& s, const VocabCall& c, void* w
       p.ldv = s.hidden;
       p.n = p.nv = (int32_t)s.hidden;
       p.ku = p.kv = (int32_t)n;
-      p.ksteps = (int32_t)((n + 63) / 64);
       // fp32 sums of all blocks but the last: in dW itself, or in the workspace
       const bool last = b + 1 == f.blocks, own = c.dw_f32 || last;
       p.out = own ? c.dw : sum;
