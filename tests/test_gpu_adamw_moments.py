@@ -74,3 +74,23 @@ def test_values_beside_m(offset):
     assert np.array_equal(v.cpu().numpy(), t.v0.astype(np.float32))
     ccl.ccl_adamw_moments(t.n, None, None, t.v, t.vsc, None, alone)
     assert np.array_equal(alone.cpu().numpy(), OT.moment_decode(t.vc, t.vs, 5).astype(np.float32))
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-30])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_subnormal_v(bits, eps):
+    """Gradients whose squares are fp32's subnormal numbers: the first step is lr of their sign, v carrying half a step of
+    2^-149 for its square and its product each, which is 1.5 2^-149 / v of it at most (b2 = 0.5: v = g^2 / 2), half of that its root."""
+    g = torch.tensor([1e-18, -1e-19, 3e-20, -1e-20] * 32, device="cuda")
+    n = g.numel()
+    if bits == 8:       # one size a block
+        g = torch.cat([torch.full((128,), x, device="cuda") for x in (1e-18, -1e-19, 3e-20, -1e-20)])
+        n = g.numel()
+    p = torch.zeros(n, device="cuda")
+    m, v = (torch.zeros(n, device="cuda", dtype=torch.uint8 if bits == 8 else torch.float32) for _ in range(2))
+    scales = [torch.zeros(-(-n // 128), device="cuda", dtype=torch.uint8) for _ in range(2)]
+    entry = ccl.ccl_adamw_tensor(p, g, m, v, exp_avg_scale=scales[0], exp_avg_sq_scale=scales[1])
+    ccl.ccl_adamw_step(ccl.ccl_adamw([entry]), step=1, lr=1e-3, beta1=0.9, beta2=0.5, eps=eps)
+    g = g.double().cpu().numpy()
+    size = 0.75 * 2.0 ** -149 / (g * g / 2) + 2.0 ** -20 + eps / np.abs(g)
+    assert (np.abs(p.double().cpu().numpy() + 1e-3 * np.sign(g)) <= 1e-3 * size * 1.01).all()
