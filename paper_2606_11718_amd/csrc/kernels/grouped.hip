@@ -14,7 +14,9 @@
 // its down projection's gradient 205 us (3.6 TB/s), dW of 1536 x 2048 368 us (2.8 TB/s);
 // 800 rows over 128 of 768 -> 2048 74 us (5.5 TB/s, as a copy). dW of one row an
 // expert, which is its stores alone, takes 160 us, and each 64 rows more 45 to 65:
-// loads wait behind the stores of the tile before.
+// loads wait behind the stores of the tile before. Without an activation: forward of 768
+// -> 2048 181 us (3.3 TB/s), gradient of 1536 -> 2048 341 us (3.1 TB/s). dW of 1536 x
+// 2048 added to in bf16 495 us (3.7 TB/s), in fp32 560 (3.3), added to in fp32 748 (4.6).
 #include "product.hpp"
 
 #include "train_kernels.hpp"
