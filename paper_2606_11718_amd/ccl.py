@@ -621,8 +621,10 @@ def ccl_cross_entropy_workspace(vocab: _Vocab, tokens: int, *, grad: bool = Fals
 
 def _vocab_weight(vocab: _Vocab, W, bf16) -> int:
     """Address of W, vocab x hidden with its rows as the description says."""
-    W, ld = _rows("W", W, vocab.w_ld if W is None or isinstance(W, int) else None, vocab.vocab, vocab.hidden, bf16)
-    if ld != (vocab.w_ld or vocab.hidden) and vocab.vocab > 1 and ld != 0:
+    if W is None or isinstance(W, int):
+        return W or 0
+    W, ld = _rows("W", W, None, vocab.vocab, vocab.hidden, bf16)
+    if vocab.vocab > 1 and ld != (vocab.w_ld or vocab.hidden):
         _refuse("W", f"rows {ld} apart, not {vocab.w_ld or vocab.hidden}")
     return W
 

@@ -272,6 +272,20 @@ def test_tensors_of_another_device():
     _refused(INV, ccl.ccl_adamw_moments, 130, b8(130), b8(2), b8(130), b8(2), f(130), f(130))
 
 
+def test_rows_of_the_output_matrix(monkeypatch):
+    """W's rows lie as the description says: one row expanded to all (stride 0), rows with gaps, or rows without the gaps
+    that w_ld names are refused; the calls would read behind them."""
+    monkeypatch.setattr(ccl, "_here", lambda **tensors: None)
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+    for w_ld, bad in ((0, bf(1, 64).expand(1000, 64)), (64, bf(1, 64).expand(1000, 64)), (0, bf(1000, 72)[:, :64]),
+                      (72, bf(1000, 64)), (72, bf(1, 64).expand(1000, 64))):
+        v = ccl.ccl_vocab(**{**VOCAB, "w_ld": w_ld})
+        for call in (lambda: ccl.ccl_cross_entropy(v, 10, P, bad, P, P, workspace=P, workspace_bytes=1 << 40),  # noqa: B023
+                     lambda: ccl.ccl_cross_entropy_grad(v, 10, P, bad, P, P, P, P, workspace=P, workspace_bytes=1 << 40)):  # noqa: B023
+            with pytest.raises(ccl.CCLError, match="W: rows"):
+                call()
+
+
 def test_workspace_tensors(monkeypatch):
     """A tensor smaller than the bytes it is given for, or with gaps, is refused, whatever it is on."""
     monkeypatch.setattr(ccl, "_here", lambda **tensors: None)
