@@ -11,8 +11,8 @@
 //
 // 8-bit moments: 128 elements share a power of two, from the largest exponent
 // among them. m is a sign, 4 exponent and 3 mantissa bits; v, never negative, 5
-// and 3: its smallest value has the square root of m's smallest, both 2^-16 of the
-// largest's power of two. Rounded up or down at random (a hash of the element's
+// and 3: m's smallest value is 2^-16 of the largest's power of two, v's 2^-32, whose
+// root is 2^-16. Rounded up or down at random (a hash of the element's
 // place and the step, so the same call gives the same bits): b2 = 0.999 moves v
 // by a thousandth of itself a step, which rounding to the nearest of 3 mantissa
 // bits would undo every time. Below its smallest value an m is then rounded up with
